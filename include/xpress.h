@@ -356,6 +356,144 @@ int xpress_profile_train(const xpress_refiner *refiner, const xpress_train_in *i
 int xpress_debug_gemm(const void *A, int a_mn, const void *B, int b_mn, int M, int N, int K, float *C, int accumulate,
                       void *stream);
 
+/* ------------------------------------------------------------------------
+ * The drafter's head in 8 bits, and the request's rules on its logits: what a
+ * serving loop runs between the drafter's last layer and xpress_refine_block
+ * (norm -> 8-bit LM head -> rules -> refinement), and on the target's logits
+ * before xpress_accept.  The paper has no counterpart to these entry points.
+ * Unlike the calls above they take row pitches (in elements), so rows may be
+ * padded or be slices of wider ones; columns are contiguous.  Outputs may not
+ * overlap inputs or each other unless an entry point says so. */
+
+/* Root-mean-square norm with the residual's addition and an 8-bit output:
+ *   t     = x + residual                          (t = x without a residual)
+ *   y     = t / sqrt(mean_i t_i^2 + eps) * weight
+ *   scale = max(max_{i in g} |y_i| / 448, 2^-126)  for each group g of 128
+ *           consecutive elements of a row (the last group may be shorter)
+ *   q     = e4m3(y / scale)                        (nearest even)
+ * in fp32, every output rounded once from it (the norm is of the unrounded
+ * sum).  sum, y and (q, scale) are optional; at least one is given.  sum and y
+ * may be the same memory as x or residual (same pitch).  A row with a NaN or
+ * an infinity gives NaNs, as the formula does; a NaN in a group shows in its
+ * scale.  rows = 0 does nothing.
+ * Errors: INVALID_ARG (NULL x / weight, no output, q without scale, a pitch
+ * below the row's length, misaligned pointers, eps < 0), UNSUPPORTED (dtype, H
+ * above 2^30), CUDA. */
+typedef struct {
+    int rows, H;
+    int dtype;              /* xpress_dtype of x, residual, weight, sum, y */
+    float eps;
+    const void *x;          /* [rows, H], pitch ldx */
+    int64_t ldx;
+    const void *residual;   /* [rows, H] or NULL */
+    int64_t ldr;
+    const void *weight;     /* [H] */
+    void *sum;              /* [rows, H] or NULL: t */
+    int64_t lds;
+    void *y;                /* [rows, H] or NULL */
+    int64_t ldy;
+    void *q;                /* [rows, H] e4m3 or NULL */
+    int64_t ldq;
+    float *scale;           /* [rows, ceil(H / 128)], with q */
+    int64_t ldscale;
+} xpress_norm_args;
+int xpress_rmsnorm(const xpress_norm_args *args, void *stream);
+
+/* Weights for xpress_matmul_fp8: each 128 x 128 block of W [rows, cols] (pitch
+ * ldw) gets scale = max(max |W| / 448, 2^-126) and q = e4m3(W / scale).
+ * scale: [ceil(rows / 128), ceil(cols / 128)], contiguous.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, a side above 2^30, 2^31 blocks
+ * or more), CUDA. */
+int xpress_quantize_weight(const void *W, int dtype, int rows, int cols, int64_t ldw, void *q, int64_t ldq,
+                           float *scale, void *stream);
+
+/* Block-scaled 8-bit matrix product (e.g. the base logits s = W_lm h):
+ *   out[m][n] = sum_kb a_scale[m][kb] w_scale[n / 128][kb]
+ *               sum_{k in block kb} a[m][k] w[n][k]
+ * a [M, K] and w [N, K] e4m3, K blocks of 128 (the last may be shorter), fp32
+ * sums, one rounding to out's type.  Any M >= 0, N, K >= 1 with K <= 65536;
+ * a and w 16-byte aligned with pitches that are multiples of 16 (the padding
+ * is never used).  workspace: xpress_matmul_fp8_workspace_size() bytes,
+ * 256-byte aligned, zeroed once by the caller; it only holds the status word
+ * (xpress_get_device_status reads and clears it) and may be shared by calls.
+ * Reproducible: the order of every sum is fixed.
+ * Errors: INVALID_ARG, UNSUPPORTED (out_dtype, K above 65536, M or N
+ * above 2^30), WORKSPACE, CUDA. */
+typedef struct {
+    int M, N, K;
+    int out_dtype;          /* xpress_dtype */
+    const void *a;          /* [M, K] e4m3, pitch lda */
+    int64_t lda;
+    const float *a_scale;   /* [M, ceil(K / 128)] */
+    int64_t ld_a_scale;
+    const void *w;          /* [N, K] e4m3, pitch ldw */
+    int64_t ldw;
+    const float *w_scale;   /* [ceil(N / 128), ceil(K / 128)] */
+    int64_t ld_w_scale;
+    void *out;              /* [M, N], pitch ldo */
+    int64_t ldo;
+} xpress_matmul_args;
+size_t xpress_matmul_fp8_workspace_size(void);
+int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws_bytes, void *stream);
+
+/* The request's rules on logits, and the first maximum of the row that
+ * results.  logits holds n_seq * rows rows of V; row j of sequence q is row
+ * q * rows + j (rows = 1: the next token; B: the base logits of a block;
+ * B + 1: the target's rows of a block).  With c the number of times token v
+ * was answered -- in history after the prompt, and among draft[q][0 .. j-1] --
+ * and seen = c > 0 or v in the prompt:
+ *   l <- (l > 0 ? l / repetition : l * repetition)   if seen
+ *   l <- l - frequency c - presence [c > 0]
+ *   l <- l + bias_v
+ *   l <- mask_value                                  if the mask forbids v
+ * fp32, one rounding to the storage type.  Every rule is optional (NULL).  Ids
+ * outside [0, V) in history, draft and bias_ids count for nothing (-1 can fill
+ * gaps); of two bias entries for one id the later one counts.
+ *   argmax  [n_seq * rows] or NULL: the smallest id among the largest values
+ *           of the stored row, over the ids that its mask allows and whose
+ *           value is not NaN; -1 if there is none (a mask that allows nothing
+ *           leaves the whole row at mask_value)
+ *   mask    [mask_rows, ld_mask] words of 32 ids, bit v % 32 of word v / 32
+ *           set = allowed; row n is masked by mask row mask_row[n] (mask_row
+ *           NULL: by row n), and not at all where that is not in
+ *           [0, mask_rows)
+ * xpress_refine_block takes rows with a finite mask_value (e.g. -1e30), so
+ * that a row that its mask left empty still has a token.
+ * out may be logits (same pitch) or NULL (argmax only).  workspace: >=
+ * xpress_process_logits_workspace_size bytes, 256-byte aligned, needed for
+ * argmax only (else it may be NULL).
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, n_seq above 65535, V above
+ * 2^30), WORKSPACE, CUDA. */
+typedef struct {
+    int n_seq, rows, V;
+    int dtype;                       /* xpress_dtype of logits and out */
+    const void *logits;              /* [n_seq * rows, V], pitch ld */
+    int64_t ld;
+    void *out;
+    int64_t ldo;
+    int32_t *argmax;
+    const float *repetition;         /* [n_seq] > 0 */
+    const float *frequency;          /* [n_seq] */
+    const float *presence;           /* [n_seq] */
+    const int32_t *history;          /* tokens of all sequences, back to back */
+    int64_t n_history;               /* tokens in history: offsets are cut to [0, n_history] */
+    const int64_t *history_offsets;  /* [n_seq + 1] */
+    const int32_t *prompt_len;       /* [n_seq] leading history tokens that are the prompt; NULL: none */
+    const int32_t *draft;            /* [n_seq, >= rows - 1], pitch ld_draft */
+    int64_t ld_draft;
+    const int32_t *bias_ids;         /* entries of all sequences, back to back */
+    const float *bias_values;
+    int64_t n_bias;                  /* entries: offsets are cut to [0, n_bias] */
+    const int64_t *bias_offsets;     /* [n_seq + 1] */
+    const int32_t *mask;
+    int64_t ld_mask;
+    int mask_rows;
+    const int32_t *mask_row;         /* [n_seq * rows] or NULL */
+    float mask_value;
+} xpress_logits_args;
+size_t xpress_process_logits_workspace_size(int n_seq, int rows, int V);
+int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_t ws_bytes, void *stream);
+
 const char *xpress_status_string(int status);
 int xpress_version(void);
 

@@ -60,6 +60,31 @@ class XpressTrainOut(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("loss", "gW_e", "gW_h", "gW_g", "gW_in", "gL", "gW1", "gW2", "gW_r")]
 
 
+class XpressNormArgs(C.Structure):
+    _fields_ = [("rows", C.c_int), ("H", C.c_int), ("dtype", C.c_int), ("eps", C.c_float), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("residual", C.c_void_p), ("ldr", C.c_int64), ("weight", C.c_void_p),
+                ("sum", C.c_void_p), ("lds", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64), ("q", C.c_void_p),
+                ("ldq", C.c_int64), ("scale", C.c_void_p), ("ldscale", C.c_int64)]
+
+
+class XpressMatmulArgs(C.Structure):
+    _fields_ = [("M", C.c_int), ("N", C.c_int), ("K", C.c_int), ("out_dtype", C.c_int), ("a", C.c_void_p),
+                ("lda", C.c_int64), ("a_scale", C.c_void_p), ("ld_a_scale", C.c_int64), ("w", C.c_void_p),
+                ("ldw", C.c_int64), ("w_scale", C.c_void_p), ("ld_w_scale", C.c_int64), ("out", C.c_void_p),
+                ("ldo", C.c_int64)]
+
+
+class XpressLogitsArgs(C.Structure):
+    _fields_ = [("n_seq", C.c_int), ("rows", C.c_int), ("V", C.c_int), ("dtype", C.c_int), ("logits", C.c_void_p),
+                ("ld", C.c_int64), ("out", C.c_void_p), ("ldo", C.c_int64), ("argmax", C.c_void_p),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("history", C.c_void_p), ("n_history", C.c_int64), ("history_offsets", C.c_void_p),
+                ("prompt_len", C.c_void_p), ("draft", C.c_void_p), ("ld_draft", C.c_int64), ("bias_ids", C.c_void_p),
+                ("bias_values", C.c_void_p), ("n_bias", C.c_int64), ("bias_offsets", C.c_void_p),
+                ("mask", C.c_void_p), ("ld_mask", C.c_int64), ("mask_rows", C.c_int), ("mask_row", C.c_void_p),
+                ("mask_value", C.c_float)]
+
+
 _lib = None
 
 
@@ -117,6 +142,18 @@ def load(path: str = LIB_PATH):
     lib.xpress_profile_read_prepare.restype = I
     lib.xpress_profile_read.argtypes = [P, P, I, P]
     lib.xpress_profile_read.restype = I
+    lib.xpress_rmsnorm.argtypes = [C.POINTER(XpressNormArgs), P]
+    lib.xpress_rmsnorm.restype = I
+    lib.xpress_quantize_weight.argtypes = [P, I, I, I, C.c_int64, P, C.c_int64, P, P]
+    lib.xpress_quantize_weight.restype = I
+    lib.xpress_matmul_fp8_workspace_size.argtypes = []
+    lib.xpress_matmul_fp8_workspace_size.restype = S
+    lib.xpress_matmul_fp8.argtypes = [C.POINTER(XpressMatmulArgs), P, S, P]
+    lib.xpress_matmul_fp8.restype = I
+    lib.xpress_process_logits_workspace_size.argtypes = [I, I, I]
+    lib.xpress_process_logits_workspace_size.restype = S
+    lib.xpress_process_logits.argtypes = [C.POINTER(XpressLogitsArgs), P, S, P]
+    lib.xpress_process_logits.restype = I
     _lib = lib
     return lib
 
@@ -252,6 +289,239 @@ def xpress_profile_read_prepare(handle, ws_ptr: int, b: int, n_tokens: int, stre
 
 def xpress_profile_read(handle, ws_ptr: int, b: int, stream: int) -> None:
     _check("xpress_profile_read", load().xpress_profile_read(handle, C.c_void_p(ws_ptr), b, C.c_void_p(stream)))
+
+
+# ------------------------------------------- the drafter's head in 8 bits
+
+def _dtype_code(t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return XPRESS_BF16
+    if t.dtype is torch.float32:
+        return XPRESS_F32
+    raise ValueError(f"bfloat16 or float32 tensors are supported, not {t.dtype}")
+
+
+def _matrix(name, t, rows, cols, dtype, dev):
+    """Address and row pitch of the [rows, cols] device matrix t (rows may be
+    padded; columns are contiguous)."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name}: expected a {dtype} [{rows}, {cols}] tensor on cuda:{dev}, got {t.dtype} "
+                         f"{list(shape)} on {t.device}")
+    if cols > 1 and stride[1] != 1:
+        raise ValueError(f"{name}: columns must be contiguous (strides {list(stride)})")
+    # the pitch of a single row is never used
+    return t.data_ptr(), stride[0] if rows > 1 else (cols + 15) // 16 * 16
+
+
+def _vector(name, t, n, dtype, dev):
+    """Address of the contiguous device vector t of n elements (any n if None)."""
+    shape = t.shape
+    if len(shape) != 1 or (n is not None and shape[0] != n) or t.dtype is not dtype or t.get_device() != dev or \
+            (shape[0] > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: expected a contiguous {dtype} vector{'' if n is None else f' of {n}'} on cuda:{dev}, "
+                         f"got {t.dtype} {list(shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _launch_on(stream, dev, tensors):
+    """Stream handle for a call on `stream` (default: torch's current stream).
+    Memory used on another stream than the current one is kept from torch's
+    allocator until that stream is done with it."""
+    import torch
+    if dev < 0:
+        raise ValueError("the tensors have to be on a CUDA device")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    current = torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    return current
+
+
+def alloc_e4m3(rows: int, cols: int, device="cuda"):
+    """An uninitialised e4m3 matrix [rows, cols] whose rows start on 16 bytes,
+    as xpress_matmul_fp8 takes it."""
+    import torch
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+
+
+def rmsnorm(x, weight, eps: float = 1e-6, residual=None, sum_out=None, y_out=None, q_out=None, scale_out=None,
+            stream=None) -> int:
+    """Root-mean-square norm of x + residual with an 8-bit output (bf16 or fp32
+    x [rows, H], weight [H]; see xpress_rmsnorm): writes those of sum_out, y_out
+    (like x), q_out (e4m3 [rows, H], with scale_out fp32 [rows, ceil(H / 128)])
+    that are given.  Asynchronous; returns XPRESS_OK."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows, H]")
+    rows, H = x.shape
+    dt, dev = x.dtype, x.get_device()
+    a = XpressNormArgs(rows, H, _dtype_code(x), eps)
+    a.x, a.ldx = _matrix("x", x, rows, H, dt, dev)
+    a.weight = _vector("weight", weight, H, dt, dev)
+    if residual is not None:
+        a.residual, a.ldr = _matrix("residual", residual, rows, H, dt, dev)
+    if sum_out is not None:
+        a.sum, a.lds = _matrix("sum_out", sum_out, rows, H, dt, dev)
+    if y_out is not None:
+        a.y, a.ldy = _matrix("y_out", y_out, rows, H, dt, dev)
+    if q_out is not None:
+        if scale_out is None:
+            raise ValueError("q_out needs scale_out")
+        a.q, a.ldq = _matrix("q_out", q_out, rows, H, torch.float8_e4m3fn, dev)
+        a.scale, a.ldscale = _matrix("scale_out", scale_out, rows, (H + 127) // 128, torch.float32, dev)
+    st = _launch_on(stream, dev, (x, weight, residual, sum_out, y_out, q_out, scale_out))
+    if rows == 0:
+        return XPRESS_OK                         # empty tensors have no address
+    _check("xpress_rmsnorm", load().xpress_rmsnorm(a, st))
+    return XPRESS_OK
+
+
+def quantize_weight(W, q_out=None, scale_out=None, stream=None):
+    """e4m3 weights with a scale per 128 x 128 block from W [rows, cols] (bf16 or
+    fp32): returns (q, scale), allocated where not given."""
+    import torch
+    if W.dim() != 2:
+        raise ValueError("W: expected [rows, cols]")
+    rows, cols = W.shape
+    dev = W.get_device()
+    nrb, ncb = (rows + 127) // 128, (cols + 127) // 128
+    if q_out is None:
+        q_out = alloc_e4m3(rows, cols, W.device)
+    if scale_out is None:
+        scale_out = torch.empty((nrb, ncb), dtype=torch.float32, device=W.device)
+    code = _dtype_code(W)
+    p, ldw = _matrix("W", W, rows, cols, W.dtype, dev)
+    q, ldq = _matrix("q_out", q_out, rows, cols, torch.float8_e4m3fn, dev)
+    sc, lds = _matrix("scale_out", scale_out, nrb, ncb, torch.float32, dev)
+    if nrb > 1 and lds != ncb:
+        raise ValueError("scale_out must be contiguous")
+    st = _launch_on(stream, dev, (W, q_out, scale_out))
+    if rows:
+        _check("xpress_quantize_weight", load().xpress_quantize_weight(p, code, rows, cols, ldw, q, ldq, sc, st))
+    return q_out, scale_out
+
+
+_status_ws: dict = {}                            # per device: the zeroed workspace of matmul_fp8
+
+
+def _matmul_workspace(dev):
+    ws = _status_ws.get(dev)
+    if ws is None:
+        import torch
+        size = load().xpress_matmul_fp8_workspace_size()
+        buf = torch.zeros(size + 256, dtype=torch.uint8, device=f"cuda:{dev}")
+        torch.cuda.synchronize(dev)              # zero before a call on any stream uses it
+        ws = _status_ws[dev] = (buf, (buf.data_ptr() + 255) & ~255, size)
+    return ws
+
+
+def matmul_fp8(a, a_scale, w, w_scale, out, stream=None) -> int:
+    """out [M, N] (bf16 or fp32) = a w^T for e4m3 a [M, K] with a_scale fp32
+    [M, ceil(K / 128)] and e4m3 w [N, K] with w_scale fp32 [ceil(N / 128),
+    ceil(K / 128)] (see xpress_matmul_fp8).  Asynchronous; returns XPRESS_OK;
+    matmul_fp8_status() reads the device status of the calls so far."""
+    import torch
+    if a.dim() != 2 or w.dim() != 2:
+        raise ValueError("a: expected [M, K]; w: expected [N, K]")
+    M, K = a.shape
+    N = w.shape[0]
+    dev, kb = a.get_device(), (K + 127) // 128
+    g = XpressMatmulArgs(M, N, K, _dtype_code(out))
+    e4m3, f32 = torch.float8_e4m3fn, torch.float32
+    g.a, g.lda = _matrix("a", a, M, K, e4m3, dev)
+    g.a_scale, g.ld_a_scale = _matrix("a_scale", a_scale, M, kb, f32, dev)
+    g.w, g.ldw = _matrix("w", w, N, K, e4m3, dev)
+    g.w_scale, g.ld_w_scale = _matrix("w_scale", w_scale, (N + 127) // 128, kb, f32, dev)
+    g.out, g.ldo = _matrix("out", out, M, N, out.dtype, dev)
+    st = _launch_on(stream, dev, (a, a_scale, w, w_scale, out))
+    if M == 0:
+        return XPRESS_OK                         # empty tensors have no address
+    _, ws, size = _matmul_workspace(dev)
+    _check("xpress_matmul_fp8", load().xpress_matmul_fp8(g, ws, size, st))
+    return XPRESS_OK
+
+
+def matmul_fp8_status(device: int = 0, stream=None) -> int:
+    """Synchronises `stream` (default: torch's current stream), then reads and
+    clears the device status of the matmul_fp8 calls so far."""
+    import torch
+    st = stream if stream is not None else torch.cuda.current_stream(device)
+    return xpress_get_device_status(_matmul_workspace(device)[1], st.cuda_stream)
+
+
+def process_logits(logits, out=None, argmax_out=None, rows: int = 1, repetition=None, frequency=None, presence=None,
+                   history=None, history_offsets=None, prompt_len=None, draft=None, bias_ids=None, bias_values=None,
+                   bias_offsets=None, mask=None, mask_row=None, mask_value: float = float("-inf"), stream=None) -> int:
+    """The request's rules on logits [n_seq * rows, V] (bf16 or fp32) into out
+    (the same type; may be logits) and / or the first maximum of the resulting
+    rows into argmax_out int32 (see xpress_process_logits for the rules).
+    repetition / frequency / presence fp32 [n_seq]; history and bias_ids int32
+    and bias_values fp32, the sequences back to back, with int64 offsets
+    [n_seq + 1]; prompt_len int32 [n_seq]; draft int32 [n_seq, >= rows - 1];
+    mask int32 [mask rows, ceil(V / 32)]; mask_row int32 [n_seq * rows].
+    Asynchronous; returns XPRESS_OK."""
+    import torch
+    if logits.dim() != 2 or rows < 1 or logits.shape[0] % rows:
+        raise ValueError("logits: expected [n_seq * rows, V]")
+    n, V = logits.shape
+    n_seq, dev = n // rows, logits.get_device()
+    i32, f32, i64 = torch.int32, torch.float32, torch.int64
+    g = XpressLogitsArgs(n_seq, rows, V, _dtype_code(logits))
+    g.logits, g.ld = _matrix("logits", logits, n, V, logits.dtype, dev)
+    if out is not None:
+        g.out, g.ldo = _matrix("out", out, n, V, logits.dtype, dev)
+    if argmax_out is not None:
+        g.argmax = _vector("argmax_out", argmax_out, n, i32, dev)
+    if repetition is not None:
+        g.repetition = _vector("repetition", repetition, n_seq, f32, dev)
+    if frequency is not None:
+        g.frequency = _vector("frequency", frequency, n_seq, f32, dev)
+    if presence is not None:
+        g.presence = _vector("presence", presence, n_seq, f32, dev)
+    if history is not None:
+        if history_offsets is None:
+            raise ValueError("history needs history_offsets")
+        if history.numel():
+            g.history, g.n_history = _vector("history", history, None, i32, dev), history.numel()
+        g.history_offsets = _vector("history_offsets", history_offsets, n_seq + 1, i64, dev)
+        if prompt_len is not None:
+            g.prompt_len = _vector("prompt_len", prompt_len, n_seq, i32, dev)
+    if draft is not None and rows > 1:
+        if draft.dim() != 2 or draft.shape[1] < rows - 1:
+            raise ValueError(f"draft: expected at least {rows - 1} tokens per sequence")
+        g.draft, g.ld_draft = _matrix("draft", draft, n_seq, draft.shape[1], i32, dev)
+    if bias_ids is not None:
+        if bias_values is None or bias_offsets is None:
+            raise ValueError("bias_ids needs bias_values and bias_offsets")
+        if bias_ids.numel():
+            g.bias_ids, g.n_bias = _vector("bias_ids", bias_ids, None, i32, dev), bias_ids.numel()
+            g.bias_values = _vector("bias_values", bias_values, bias_ids.shape[0], f32, dev)
+            g.bias_offsets = _vector("bias_offsets", bias_offsets, n_seq + 1, i64, dev)
+    if mask is not None:
+        if mask.dim() != 2:
+            raise ValueError("mask: expected [mask rows, ceil(V / 32)]")
+        g.mask_rows = mask.shape[0]
+        if g.mask_rows:
+            g.mask, g.ld_mask = _matrix("mask", mask, g.mask_rows, (V + 31) // 32, i32, dev)
+        if mask_row is not None:
+            g.mask_row = _vector("mask_row", mask_row, n, i32, dev)
+    g.mask_value = mask_value
+    ws, ws_ptr, size = None, 0, 0
+    if argmax_out is not None and n:
+        size = load().xpress_process_logits_workspace_size(n_seq, rows, V)
+        ws = torch.empty(size, dtype=torch.uint8, device=logits.device)
+        ws_ptr = ws.data_ptr()                   # torch's blocks start on 512 bytes
+    st = _launch_on(stream, dev, (logits, out, argmax_out, repetition, frequency, presence, history, history_offsets,
+                                  prompt_len, draft, bias_ids, bias_values, bias_offsets, mask, mask_row, ws))
+    if n == 0:
+        return XPRESS_OK                         # empty tensors have no address
+    _check("xpress_process_logits", load().xpress_process_logits(g, ws_ptr, size, st))
+    return XPRESS_OK
 
 
 # ------------------------------------------------------------ torch helper

@@ -1,0 +1,140 @@
+// head.h -- what the kernels of the 8-bit drafter head share (rmsnorm.cu,
+// quant_fp8.cu, matmul_fp8.cu, logits.cu): the 8-bit conversion, 8-wide loads
+// and stores, and the host helpers of their entry points.
+#pragma once
+
+#include "common.cuh"
+#include "xpress.h"
+
+namespace xp {
+
+constexpr int MAX_DIM = 1 << 30;         // largest row or column count (index arithmetic in 32 bits)
+constexpr int QBLOCK = 128;              // elements along K (and weight rows) that share a scale
+constexpr float FP8_MAX = 448.0f;        // largest e4m3 value
+constexpr float MIN_SCALE = 1.17549435e-38f;   // 2^-126: the scale of an all-zero group
+
+// The scale of a group whose largest magnitude has the bits `amax_bits`
+// (magnitudes compare as unsigned words, and a NaN's word is above every
+// other's, so that a NaN in the group shows in its scale).
+__device__ __forceinline__ float group_scale(uint32_t amax_bits)
+{
+    const float s = __uint_as_float(amax_bits) / FP8_MAX;
+    return s < MIN_SCALE ? MIN_SCALE : s;
+}
+
+// Two values as e4m3 (nearest even, magnitudes above 448 become 448, NaN stays NaN).
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint8_t to_e4m3(float x) { return (uint8_t)to_e4m3x2(x, 0.0f); }
+
+// 8 consecutive elements at p (16-byte aligned) as fp32.
+__device__ __forceinline__ void load8(const uint16_t *p, float (&v)[8])
+{
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float *p, float (&v)[8])
+{
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    return (uint32_t)f2bf(lo) | ((uint32_t)f2bf(hi) << 16);
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8])
+{
+    *reinterpret_cast<uint4 *>(p) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8])
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store1(uint16_t *p, float v) { *p = f2bf(v); }
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ float load1(const uint16_t *p) { return bf2f(*p); }
+__device__ __forceinline__ float load1(const float *p) { return *p; }
+
+// Division by a group's scale.  x / s as x times 1 / s with the remainder put
+// back, q + (x - q s) / s, which rounds as the division does (ties between
+// e4m3 values are common: inputs of few bits over a scale made of one of them)
+// at a fraction of its instructions.  An infinite scale takes no remainder:
+// finite elements become 0 and infinite ones NaN, as x / s.
+struct ScaleDiv {
+    float inv, s;
+    __device__ __forceinline__ explicit ScaleDiv(float scale)
+        : inv(1.0f / scale), s(scale == INFINITY ? 0.0f : scale) {}
+    __device__ __forceinline__ float operator()(float x) const
+    {
+        const float q = x * inv;
+        return fmaf(fmaf(-q, s, x), inv, q);
+    }
+};
+
+// 8 values over their scale as e4m3 at p (8-byte aligned).
+__device__ __forceinline__ void store8_e4m3(uint8_t *p, const float (&v)[8], const ScaleDiv &d)
+{
+    const uint32_t lo = to_e4m3x2(d(v[0]), d(v[1])) | (to_e4m3x2(d(v[2]), d(v[3])) << 16);
+    const uint32_t hi = to_e4m3x2(d(v[4]), d(v[5])) | (to_e4m3x2(d(v[6]), d(v[7])) << 16);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(lo, hi);
+}
+
+// ------------------------------------------------------------------- host
+
+#define XH_CUDA(call)                                                                                          \
+    do {                                                                                                       \
+        if ((call) != cudaSuccess) {                                                                           \
+            (void)cudaGetLastError();                                                                          \
+            return XPRESS_ERR_CUDA;                                                                            \
+        }                                                                                                      \
+    } while (0)
+
+inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Launch with programmatic stream serialization (every kernel here waits with
+// griddepcontrol.wait before it touches global memory, so that its set-up
+// overlaps the end of the stream's previous kernel), optionally in clusters.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_head(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st,
+                        unsigned cluster, Args... args)
+{
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e;
+}
+
+// SMs of the current device (0 on an error).
+int current_sms();
+
+// 2-D byte tensor [rows][inner] with a row pitch of `pitch` bytes, 128-byte
+// swizzle, zero fill out of bounds (base 16-byte aligned, pitch a multiple of 16).
+bool tmap_bytes(CUtensorMap *m, const void *base, uint64_t inner, uint64_t rows, uint64_t pitch, uint32_t box_inner,
+                uint32_t box_rows);
+
+}  // namespace xp

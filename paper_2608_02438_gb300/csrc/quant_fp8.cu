@@ -1,0 +1,113 @@
+// quant_fp8.cu -- weights for the block-scaled 8-bit product: every 128 x 128
+// block of W gets the scale max(max |W| / 448, 2^-126) and its elements become
+// e4m3(W / scale).
+//
+// One CTA per block, which it holds in registers (64 elements per thread), so
+// W is read once; the only exchange is the block's largest magnitude.  HBM
+// bound.  Threads take 8 consecutive elements (16 lanes span a row of the
+// block) where rows start on 16 bytes, else single elements that are
+// consecutive across the warp.
+#include "head.h"
+
+namespace xp {
+
+namespace {
+
+constexpr int QT = 256;                  // threads: 8 warps
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(QT) k_quant_weight(const T *W, int64_t ldw, int rows, int cols, uint8_t *q,
+                                                      int64_t ldq, float *scale, int ncb)
+{
+    __shared__ uint32_t part[QT / 32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int rb = blockIdx.x / ncb, cb = blockIdx.x % ncb;
+    const int c0 = cb * QBLOCK;
+    pdl_trigger();
+    pdl_wait();
+    // VEC: slot i is row 16 i + thread / 16, columns 8 (thread % 16) + j;
+    // else slot i holds rows 16 i + 2 warp + (j / 4), columns 32 (j % 4) + lane
+    float v[8][8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (VEC) {
+            const int r = rb * QBLOCK + i * 16 + threadIdx.x / 16, c = c0 + (threadIdx.x % 16) * 8;
+            const T *p = W + (int64_t)r * ldw + c;
+            if (r < rows && c + 8 <= cols) load8(p, v[i]);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = r < rows && c + j < cols ? load1(p + j) : 0.0f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = rb * QBLOCK + i * 16 + 2 * warp + j / 4, c = c0 + (j % 4) * 32 + lane;
+                v[i][j] = r < rows && c < cols ? load1(W + (int64_t)r * ldw + c) : 0.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (lane == 0) part[warp] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < QT / 32; ++k) m = max(m, part[k]);
+    const float s = group_scale(m);
+    const ScaleDiv div(s);
+    if (threadIdx.x == 0) scale[blockIdx.x] = s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (VEC) {
+            const int r = rb * QBLOCK + i * 16 + threadIdx.x / 16, c = c0 + (threadIdx.x % 16) * 8;
+            uint8_t *p = q + (int64_t)r * ldq + c;
+            if (r < rows && c + 8 <= cols) store8_e4m3(p, v[i], div);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (r < rows && c + j < cols) p[j] = to_e4m3(div(v[i][j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = rb * QBLOCK + i * 16 + 2 * warp + j / 4, c = c0 + (j % 4) * 32 + lane;
+                if (r < rows && c < cols) q[(int64_t)r * ldq + c] = to_e4m3(div(v[i][j]));
+            }
+        }
+    }
+}
+
+template <typename T>
+cudaError_t launch_quant(const void *W, int64_t ldw, int rows, int cols, uint8_t *q, int64_t ldq, float *scale,
+                         cudaStream_t st)
+{
+    const int nrb = (rows + QBLOCK - 1) / QBLOCK, ncb = (cols + QBLOCK - 1) / QBLOCK;
+    const bool vec = aligned(W, 16) && ldw * sizeof(T) % 16 == 0 && aligned(q, 8) && ldq % 8 == 0;
+    auto *k = vec ? k_quant_weight<T, true> : k_quant_weight<T, false>;
+    return launch_head(k, dim3((unsigned)((int64_t)nrb * ncb)), QT, 0, st, 1, static_cast<const T *>(W), ldw, rows, cols,
+                       q, ldq, scale, ncb);
+}
+
+}  // namespace
+}  // namespace xp
+
+using namespace xp;
+
+extern "C" int xpress_quantize_weight(const void *W, int dtype, int rows, int cols, int64_t ldw, void *q, int64_t ldq,
+                                      float *scale, void *stream)
+{
+    if (!W || !q || !scale || rows < 0 || cols < 1 || ldw < cols || ldq < cols) return XPRESS_ERR_INVALID_ARG;
+    if (dtype != XPRESS_F32 && dtype != XPRESS_BF16) return XPRESS_ERR_UNSUPPORTED;
+    const uintptr_t es = dtype == XPRESS_BF16 ? 2 : 4;
+    if (!aligned(W, es) || !aligned(scale, 4)) return XPRESS_ERR_INVALID_ARG;
+    if (rows == 0) return XPRESS_OK;
+    if (rows > MAX_DIM || cols > MAX_DIM ||
+        (int64_t)((rows + QBLOCK - 1) / QBLOCK) * ((cols + QBLOCK - 1) / QBLOCK) > 0x7fffffff)
+        return XPRESS_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t *qb = static_cast<uint8_t *>(q);
+    XH_CUDA(dtype == XPRESS_BF16 ? launch_quant<uint16_t>(W, ldw, rows, cols, qb, ldq, scale, st)
+                                 : launch_quant<float>(W, ldw, rows, cols, qb, ldq, scale, st));
+    return XPRESS_OK;
+}

@@ -4,6 +4,7 @@
 // reduce kernel updates after every pass).
 #include <cudaTypedefs.h>
 
+#include <atomic>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -11,6 +12,7 @@
 #include <mutex>
 #include <new>
 
+#include "head.h"
 #include "kernels.h"
 #include "xpress.h"
 
@@ -1017,6 +1019,35 @@ cudaStream_t refiner_train_aux(const xpress_refiner *R, cudaEvent_t (&ev)[4])
 bool tmap_bf16_kblocks(CUtensorMap *m, const void *base, uint64_t rows, uint32_t box_rows)
 {
     return make_tmap_bf16_kblocks(m, base, rows, box_rows);
+}
+
+bool tmap_bytes(CUtensorMap *m, const void *base, uint64_t inner, uint64_t rows, uint64_t pitch, uint32_t box_inner,
+                uint32_t box_rows)
+{
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    cuuint64_t dims[2] = {inner, rows};
+    cuuint64_t strides[1] = {pitch};
+    cuuint32_t box[2] = {box_inner, box_rows};
+    cuuint32_t es[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int current_sms()
+{
+    constexpr int MAX_DEVICES = 64;
+    static std::atomic<int> sms[MAX_DEVICES];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    if (dev < MAX_DEVICES && (n = sms[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    if (dev < MAX_DEVICES) sms[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 bool tmap_bf16(CUtensorMap *m, const void *base, uint64_t inner, uint64_t outer, uint64_t pitch, uint32_t box_inner,
