@@ -293,53 +293,43 @@ def xpress_profile_read(handle, ws_ptr: int, b: int, stream: int) -> None:
 
 # ------------------------------------------- the drafter's head in 8 bits
 
-def _dtype_code(t):
-    import torch
-    if t.dtype is torch.bfloat16:
-        return XPRESS_BF16
-    if t.dtype is torch.float32:
-        return XPRESS_F32
-    raise ValueError(f"bfloat16 or float32 tensors are supported, not {t.dtype}")
+EXT_PATH = os.path.join(HERE, "_build", "xpress_torch.so")
+_ext = None
 
 
-def _matrix(name, t, rows, cols, dtype, dev):
-    """Address and row pitch of the [rows, cols] device matrix t (rows may be
-    padded; columns are contiguous)."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or shape[0] != rows or shape[1] != cols or t.dtype is not dtype or t.get_device() != dev:
-        raise ValueError(f"{name}: expected a {dtype} [{rows}, {cols}] tensor on cuda:{dev}, got {t.dtype} "
-                         f"{list(shape)} on {t.device}")
-    if cols > 1 and stride[1] != 1:
-        raise ValueError(f"{name}: columns must be contiguous (strides {list(stride)})")
-    # the pitch of a single row is never used
-    return t.data_ptr(), stride[0] if rows > 1 else (cols + 15) // 16 * 16
+def _load_ext():
+    """The torch side of the calls below (csrc/torch_ext.cpp): it checks the
+    tensors -- ValueError names the one that does not fit -- and calls the
+    library on torch's current stream."""
+    global _ext
+    import importlib.util
+
+    import torch  # noqa: F401  (its libraries come first)
+    load()
+    if not os.path.exists(EXT_PATH):
+        raise RuntimeError(f"{EXT_PATH} is missing: run paper_2608_02438_gb300.build.build() first")
+    spec = importlib.util.spec_from_file_location("xpress_torch", EXT_PATH)
+    _ext = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(_ext)
+    return _ext
 
 
-def _vector(name, t, n, dtype, dev):
-    """Address of the contiguous device vector t of n elements (any n if None)."""
-    shape = t.shape
-    if len(shape) != 1 or (n is not None and shape[0] != n) or t.dtype is not dtype or t.get_device() != dev or \
-            (shape[0] > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: expected a contiguous {dtype} vector{'' if n is None else f' of {n}'} on cuda:{dev}, "
-                         f"got {t.dtype} {list(shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _launch_on(stream, dev, tensors):
-    """Stream handle for a call on `stream` (default: torch's current stream).
-    Memory used on another stream than the current one is kept from torch's
-    allocator until that stream is done with it."""
-    import torch
-    if dev < 0:
-        raise ValueError("the tensors have to be on a CUDA device")
-    if dev != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
-    current = torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-    return current
+def _call(name, stream, *args):
+    """One call of the extension, on `stream` if given (memory used there is
+    kept from torch's allocator until that stream is done with it)."""
+    f = getattr(_ext or _load_ext(), name)
+    if stream is None:
+        code = f(*args)
+    else:
+        import torch
+        with torch.cuda.stream(stream):
+            code = f(*args)
+            for t in args:
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+    if code:
+        _check("xpress_" + name, code)
+    return XPRESS_OK
 
 
 def alloc_e4m3(rows: int, cols: int, device="cuda"):
@@ -355,69 +345,24 @@ def rmsnorm(x, weight, eps: float = 1e-6, residual=None, sum_out=None, y_out=Non
     x [rows, H], weight [H]; see xpress_rmsnorm): writes those of sum_out, y_out
     (like x), q_out (e4m3 [rows, H], with scale_out fp32 [rows, ceil(H / 128)])
     that are given.  Asynchronous; returns XPRESS_OK."""
-    import torch
-    if x.dim() != 2:
-        raise ValueError("x: expected [rows, H]")
-    rows, H = x.shape
-    dt, dev = x.dtype, x.get_device()
-    a = XpressNormArgs(rows, H, _dtype_code(x), eps)
-    a.x, a.ldx = _matrix("x", x, rows, H, dt, dev)
-    a.weight = _vector("weight", weight, H, dt, dev)
-    if residual is not None:
-        a.residual, a.ldr = _matrix("residual", residual, rows, H, dt, dev)
-    if sum_out is not None:
-        a.sum, a.lds = _matrix("sum_out", sum_out, rows, H, dt, dev)
-    if y_out is not None:
-        a.y, a.ldy = _matrix("y_out", y_out, rows, H, dt, dev)
-    if q_out is not None:
-        if scale_out is None:
-            raise ValueError("q_out needs scale_out")
-        a.q, a.ldq = _matrix("q_out", q_out, rows, H, torch.float8_e4m3fn, dev)
-        a.scale, a.ldscale = _matrix("scale_out", scale_out, rows, (H + 127) // 128, torch.float32, dev)
-    st = _launch_on(stream, dev, (x, weight, residual, sum_out, y_out, q_out, scale_out))
-    if rows == 0:
-        return XPRESS_OK                         # empty tensors have no address
-    _check("xpress_rmsnorm", load().xpress_rmsnorm(a, st))
-    return XPRESS_OK
+    return _call("rmsnorm", stream, x, weight, eps, residual, sum_out, y_out, q_out, scale_out)
 
 
 def quantize_weight(W, q_out=None, scale_out=None, stream=None):
     """e4m3 weights with a scale per 128 x 128 block from W [rows, cols] (bf16 or
     fp32): returns (q, scale), allocated where not given."""
-    import torch
-    if W.dim() != 2:
-        raise ValueError("W: expected [rows, cols]")
-    rows, cols = W.shape
-    dev = W.get_device()
-    nrb, ncb = (rows + 127) // 128, (cols + 127) // 128
-    if q_out is None:
-        q_out = alloc_e4m3(rows, cols, W.device)
-    if scale_out is None:
-        scale_out = torch.empty((nrb, ncb), dtype=torch.float32, device=W.device)
-    code = _dtype_code(W)
-    p, ldw = _matrix("W", W, rows, cols, W.dtype, dev)
-    q, ldq = _matrix("q_out", q_out, rows, cols, torch.float8_e4m3fn, dev)
-    sc, lds = _matrix("scale_out", scale_out, nrb, ncb, torch.float32, dev)
-    if nrb > 1 and lds != ncb:
-        raise ValueError("scale_out must be contiguous")
-    st = _launch_on(stream, dev, (W, q_out, scale_out))
-    if rows:
-        _check("xpress_quantize_weight", load().xpress_quantize_weight(p, code, rows, cols, ldw, q, ldq, sc, st))
-    return q_out, scale_out
+    if W.dim() == 2 and (q_out is None or scale_out is None):
+        import contextlib
 
-
-_status_ws: dict = {}                            # per device: the zeroed workspace of matmul_fp8
-
-
-def _matmul_workspace(dev):
-    ws = _status_ws.get(dev)
-    if ws is None:
         import torch
-        size = load().xpress_matmul_fp8_workspace_size()
-        buf = torch.zeros(size + 256, dtype=torch.uint8, device=f"cuda:{dev}")
-        torch.cuda.synchronize(dev)              # zero before a call on any stream uses it
-        ws = _status_ws[dev] = (buf, (buf.data_ptr() + 255) & ~255, size)
-    return ws
+        rows, cols = W.shape
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            if q_out is None:
+                q_out = alloc_e4m3(rows, cols, W.device)
+            if scale_out is None:
+                scale_out = torch.empty(((rows + 127) // 128, (cols + 127) // 128), dtype=torch.float32, device=W.device)
+    _call("quantize_weight", stream, W, q_out, scale_out)
+    return q_out, scale_out
 
 
 def matmul_fp8(a, a_scale, w, w_scale, out, stream=None) -> int:
@@ -425,33 +370,15 @@ def matmul_fp8(a, a_scale, w, w_scale, out, stream=None) -> int:
     [M, ceil(K / 128)] and e4m3 w [N, K] with w_scale fp32 [ceil(N / 128),
     ceil(K / 128)] (see xpress_matmul_fp8).  Asynchronous; returns XPRESS_OK;
     matmul_fp8_status() reads the device status of the calls so far."""
-    import torch
-    if a.dim() != 2 or w.dim() != 2:
-        raise ValueError("a: expected [M, K]; w: expected [N, K]")
-    M, K = a.shape
-    N = w.shape[0]
-    dev, kb = a.get_device(), (K + 127) // 128
-    g = XpressMatmulArgs(M, N, K, _dtype_code(out))
-    e4m3, f32 = torch.float8_e4m3fn, torch.float32
-    g.a, g.lda = _matrix("a", a, M, K, e4m3, dev)
-    g.a_scale, g.ld_a_scale = _matrix("a_scale", a_scale, M, kb, f32, dev)
-    g.w, g.ldw = _matrix("w", w, N, K, e4m3, dev)
-    g.w_scale, g.ld_w_scale = _matrix("w_scale", w_scale, (N + 127) // 128, kb, f32, dev)
-    g.out, g.ldo = _matrix("out", out, M, N, out.dtype, dev)
-    st = _launch_on(stream, dev, (a, a_scale, w, w_scale, out))
-    if M == 0:
-        return XPRESS_OK                         # empty tensors have no address
-    _, ws, size = _matmul_workspace(dev)
-    _check("xpress_matmul_fp8", load().xpress_matmul_fp8(g, ws, size, st))
-    return XPRESS_OK
+    return _call("matmul_fp8", stream, a, a_scale, w, w_scale, out)
 
 
-def matmul_fp8_status(device: int = 0, stream=None) -> int:
+def matmul_fp8_status(stream=None) -> int:
     """Synchronises `stream` (default: torch's current stream), then reads and
-    clears the device status of the matmul_fp8 calls so far."""
+    clears the device status of the matmul_fp8 calls so far on this device."""
     import torch
-    st = stream if stream is not None else torch.cuda.current_stream(device)
-    return xpress_get_device_status(_matmul_workspace(device)[1], st.cuda_stream)
+    st = stream if stream is not None else torch.cuda.current_stream()
+    return xpress_get_device_status((_ext or _load_ext()).matmul_fp8_workspace(), st.cuda_stream)
 
 
 def process_logits(logits, out=None, argmax_out=None, rows: int = 1, repetition=None, frequency=None, presence=None,
@@ -465,63 +392,8 @@ def process_logits(logits, out=None, argmax_out=None, rows: int = 1, repetition=
     [n_seq + 1]; prompt_len int32 [n_seq]; draft int32 [n_seq, >= rows - 1];
     mask int32 [mask rows, ceil(V / 32)]; mask_row int32 [n_seq * rows].
     Asynchronous; returns XPRESS_OK."""
-    import torch
-    if logits.dim() != 2 or rows < 1 or logits.shape[0] % rows:
-        raise ValueError("logits: expected [n_seq * rows, V]")
-    n, V = logits.shape
-    n_seq, dev = n // rows, logits.get_device()
-    i32, f32, i64 = torch.int32, torch.float32, torch.int64
-    g = XpressLogitsArgs(n_seq, rows, V, _dtype_code(logits))
-    g.logits, g.ld = _matrix("logits", logits, n, V, logits.dtype, dev)
-    if out is not None:
-        g.out, g.ldo = _matrix("out", out, n, V, logits.dtype, dev)
-    if argmax_out is not None:
-        g.argmax = _vector("argmax_out", argmax_out, n, i32, dev)
-    if repetition is not None:
-        g.repetition = _vector("repetition", repetition, n_seq, f32, dev)
-    if frequency is not None:
-        g.frequency = _vector("frequency", frequency, n_seq, f32, dev)
-    if presence is not None:
-        g.presence = _vector("presence", presence, n_seq, f32, dev)
-    if history is not None:
-        if history_offsets is None:
-            raise ValueError("history needs history_offsets")
-        if history.numel():
-            g.history, g.n_history = _vector("history", history, None, i32, dev), history.numel()
-        g.history_offsets = _vector("history_offsets", history_offsets, n_seq + 1, i64, dev)
-        if prompt_len is not None:
-            g.prompt_len = _vector("prompt_len", prompt_len, n_seq, i32, dev)
-    if draft is not None and rows > 1:
-        if draft.dim() != 2 or draft.shape[1] < rows - 1:
-            raise ValueError(f"draft: expected at least {rows - 1} tokens per sequence")
-        g.draft, g.ld_draft = _matrix("draft", draft, n_seq, draft.shape[1], i32, dev)
-    if bias_ids is not None:
-        if bias_values is None or bias_offsets is None:
-            raise ValueError("bias_ids needs bias_values and bias_offsets")
-        if bias_ids.numel():
-            g.bias_ids, g.n_bias = _vector("bias_ids", bias_ids, None, i32, dev), bias_ids.numel()
-            g.bias_values = _vector("bias_values", bias_values, bias_ids.shape[0], f32, dev)
-            g.bias_offsets = _vector("bias_offsets", bias_offsets, n_seq + 1, i64, dev)
-    if mask is not None:
-        if mask.dim() != 2:
-            raise ValueError("mask: expected [mask rows, ceil(V / 32)]")
-        g.mask_rows = mask.shape[0]
-        if g.mask_rows:
-            g.mask, g.ld_mask = _matrix("mask", mask, g.mask_rows, (V + 31) // 32, i32, dev)
-        if mask_row is not None:
-            g.mask_row = _vector("mask_row", mask_row, n, i32, dev)
-    g.mask_value = mask_value
-    ws, ws_ptr, size = None, 0, 0
-    if argmax_out is not None and n:
-        size = load().xpress_process_logits_workspace_size(n_seq, rows, V)
-        ws = torch.empty(size, dtype=torch.uint8, device=logits.device)
-        ws_ptr = ws.data_ptr()                   # torch's blocks start on 512 bytes
-    st = _launch_on(stream, dev, (logits, out, argmax_out, repetition, frequency, presence, history, history_offsets,
-                                  prompt_len, draft, bias_ids, bias_values, bias_offsets, mask, mask_row, ws))
-    if n == 0:
-        return XPRESS_OK                         # empty tensors have no address
-    _check("xpress_process_logits", load().xpress_process_logits(g, ws_ptr, size, st))
-    return XPRESS_OK
+    return _call("process_logits", stream, logits, out, argmax_out, rows, repetition, frequency, presence, history,
+                 history_offsets, prompt_len, draft, bias_ids, bias_values, bias_offsets, mask, mask_row, mask_value)
 
 
 # ------------------------------------------------------------ torch helper
