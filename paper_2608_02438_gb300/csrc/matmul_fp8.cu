@@ -22,29 +22,17 @@
 // cluster in rank order, so that the result does not depend on timing.
 #include <mutex>
 
-#include "head.h"
+#include "matmul_fp8.h"
 
 namespace xp {
 
 namespace {
-
-struct MmArgs {
-    int M, N, K, S;
-    const float *sa, *sw;
-    int64_t ldsa, ldsw, ldo;
-    void *out;
-    int bf16;
-    int stages;
-    uint32_t table_bytes;
-    int32_t *status;
-};
 
 constexpr int MM_BN = 128;                             // weight rows per tile
 constexpr int MM_EPI = 4;                              // epilogue warps
 constexpr int MM_THREADS = 32 * (2 + MM_EPI);
 constexpr uint32_t MM_W_STAGE = MM_BN * QBLOCK;        // 16 KB
 constexpr int MM_MAX_STAGES = 12;
-constexpr size_t MM_SMEM_LIMIT = 227 * 1024;
 
 template <int NT>
 struct MmShape {
@@ -52,7 +40,7 @@ struct MmShape {
     static constexpr uint32_t STAGE = MM_W_STAGE + A_STAGE;
     static constexpr int NBUF = 4;
     static constexpr uint32_t TMEM_COLS = NBUF * NT;   // a power of two from 64 to 256
-    static constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(MM_BN >> 4) << 24);
+    static constexpr uint32_t IDESC = idesc_e4m3(MM_BN, NT);
     static constexpr size_t PART = (size_t)NT * MM_BN * 4;    // sums of a K split
 };
 
@@ -91,21 +79,11 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *v)
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 // A float of CTA `rank`'s shared memory at this CTA's address `p`.
 __device__ __forceinline__ float ld_cluster(const float *p, uint32_t rank)
 {
-    uint32_t a;
     float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr(p, rank)) : "memory");
     return v;
 }
 
@@ -365,6 +343,7 @@ extern "C" int xpress_matmul_fp8(const xpress_matmul_args *in, void *ws, size_t 
     g.bf16 = in->out_dtype == XPRESS_BF16;
     g.status = static_cast<int32_t *>(ws);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (in->M > 64) return launch_mm_wide(g, in->a, in->lda, in->w, in->ldw, sms, st);
     if (in->M <= 16) return launch_mm<16>(g, in->a, in->lda, in->w, in->ldw, sms, st);
     return launch_mm<32>(g, in->a, in->lda, in->w, in->ldw, sms, st);
 }
