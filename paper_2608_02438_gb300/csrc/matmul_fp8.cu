@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
             for (int64_t it = first; it < items && ok; it += step) {
                 const int rb = (int)(it / NC), mc = (int)(it % NC);
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
+                    if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
                     uint8_t *dst = base + stage * Sh::STAGE;
                     mbar_expect_tx(&sh.full[stage], Sh::STAGE);
                     tma_load_2d(dst, &tmap_w, &sh.full[stage], kb * QBLOCK, rb * MM_BN);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
             // no copy may still be landing when the CTA leaves
             int dummy = 0;
             for (int st = 0; st < stages; ++st)
-                if (pending & (1u << st)) mbar_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, 100000000ull);
+                if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
         }
     } else if (warp == 1) {
         // ---------------------------------------------------- MMA issuer
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
             bool ok = true;
             for (int64_t it = first; it < items && ok; it += step) {
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait(&sh.tempty[buf], tphase ^ 1, abort) || !mbar_wait(&sh.full[stage], phase, abort)) {
+                    if (!mm_wait(&sh.tempty[buf], tphase ^ 1, abort) || !mm_wait(&sh.full[stage], phase, abort)) {
                         ok = false;
                         break;
                     }
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
             }
             tc_commit(&sh.drain);
             int dummy = 0;
-            mbar_wait(&sh.drain, 0, &dummy, 100000000ull);
+            mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
         }
         __syncwarp();
     } else {
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
                 const int i = kb - kb0;
                 if ((i & 31) == 0) sw32 = kb + lane < kb1 ? swr[kb + lane] : 0.0f;
                 const float sw = __shfl_sync(0xffffffffu, sw32, i & 31);
-                if (ok) ok = mbar_wait(&sh.tfull[buf], tphase, abort);
+                if (ok) ok = mm_wait(&sh.tfull[buf], tphase, abort);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();

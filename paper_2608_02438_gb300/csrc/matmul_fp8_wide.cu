@@ -9,13 +9,15 @@
 // block is 4 MMAs into one of two TMEM buffers of 256 columns; the epilogue
 // adds the other to the running sums with its scale.  With a's rows on the
 // lanes a thread has one scale per K block (its row's, times that of the
-// weight block its 128 columns are), and the addition is 64 packed FMAs.
+// weight block its columns are in).
 //
-// Roles (384 threads): warp 0 TMA producer (both CTAs load their own halves;
+// Roles (640 threads): warp 0 TMA producer (both CTAs load their own halves;
 // the copies complete on the leader's barrier), warp 1 TMEM allocator and, in
-// the leader, MMA issuer; warps 4-11 epilogue (lane quarter warp % 4, column
-// half (warp - 4) / 4) with the 128 sums of a thread in registers: the first
-// warpgroup hands its registers to theirs.
+// the leader, MMA issuer; warps 2-3 stage the products of the scales (128 rows
+// by the tile's 2 weight blocks, four K blocks at a time) in shared memory;
+// warps 4-19 epilogue (lane quarter warp % 4, 64 columns of it) with the 64
+// sums of a thread in registers: the first warpgroup hands registers to the
+// others.
 #include <mutex>
 
 #include "matmul_fp8.h"
@@ -25,22 +27,29 @@ namespace xp {
 namespace {
 
 constexpr int WD_BM = 256, WD_BN = 256;                 // tile of a pair
-constexpr int WD_EPI = 8;
+constexpr int WD_EPI = 16;
+constexpr int WD_COLS = WD_BN / (WD_EPI / 4);           // columns of an epilogue warp
 constexpr int WD_THREADS = 32 * (4 + WD_EPI);
-// registers per thread: the kernel is launched with 168 x 384 (the most that
-// 65,536 allow); 80 x 128 + 208 x 256 = 63,488 of those 64,512
-constexpr int WD_REGS_FEW = 80, WD_REGS_MANY = 208;
+// registers per thread: the kernel is launched with 96 x 640 (the most that
+// five warps of a sub-partition's 16,384 allow); 64 x 128 + 104 x 512 = 61,440
+// are all of them
+constexpr int WD_REGS_FEW = 64, WD_REGS_MANY = 104;
 constexpr uint32_t WD_HALF = 128 * QBLOCK;              // 16 KB: 128 rows of one operand
-constexpr uint32_t WD_STAGE = 2 * WD_HALF;
-constexpr int WD_STAGES = 6;
+constexpr int WD_SKB = 2;                               // K blocks of a stage
+constexpr uint32_t WD_STAGE = WD_SKB * 2 * WD_HALF;     // [operand][K block][128 rows][128 bytes]
+constexpr int WD_STAGES = 3;
 constexpr uint32_t WD_IDESC = idesc_e4m3(WD_BM, WD_BN);
-constexpr size_t WD_TILE = 32 * 33 * 4;                 // a warp's transpose
-constexpr size_t WD_SMEM = 1024 + WD_STAGES * WD_STAGE + WD_EPI * WD_TILE;
+constexpr int WD_TCOLS = 8;                             // columns of a transpose
+constexpr size_t WD_TILE = 32 * (WD_TCOLS + 1) * 4;
+constexpr int WD_GROUP = 4;                             // K blocks whose scales are staged together
+constexpr size_t WD_SCALES = WD_GROUP * 2 * 128 * 4;    // [K block][weight block][row]                 // a warp's transpose
+constexpr size_t WD_SMEM = 1024 + WD_STAGES * WD_STAGE + WD_EPI * WD_TILE + 2 * WD_SCALES;
 constexpr int WD_BAND = 16;                             // row tiles that share the weights while they are in L2
 
 struct WideBars {
     uint64_t full[WD_STAGES], empty[WD_STAGES];
     uint64_t tfull[2], tempty[2];
+    uint64_t sfull[2], sempty[2];
     uint64_t drain;
     uint32_t tmem_base;
     int abort;
@@ -52,6 +61,15 @@ __device__ __forceinline__ void tma_load_pair(void *dst, const CUtensorMap *map,
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
         "[%4];" ::"r"(smem_u32(dst)),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_pair_3d(void *dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+        "%4}], [%5];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
 
@@ -75,62 +93,25 @@ __device__ __forceinline__ void tc_commit_pair(uint64_t *bar)
         : "memory");
 }
 
-// mbar_wait for a barrier that the other CTA of the pair arrives on.
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *abort)
-{
-    unsigned long long t0 = 0;
-    for (uint32_t it = 0;; ++it) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
-            : "memory");
-        if (ok) return true;
-        if ((it & 7u) == 0) {
-            if (*abort) return false;
-            if (t0 == 0) t0 = globaltimer();
-            else if (globaltimer() - t0 > 2000000000ull) { *abort = 1; return false; }
-        }
-    }
-}
-
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// 32 TMEM columns of this warp's lane quarter.
-__device__ __forceinline__ void tmem_ld32w(uint32_t taddr, uint32_t (&r)[32])
+// 16 TMEM columns of this warp's lane quarter.
+__device__ __forceinline__ void tmem_ld16w(uint32_t taddr, float (&v)[16])
 {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
-        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15}, [%16];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
-          "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-          "=r"(r[30]), "=r"(r[31])
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr)
         : "memory");
-}
-
-// (a0, a1) += (d0, d1) * (f0, f1)
-__device__ __forceinline__ void fma2(uint64_t &a, uint32_t d0, uint32_t d1, uint64_t f)
-{
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(d0), "r"(d1));
-    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(d), "l"(f));
-}
-__device__ __forceinline__ void halves(uint64_t a, float &lo, float &hi)
-{
-    uint32_t l, h;
-    asm("mov.b64 {%0, %1}, %2;" : "=r"(l), "=r"(h) : "l"(a));
-    lo = __uint_as_float(l);
-    hi = __uint_as_float(h);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
@@ -138,6 +119,11 @@ __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
                  "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                  : "memory");
+}
+
+__device__ __forceinline__ bool aligned_dev(const void *p, uintptr_t a)
+{
+    return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }
 
 // Tile t in the order of bands of WD_BAND row tiles, within a band the row
@@ -154,7 +140,8 @@ __device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &mt, int 
 // grid: pairs of CTAs, WD_THREADS threads, WD_SMEM bytes; vec: out's rows start on 32 bytes.
 __global__ void __launch_bounds__(WD_THREADS, 1)
     k_matmul_fp8_wide(const __grid_constant__ MmArgs g, const __grid_constant__ CUtensorMap tmap_a,
-                      const __grid_constant__ CUtensorMap tmap_w, int vec)
+                      const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_a2,
+                      const __grid_constant__ CUtensorMap tmap_w2, int vec)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -168,6 +155,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < WD_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 2 * WD_EPI); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.sfull[i], 2); mbar_init(&sh.sempty[i], WD_EPI); }
         mbar_init(&sh.drain, 1);
         sh.abort = 0;
         fence_barrier_init();
@@ -187,6 +175,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
     volatile int *abort = &sh.abort;
+    float *scales = reinterpret_cast<float *>(base + WD_STAGES * WD_STAGE + WD_EPI * WD_TILE);
     pdl_trigger();
     pdl_wait();
 
@@ -202,13 +191,21 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                 int mt, nt;
                 tile_at(t, MT, NT, mt, nt);
                 const int row = mt * WD_BM + (int)rank * 128, col = nt * WD_BN + (int)rank * 128;
-                for (int kb = 0; kb < KB; ++kb) {
-                    if (!mbar_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
+                for (int kb = 0; kb < KB; kb += WD_SKB) {
+                    if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
                     uint8_t *dst = base + stage * WD_STAGE;
                     const uint32_t bar = cluster_addr(&sh.full[stage], 0);
-                    if (rank == 0) mbar_expect_tx(&sh.full[stage], 2 * WD_STAGE);
-                    tma_load_pair(dst, &tmap_a, bar, kb * QBLOCK, row);
-                    tma_load_pair(dst + WD_HALF, &tmap_w, bar, kb * QBLOCK, col);
+                    const int n = min(WD_SKB, KB - kb);
+                    if (rank == 0) mbar_expect_tx(&sh.full[stage], n * 4 * WD_HALF);
+                    if ((kb + WD_SKB) * QBLOCK <= g.K) {
+                        // one copy per operand: 32 KB boxes stream faster than 16 KB ones
+                        tma_load_pair_3d(dst, &tmap_a2, bar, 0, row, kb);
+                        tma_load_pair_3d(dst + WD_SKB * WD_HALF, &tmap_w2, bar, 0, col, kb);
+                    } else
+                        for (int i = 0; i < n; ++i) {
+                            tma_load_pair(dst + i * WD_HALF, &tmap_a, bar, (kb + i) * QBLOCK, row);
+                            tma_load_pair(dst + (WD_SKB + i) * WD_HALF, &tmap_w, bar, (kb + i) * QBLOCK, col);
+                        }
                     pending |= 1u << stage;
                     pend_par = (pend_par & ~(1u << stage)) | (phase << stage);
                     if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
@@ -218,7 +215,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             int dummy = 0;
             if (rank == 0)
                 for (int st = 0; st < WD_STAGES; ++st)
-                    if (pending & (1u << st)) mbar_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, 100000000ull);
+                    if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
         }
     } else if (warp == 1) {
         // ---------------------------------------------------- MMA issuer
@@ -227,124 +224,157 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             uint32_t phase = 0, tphase = 0;
             bool ok = true;
             for (int64_t t = first; t < tiles && ok; t += step) {
-                for (int kb = 0; kb < KB; ++kb) {
-                    if (!mbar_wait_cluster(&sh.tempty[buf], tphase ^ 1, abort) || !mbar_wait(&sh.full[stage], phase, abort)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t d = tmem + buf * WD_BN;
-                    const uint64_t ad = smem_desc_sw128(smem_u32(base + stage * WD_STAGE));
-                    const uint64_t wd = smem_desc_sw128(smem_u32(base + stage * WD_STAGE + WD_HALF));
+                for (int kb = 0; kb < KB && ok; kb += WD_SKB) {
+                    if (!mm_wait(&sh.full[stage], phase, abort)) { ok = false; break; }
+                    for (int i = 0; i < WD_SKB && kb + i < KB; ++i) {
+                        if (!mm_wait<true>(&sh.tempty[buf], tphase ^ 1, abort)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t d = tmem + buf * WD_BN, at = smem_u32(base + stage * WD_STAGE + i * WD_HALF);
+                        const uint64_t ad = smem_desc_sw128(at), wd = smem_desc_sw128(at + WD_SKB * WD_HALF);
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) tc_mma_fp8_pair(d, ad + 2 * kk, wd + 2 * kk, WD_IDESC, kk != 0);
+                        for (int kk = 0; kk < 4; ++kk) tc_mma_fp8_pair(d, ad + 2 * kk, wd + 2 * kk, WD_IDESC, kk != 0);
+                        tc_commit_pair(&sh.tfull[buf]);
+                        buf ^= 1;
+                        if (buf == 0) tphase ^= 1;
+                    }
                     tc_commit_pair(&sh.empty[stage]);
-                    tc_commit_pair(&sh.tfull[buf]);
                     if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
-                    buf ^= 1;
-                    if (buf == 0) tphase ^= 1;
                 }
             }
             tc_commit_pair(&sh.drain);
             int dummy = 0;
-            mbar_wait(&sh.drain, 0, &dummy, 100000000ull);
+            mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
+        }
+    } else if (warp >= 2) {
+        // -------------------------------------------------- scale products
+        const int r0 = (warp - 2) * 32 + lane;               // rows r0 and r0 + 64 of this CTA's 128
+        const bool vec4 = aligned_dev(g.sa, 16) && g.ldsa % 4 == 0;
+        int slot = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int64_t t = first; t < tiles && ok; t += step) {
+            int mt, nt;
+            tile_at(t, MT, NT, mt, nt);
+            const int m = mt * WD_BM + (int)rank * 128 + r0;
+            const float *s0 = g.sa + (int64_t)min(m, g.M - 1) * g.ldsa, *s1 = g.sa + (int64_t)min(m + 64, g.M - 1) * g.ldsa;
+            const float *w0 = g.sw + (int64_t)(2 * nt) * g.ldsw;
+            const float *w1 = g.sw + (int64_t)min(2 * nt + 1, (g.N - 1) / QBLOCK) * g.ldsw;
+            for (int kb = 0; kb < KB; kb += WD_GROUP) {
+                float a0[WD_GROUP], a1[WD_GROUP], b0[WD_GROUP], b1[WD_GROUP];
+                if (vec4 && kb + WD_GROUP <= KB) {
+                    const float4 x = *reinterpret_cast<const float4 *>(s0 + kb), y = *reinterpret_cast<const float4 *>(s1 + kb);
+                    a0[0] = x.x; a0[1] = x.y; a0[2] = x.z; a0[3] = x.w;
+                    a1[0] = y.x; a1[1] = y.y; a1[2] = y.z; a1[3] = y.w;
+                } else
+#pragma unroll
+                    for (int i = 0; i < WD_GROUP; ++i) {
+                        a0[i] = kb + i < KB ? s0[kb + i] : 0.0f;
+                        a1[i] = kb + i < KB ? s1[kb + i] : 0.0f;
+                    }
+#pragma unroll
+                for (int i = 0; i < WD_GROUP; ++i) {
+                    b0[i] = kb + i < KB ? w0[kb + i] : 0.0f;
+                    b1[i] = kb + i < KB ? w1[kb + i] : 0.0f;
+                }
+                if (ok) ok = mm_wait(&sh.sempty[slot], phase ^ 1, abort);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                float *f = scales + slot * (WD_SCALES / 4) + r0;
+#pragma unroll
+                for (int i = 0; i < WD_GROUP; ++i) {
+                    f[(2 * i) * 128] = a0[i] * b0[i];
+                    f[(2 * i) * 128 + 64] = a1[i] * b0[i];
+                    f[(2 * i + 1) * 128] = a0[i] * b1[i];
+                    f[(2 * i + 1) * 128 + 64] = a1[i] * b1[i];
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.sfull[slot]);
+                slot ^= 1;
+                if (slot == 0) phase ^= 1;
+            }
         }
     }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WD_REGS_MANY));
         // ------------------------------------------------------ epilogue
-        const int q = warp & 3, half = (warp - 4) / 4;
-        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + half * 128;
-        float (*tp)[33] = reinterpret_cast<float (*)[33]>(base + WD_STAGES * WD_STAGE + (warp - 4) * WD_TILE);
-        int buf = 0;
-        uint32_t tphase = 0;
+        const int q = warp & 3, part = (warp - 4) / 4;
+        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + part * WD_COLS;
+        float (*tp)[WD_TCOLS + 1] = reinterpret_cast<float (*)[WD_TCOLS + 1]>(base + WD_STAGES * WD_STAGE + (warp - 4) * WD_TILE);
+        int buf = 0, slot = 0;
+        uint32_t tphase = 0, sphase = 0;
         bool ok = true;
         for (int64_t t = first; t < tiles && ok; t += step) {
             int mt, nt;
             tile_at(t, MT, NT, mt, nt);
-            const int m0 = mt * WD_BM + (int)rank * 128 + q * 32, n0 = nt * WD_BN + half * 128;
-            const float *sar = g.sa + (int64_t)min(m0 + lane, g.M - 1) * g.ldsa;
-            const float *swr = g.sw + (int64_t)(min(n0, g.N - 1) / QBLOCK) * g.ldsw;
-            uint64_t acc[64];
+            const int m0 = mt * WD_BM + (int)rank * 128 + q * 32, n0 = nt * WD_BN + part * WD_COLS;
+            float acc[WD_COLS];
 #pragma unroll
-            for (int j = 0; j < 64; ++j) acc[j] = 0;
-            float f_next = sar[0] * swr[0];
+            for (int j = 0; j < WD_COLS; ++j) acc[j] = 0.0f;
             for (int kb = 0; kb < KB; ++kb) {
-                const float f = f_next;
-                uint64_t f2;
-                asm("mov.b64 %0, {%1, %1};" : "=l"(f2) : "r"(__float_as_uint(f)));
-                if (kb + 1 < KB) f_next = sar[kb + 1] * swr[kb + 1];
-                if (ok) ok = mbar_wait(&sh.tfull[buf], tphase, abort);
-                ok = __all_sync(0xffffffffu, ok);
+                const int i = kb % WD_GROUP;
+                if (i == 0) ok = mm_wait(&sh.sfull[slot], sphase, abort);
+                ok = __all_sync(0xffffffffu, ok && mm_wait(&sh.tfull[buf], tphase, abort));
                 if (!ok) break;
                 tc_fence_after();
+                const float f = scales[slot * (WD_SCALES / 4) + (2 * i + part / 2) * 128 + q * 32 + lane];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t d[32];
-                    tmem_ld32w(taddr + buf * WD_BN + c * 32, d);
-                    if (c == 3) {
+                for (int c = 0; c < WD_COLS; c += 16) {
+                    float d[16];
+                    tmem_ld16w(taddr + buf * WD_BN + c, d);
+                    if (c + 16 == WD_COLS) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(cluster_addr(&sh.tempty[buf], 0));
                     }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) fma2(acc[c * 16 + j], d[2 * j], d[2 * j + 1], f2);
+                    for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(d[j], f, acc[c + j]);
                 }
                 buf ^= 1;
                 if (buf == 0) tphase ^= 1;
+                if (i == WD_GROUP - 1 || kb == KB - 1) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.sempty[slot]);
+                    slot ^= 1;
+                    if (slot == 0) sphase ^= 1;
+                }
             }
             if (!ok || m0 >= g.M || n0 >= g.N) continue;
-            if (vec && n0 + 128 <= g.N) {
+            if (vec && n0 + WD_COLS <= g.N) {
                 if (m0 + lane < g.M) {
+                    const int64_t at = (int64_t)(m0 + lane) * g.ldo + n0;
                     if (g.bf16) {
-                        uint16_t *p = static_cast<uint16_t *>(g.out) + (int64_t)(m0 + lane) * g.ldo + n0;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {
+                        for (int c = 0; c < WD_COLS; c += 16) {
                             uint32_t w[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                float lo, hi;
-                                halves(acc[c * 8 + j], lo, hi);
-                                w[j] = pack_bf16(lo, hi);
-                            }
-                            store32(p + c * 16, w);
+                            for (int j = 0; j < 8; ++j) w[j] = pack_bf16(acc[c + 2 * j], acc[c + 2 * j + 1]);
+                            store32(static_cast<uint16_t *>(g.out) + at + c, w);
                         }
                     } else {
-                        float *p = static_cast<float *>(g.out) + (int64_t)(m0 + lane) * g.ldo + n0;
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) {
+                        for (int c = 0; c < WD_COLS; c += 8) {
                             uint32_t w[8];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                float lo, hi;
-                                halves(acc[c * 4 + j], lo, hi);
-                                w[2 * j] = __float_as_uint(lo);
-                                w[2 * j + 1] = __float_as_uint(hi);
-                            }
-                            store32(p + c * 8, w);
+                            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(acc[c + j]);
+                            store32(static_cast<float *>(g.out) + at + c, w);
                         }
                     }
                 }
             } else {
-                // rows of out that start anywhere, or a partial tile: transpose
-                // 32 columns at a time, so that a warp stores consecutive elements
-                const int rows = min(32, g.M - m0);
+                // rows of out that start anywhere, or a partial tile: transpose 8
+                // columns at a time, so that 8 lanes store consecutive elements
+                const int rows = min(32, g.M - m0), cl = lane % WD_TCOLS;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int n = n0 + c * 32 + lane;
+                for (int c = 0; c < WD_COLS; c += WD_TCOLS) {
+                    const int n = n0 + c + cl;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float lo, hi;
-                        halves(acc[c * 16 + j], lo, hi);
-                        tp[lane][2 * j] = lo;
-                        tp[lane][2 * j + 1] = hi;
-                    }
+                    for (int j = 0; j < WD_TCOLS; ++j) tp[lane][j] = acc[c + j];
                     __syncwarp();
                     if (n < g.N)
-                        for (int r = 0; r < rows; ++r) {
+                        for (int r = lane / WD_TCOLS; r < rows; r += 32 / WD_TCOLS) {
                             const int64_t at = (int64_t)(m0 + r) * g.ldo + n;
-                            if (g.bf16) static_cast<uint16_t *>(g.out)[at] = f2bf(tp[r][lane]);
-                            else static_cast<float *>(g.out)[at] = tp[r][lane];
+                            if (g.bf16) static_cast<uint16_t *>(g.out)[at] = f2bf(tp[r][cl]);
+                            else static_cast<float *>(g.out)[at] = tp[r][cl];
                         }
                     __syncwarp();
                 }
@@ -372,15 +402,20 @@ int launch_mm_wide(const MmArgs &g, const void *a, int64_t lda, const void *w, i
         attr = cudaFuncSetAttribute(k_matmul_fp8_wide, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WD_SMEM);
     });
     if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
-    CUtensorMap ta{}, tw{};
+    CUtensorMap ta{}, tw{}, ta2{}, tw2{};
     if (!tmap_bytes(&ta, a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)lda, QBLOCK, 128) ||
         !tmap_bytes(&tw, w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)ldw, QBLOCK, 128))
+        return XPRESS_ERR_CUDA;
+    // whole K blocks only: past them the rows' padding would be read
+    const uint64_t kbs = g.K / QBLOCK;
+    if (kbs >= WD_SKB && (!tmap_bytes_kblocks(&ta2, a, kbs, (uint64_t)g.M, (uint64_t)lda, 128, WD_SKB) ||
+                          !tmap_bytes_kblocks(&tw2, w, kbs, (uint64_t)g.N, (uint64_t)ldw, 128, WD_SKB)))
         return XPRESS_ERR_CUDA;
     const int64_t tiles = (int64_t)((g.M + WD_BM - 1) / WD_BM) * ((g.N + WD_BN - 1) / WD_BN);
     const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
     const int es = g.bf16 ? 2 : 4;
     const int vec = aligned(g.out, 32) && g.ldo * es % 32 == 0;
-    XH_CUDA(launch_head(k_matmul_fp8_wide, dim3((unsigned)(2 * pairs)), WD_THREADS, WD_SMEM, st, 2, g, ta, tw, vec));
+    XH_CUDA(launch_head(k_matmul_fp8_wide, dim3((unsigned)(2 * pairs)), WD_THREADS, WD_SMEM, st, 2, g, ta, tw, ta2, tw2, vec));
     return XPRESS_OK;
 }
 
