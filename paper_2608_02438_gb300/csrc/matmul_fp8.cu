@@ -52,18 +52,6 @@ struct MmBars {
     int abort;
 };
 
-// D[tmem] (+)= A[smem] B[smem]^T, e4m3 operands (K = 32 per instruction), fp32 sums
-__device__ __forceinline__ void tc_mma_fp8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                           uint32_t accumulate)
-{
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *v)
 {
     uint32_t r[16];
@@ -162,32 +150,35 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
         }
     } else if (warp == 1) {
         // ---------------------------------------------------- MMA issuer
-        if (lane == 0) {
-            int stage = 0, buf = 0;
-            uint32_t phase = 0, tphase = 0;
-            bool ok = true;
-            for (int64_t it = first; it < items && ok; it += step) {
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mm_wait(&sh.tempty[buf], tphase ^ 1, abort) || !mm_wait(&sh.full[stage], phase, abort)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t d = tmem + buf * NT;
-                    const uint64_t wd = smem_desc_sw128(smem_u32(base + stage * Sh::STAGE));
-                    const uint64_t ad = smem_desc_sw128(smem_u32(base + stage * Sh::STAGE + MM_W_STAGE));
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) tc_mma_fp8(d, wd + 2 * kk, ad + 2 * kk, Sh::IDESC, kk != 0);
+        // the whole warp runs the loop, so that the descriptors stay in uniform
+        // registers, and one elected lane issues
+        const uint32_t base_u = __shfl_sync(0xffffffffu, smem_u32(base), 0);
+        const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t lo0 = (uint32_t)smem_desc_sw128(base_u), hi = (uint32_t)(smem_desc_sw128(base_u) >> 32);
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, tphase = 0;
+        bool ok = true;
+        for (int64_t it = first; it < items && ok; it += step) {
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = mm_wait(&sh.tempty[buf], tphase ^ 1, abort) && mm_wait(&sh.full[stage], phase, abort);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t w_lo = lo0 + stage * (Sh::STAGE >> 4);
+                    tc_mma_fp8_kblock(tmem_u + buf * NT, w_lo, w_lo + (MM_W_STAGE >> 4), hi, Sh::IDESC);
                     tc_commit(&sh.empty[stage]);
                     tc_commit(&sh.tfull[buf]);
-                    if (++stage == stages) { stage = 0; phase ^= 1; }
-                    if (++buf == Sh::NBUF) { buf = 0; tphase ^= 1; }
                 }
+                __syncwarp();
+                if (++stage == stages) { stage = 0; phase ^= 1; }
+                if (++buf == Sh::NBUF) { buf = 0; tphase ^= 1; }
             }
-            tc_commit(&sh.drain);
-            int dummy = 0;
-            mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
         }
+        if (elect_one()) tc_commit(&sh.drain);
+        __syncwarp();
+        int dummy = 0;
+        mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
         __syncwarp();
     } else {
         // ------------------------------------------------------ epilogue

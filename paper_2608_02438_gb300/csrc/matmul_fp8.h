@@ -35,30 +35,17 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank)
     return a;
 }
 
-// Bounded wait for a phase of `bar` (CLUSTER: the other CTA of a pair arrives
-// on it).  It polls (a wait with a sleep hint wakes up later: 2048 x 38912 x
-// 4096 took 739 us against 683) and bounds itself by the SM's cycle counter,
-// read once in 64 polls: the global timer's latency would sit in every
-// hand-off of a K block.
+// Bounded wait for a phase of `bar`.  It polls (a wait with a sleep hint wakes
+// up later: 2048 x 38912 x 4096 took 739 us against 683) and bounds itself by
+// the SM's cycle counter, read once in 64 polls: the global timer's latency
+// would sit in every hand-off of a K block.
 constexpr long long MM_WAIT_CYCLES = 4000000000ll;       // about 2 s
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool mm_wait(uint64_t *bar, uint32_t parity, volatile int *abort,
                                         long long cycles = MM_WAIT_CYCLES)
 {
     long long t0 = 0;
     for (uint32_t it = 1;; ++it) {
-        uint32_t ok;
-        if (CLUSTER)
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                "selp.u32 %0, 1, 0, p;\n\t}"
-                : "=r"(ok)
-                : "r"(smem_u32(bar)), "r"(parity)
-                : "memory");
-        else
-            ok = mbar_try_wait(bar, parity);
-        if (ok) return true;
+        if (mbar_try_wait(bar, parity)) return true;
         if ((it & 63u) == 0) {
             if (*abort) return false;
             const long long t = clock64();
@@ -72,6 +59,40 @@ __device__ __forceinline__ bool mm_wait(uint64_t *bar, uint32_t parity, volatile
 constexpr uint32_t idesc_e4m3(int M, int N)
 {
     return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+
+// D[tmem] = A[smem] B[smem]^T over one 128-wide K block, e4m3 operands (K = 32
+// per instruction), fp32 sums: the descriptors' low words step by 32 bytes, the
+// high word (the layout) is the same for both operands.
+__device__ __forceinline__ void tc_mma_fp8_kblock(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
+                                                  uint32_t idesc)
+{
+    asm volatile(
+        "{\n\t.reg .pred f, t;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 f, 0, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "mov.b64 a, {%1, %9};\n\tmov.b64 b, {%5, %9};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %10, f;\n\t"
+        "mov.b64 a, {%2, %9};\n\tmov.b64 b, {%6, %9};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %10, t;\n\t"
+        "mov.b64 a, {%3, %9};\n\tmov.b64 b, {%7, %9};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %10, t;\n\t"
+        "mov.b64 a, {%4, %9};\n\tmov.b64 b, {%8, %9};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %10, t;}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_lo + 2), "r"(a_lo + 4), "r"(a_lo + 6), "r"(b_lo), "r"(b_lo + 2), "r"(b_lo + 4),
+        "r"(b_lo + 6), "r"(hi), "r"(idesc)
+        : "memory");
 }
 
 // many rows of a (matmul_fp8_wide.cu)

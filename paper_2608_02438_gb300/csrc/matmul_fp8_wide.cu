@@ -2,22 +2,20 @@
 // the definition) for many rows of a: bound by the tensor cores and by what
 // feeds them, not by the weights' stream.
 //
-// A pair of CTAs (tcgen05 cta_group::2) takes a tile of 256 rows of a (the
-// MMA's M, 128 in each CTA's TMEM) by 256 weight rows (N; each CTA stages half
-// of them, and the pair's MMA reads both halves), so that every byte brought
-// from L2 feeds twice the products of a single CTA's tile.  One 128-wide K
-// block is 4 MMAs into one of two TMEM buffers of 256 columns; the epilogue
-// adds the other to the running sums with its scale.  With a's rows on the
-// lanes a thread has one scale per K block (its row's, times that of the
-// weight block its columns are in).
+// A CTA takes a tile of 128 rows of a (the MMA's M) by 256 weight rows (two
+// MMAs' N of 128).  One 128-wide K block of a half tile is 4 MMAs into one of
+// four TMEM buffers of 128 columns; the epilogue adds the others to the running
+// sums with their scales.  With a's rows on the lanes a thread has one scale
+// per K block (its row's, times that of the weight block its columns are in).
+// The running sums (128 KB) are what limits the tile; four small buffers
+// instead of two large ones cover the way from a finished MMA over the epilogue
+// back to the MMA that reuses its buffer.
 //
-// Roles (640 threads): warp 0 TMA producer (both CTAs load their own halves;
-// the copies complete on the leader's barrier), warp 1 TMEM allocator and, in
-// the leader, MMA issuer; warps 2-3 stage the products of the scales (128 rows
-// by the tile's 2 weight blocks, four K blocks at a time) in shared memory;
-// warps 4-19 epilogue (lane quarter warp % 4, 64 columns of it) with the 64
-// sums of a thread in registers: the first warpgroup hands registers to the
-// others.
+// Roles (640 threads): warp 0 TMA producer, warp 1 TMEM allocator and MMA
+// issuer, warps 2-3 stage the products of the scales (128 rows by the tile's 2
+// weight blocks, four K blocks at a time) in shared memory; warps 4-19
+// epilogue (lane quarter warp % 4, 64 columns of a half tile) with the 64 sums
+// of a thread in registers: the first warpgroup hands registers to the others.
 #include <mutex>
 
 #include "matmul_fp8.h"
@@ -26,77 +24,34 @@ namespace xp {
 
 namespace {
 
-constexpr int WD_BM = 256, WD_BN = 256;                 // tile of a pair
+constexpr int WD_BM = 128, WD_BN = 256;                 // tile of a CTA
 constexpr int WD_EPI = 16;
-constexpr int WD_COLS = WD_BN / (WD_EPI / 4);           // columns of an epilogue warp
+constexpr int WD_COLS = 64;                             // columns of an epilogue warp
 constexpr int WD_THREADS = 32 * (4 + WD_EPI);
 // registers per thread: the kernel is launched with 96 x 640 (the most that
 // five warps of a sub-partition's 16,384 allow); 64 x 128 + 104 x 512 = 61,440
 // are all of them
 constexpr int WD_REGS_FEW = 64, WD_REGS_MANY = 104;
-constexpr uint32_t WD_HALF = 128 * QBLOCK;              // 16 KB: 128 rows of one operand
-constexpr int WD_SKB = 2;                               // K blocks of a stage
-constexpr uint32_t WD_STAGE = WD_SKB * 2 * WD_HALF;     // [operand][K block][128 rows][128 bytes]
-constexpr int WD_STAGES = 3;
-constexpr uint32_t WD_IDESC = idesc_e4m3(WD_BM, WD_BN);
+constexpr uint32_t WD_HALF = 128 * QBLOCK;              // 16 KB: 128 rows of an operand's K block
+constexpr uint32_t WD_STAGE = 3 * WD_HALF;              // a, then the two halves of w
+constexpr int WD_STAGES = 4;
+constexpr uint32_t WD_IDESC = idesc_e4m3(128, 128);
+constexpr int WD_BUFS = 4;                              // TMEM buffers: K block parity, half
 constexpr int WD_TCOLS = 8;                             // columns of a transpose
 constexpr size_t WD_TILE = 32 * (WD_TCOLS + 1) * 4;
 constexpr int WD_GROUP = 4;                             // K blocks whose scales are staged together
 constexpr size_t WD_SCALES = WD_GROUP * 2 * 128 * 4;    // [K block][weight block][row]                 // a warp's transpose
 constexpr size_t WD_SMEM = 1024 + WD_STAGES * WD_STAGE + WD_EPI * WD_TILE + 2 * WD_SCALES;
-constexpr int WD_BAND = 16;                             // row tiles that share the weights while they are in L2
+constexpr int WD_BAND = 32;                             // row tiles that share the weights while they are in L2
 
 struct WideBars {
     uint64_t full[WD_STAGES], empty[WD_STAGES];
-    uint64_t tfull[2], tempty[2];
+    uint64_t tfull[WD_BUFS], tempty[WD_BUFS];
     uint64_t sfull[2], sempty[2];
     uint64_t drain;
     uint32_t tmem_base;
     int abort;
 };
-
-__device__ __forceinline__ void tma_load_pair(void *dst, const CUtensorMap *map, uint32_t bar, int x, int y)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
-        "[%4];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-}
-
-__device__ __forceinline__ void tma_load_pair_3d(void *dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
-        "%4}], [%5];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
-}
-
-__device__ __forceinline__ void tc_mma_fp8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                                uint32_t accumulate)
-{
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
-// Arrive on `bar` of both CTAs once every MMA issued so far by this thread is done.
-__device__ __forceinline__ void tc_commit_pair(uint64_t *bar)
-{
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-        ::"r"(smem_u32(bar)), "h"((uint16_t)3)
-        : "memory");
-}
-
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
 
 // 16 TMEM columns of this warp's lane quarter.
 __device__ __forceinline__ void tmem_ld16w(uint32_t taddr, float (&v)[16])
@@ -126,35 +81,33 @@ __device__ __forceinline__ bool aligned_dev(const void *p, uintptr_t a)
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }
 
-// Tile t in the order of bands of WD_BAND row tiles, within a band the row
-// tiles of one column tile after another.
-__device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &mt, int &nt)
+// First row and column of tile t, in the order of bands of WD_BAND row tiles,
+// within a band the row tiles of one column tile after another.
+__device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &row, int &col)
 {
     const int64_t band = t / ((int64_t)WD_BAND * NT);
     const int m0 = (int)band * WD_BAND, rows = min(WD_BAND, MT - m0);
     const int64_t in = t - band * WD_BAND * NT;
-    mt = m0 + (int)(in % rows);
-    nt = (int)(in / rows);
+    row = (m0 + (int)(in % rows)) * WD_BM;
+    col = (int)(in / rows) * WD_BN;
 }
 
-// grid: pairs of CTAs, WD_THREADS threads, WD_SMEM bytes; vec: out's rows start on 32 bytes.
+// grid: any; WD_THREADS threads, WD_SMEM bytes; vec: out's rows start on 32 bytes.
 __global__ void __launch_bounds__(WD_THREADS, 1)
     k_matmul_fp8_wide(const __grid_constant__ MmArgs g, const __grid_constant__ CUtensorMap tmap_a,
-                      const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_a2,
-                      const __grid_constant__ CUtensorMap tmap_w2, int vec)
+                      const __grid_constant__ CUtensorMap tmap_w, int vec)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ WideBars sh;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t rank = cluster_rank();
     const int KB = (g.K + QBLOCK - 1) / QBLOCK;
     const int MT = (g.M + WD_BM - 1) / WD_BM, NT = (g.N + WD_BN - 1) / WD_BN;
-    const int64_t tiles = (int64_t)MT * NT, first = blockIdx.x / 2, step = gridDim.x / 2;
+    const int64_t tiles = (int64_t)MT * NT, first = blockIdx.x, step = gridDim.x;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < WD_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 2 * WD_EPI); }
+        for (int i = 0; i < WD_BUFS; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], WD_EPI / 2); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.sfull[i], 2); mbar_init(&sh.sempty[i], WD_EPI); }
         mbar_init(&sh.drain, 1);
         sh.abort = 0;
@@ -162,16 +115,9 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
         tma_prefetch_desc(&tmap_w);
         tma_prefetch_desc(&tmap_a);
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)),
-                     "r"(512u)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
+    if (warp == 1) { tmem_alloc(&sh.tmem_base, WD_BUFS * 128); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
-    cluster_arrive();                                    // both CTAs' barriers exist before either signals the other
-    cluster_wait();
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
     volatile int *abort = &sh.abort;
@@ -188,63 +134,62 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             uint32_t phase = 0, pending = 0, pend_par = 0;
             bool ok = true;
             for (int64_t t = first; t < tiles && ok; t += step) {
-                int mt, nt;
-                tile_at(t, MT, NT, mt, nt);
-                const int row = mt * WD_BM + (int)rank * 128, col = nt * WD_BN + (int)rank * 128;
-                for (int kb = 0; kb < KB; kb += WD_SKB) {
+                int row, col;
+                tile_at(t, MT, NT, row, col);
+                for (int kb = 0; kb < KB; ++kb) {
                     if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
                     uint8_t *dst = base + stage * WD_STAGE;
-                    const uint32_t bar = cluster_addr(&sh.full[stage], 0);
-                    const int n = min(WD_SKB, KB - kb);
-                    if (rank == 0) mbar_expect_tx(&sh.full[stage], n * 4 * WD_HALF);
-                    if ((kb + WD_SKB) * QBLOCK <= g.K) {
-                        // one copy per operand: 32 KB boxes stream faster than 16 KB ones
-                        tma_load_pair_3d(dst, &tmap_a2, bar, 0, row, kb);
-                        tma_load_pair_3d(dst + WD_SKB * WD_HALF, &tmap_w2, bar, 0, col, kb);
-                    } else
-                        for (int i = 0; i < n; ++i) {
-                            tma_load_pair(dst + i * WD_HALF, &tmap_a, bar, (kb + i) * QBLOCK, row);
-                            tma_load_pair(dst + (WD_SKB + i) * WD_HALF, &tmap_w, bar, (kb + i) * QBLOCK, col);
-                        }
+                    mbar_expect_tx(&sh.full[stage], WD_STAGE);
+                    tma_load_2d(dst, &tmap_a, &sh.full[stage], kb * QBLOCK, row);
+                    tma_load_2d(dst + WD_HALF, &tmap_w, &sh.full[stage], kb * QBLOCK, col);
                     pending |= 1u << stage;
                     pend_par = (pend_par & ~(1u << stage)) | (phase << stage);
                     if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
                 }
             }
-            // no copy of the pair may still be landing when it leaves
+            // no copy may still be landing when the CTA leaves
             int dummy = 0;
-            if (rank == 0)
-                for (int st = 0; st < WD_STAGES; ++st)
-                    if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
+            for (int st = 0; st < WD_STAGES; ++st)
+                if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
         }
     } else if (warp == 1) {
         // ---------------------------------------------------- MMA issuer
-        if (lane == 0 && rank == 0) {
-            int stage = 0, buf = 0;
-            uint32_t phase = 0, tphase = 0;
-            bool ok = true;
-            for (int64_t t = first; t < tiles && ok; t += step) {
-                for (int kb = 0; kb < KB && ok; kb += WD_SKB) {
-                    if (!mm_wait(&sh.full[stage], phase, abort)) { ok = false; break; }
-                    for (int i = 0; i < WD_SKB && kb + i < KB; ++i) {
-                        if (!mm_wait<true>(&sh.tempty[buf], tphase ^ 1, abort)) { ok = false; break; }
-                        tc_fence_after();
-                        const uint32_t d = tmem + buf * WD_BN, at = smem_u32(base + stage * WD_STAGE + i * WD_HALF);
-                        const uint64_t ad = smem_desc_sw128(at), wd = smem_desc_sw128(at + WD_SKB * WD_HALF);
+        // the whole warp runs the loop, so that the descriptors stay in uniform
+        // registers, and one elected lane issues
+        const uint32_t base_u = __shfl_sync(0xffffffffu, smem_u32(base), 0);
+        const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t lo0 = (uint32_t)smem_desc_sw128(base_u), hi = (uint32_t)(smem_desc_sw128(base_u) >> 32);
+        int stage = 0;
+        uint32_t phase = 0, par = 0, tphase = 0;               // par: K block parity, which names the TMEM buffers
+        bool ok = true;
+        for (int64_t t = first; t < tiles && ok; t += step) {
+            for (int kb = 0; kb < KB && ok; ++kb) {
+                ok = __all_sync(0xffffffffu, mm_wait(&sh.full[stage], phase, abort));
+                if (!ok) break;
+                const uint32_t a_lo = lo0 + stage * (WD_STAGE >> 4);
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) tc_mma_fp8_pair(d, ad + 2 * kk, wd + 2 * kk, WD_IDESC, kk != 0);
-                        tc_commit_pair(&sh.tfull[buf]);
-                        buf ^= 1;
-                        if (buf == 0) tphase ^= 1;
+                for (int h = 0; h < 2; ++h) {
+                    const int buf = par * 2 + h;
+                    ok = __all_sync(0xffffffffu, mm_wait(&sh.tempty[buf], tphase ^ 1, abort));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        tc_mma_fp8_kblock(tmem_u + buf * 128, a_lo, a_lo + (1 + h) * (WD_HALF >> 4), hi, WD_IDESC);
+                        tc_commit(&sh.tfull[buf]);
+                        if (h == 1) tc_commit(&sh.empty[stage]);
                     }
-                    tc_commit_pair(&sh.empty[stage]);
-                    if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
+                    __syncwarp();
                 }
+                if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
+                par ^= 1;
+                if (par == 0) tphase ^= 1;
             }
-            tc_commit_pair(&sh.drain);
-            int dummy = 0;
-            mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
         }
+        if (elect_one()) tc_commit(&sh.drain);
+        __syncwarp();
+        int dummy = 0;
+        mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
+        __syncwarp();
     } else if (warp >= 2) {
         // -------------------------------------------------- scale products
         const int r0 = (warp - 2) * 32 + lane;               // rows r0 and r0 + 64 of this CTA's 128
@@ -253,12 +198,11 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
         uint32_t phase = 0;
         bool ok = true;
         for (int64_t t = first; t < tiles && ok; t += step) {
-            int mt, nt;
-            tile_at(t, MT, NT, mt, nt);
-            const int m = mt * WD_BM + (int)rank * 128 + r0;
+            int row, col;
+            tile_at(t, MT, NT, row, col);
+            const int m = row + r0, wb = col / QBLOCK, wl = (g.N - 1) / QBLOCK;
             const float *s0 = g.sa + (int64_t)min(m, g.M - 1) * g.ldsa, *s1 = g.sa + (int64_t)min(m + 64, g.M - 1) * g.ldsa;
-            const float *w0 = g.sw + (int64_t)(2 * nt) * g.ldsw;
-            const float *w1 = g.sw + (int64_t)min(2 * nt + 1, (g.N - 1) / QBLOCK) * g.ldsw;
+            const float *w0 = g.sw + (int64_t)min(wb, wl) * g.ldsw, *w1 = g.sw + (int64_t)min(wb + 1, wl) * g.ldsw;
             for (int kb = 0; kb < KB; kb += WD_GROUP) {
                 float a0[WD_GROUP], a1[WD_GROUP], b0[WD_GROUP], b1[WD_GROUP];
                 if (vec4 && kb + WD_GROUP <= KB) {
@@ -297,40 +241,40 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WD_REGS_MANY));
         // ------------------------------------------------------ epilogue
-        const int q = warp & 3, part = (warp - 4) / 4;
+        const int q = warp & 3, part = (warp - 4) / 4, half = part / 2;
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + part * WD_COLS;
         float (*tp)[WD_TCOLS + 1] = reinterpret_cast<float (*)[WD_TCOLS + 1]>(base + WD_STAGES * WD_STAGE + (warp - 4) * WD_TILE);
-        int buf = 0, slot = 0;
-        uint32_t tphase = 0, sphase = 0;
+        int slot = 0;
+        uint32_t par = 0, tphase = 0, sphase = 0;
         bool ok = true;
         for (int64_t t = first; t < tiles && ok; t += step) {
-            int mt, nt;
-            tile_at(t, MT, NT, mt, nt);
-            const int m0 = mt * WD_BM + (int)rank * 128 + q * 32, n0 = nt * WD_BN + part * WD_COLS;
+            int row, col;
+            tile_at(t, MT, NT, row, col);
+            const int m0 = row + q * 32, n0 = col + part * WD_COLS;
             float acc[WD_COLS];
 #pragma unroll
             for (int j = 0; j < WD_COLS; ++j) acc[j] = 0.0f;
             for (int kb = 0; kb < KB; ++kb) {
                 const int i = kb % WD_GROUP;
                 if (i == 0) ok = mm_wait(&sh.sfull[slot], sphase, abort);
-                ok = __all_sync(0xffffffffu, ok && mm_wait(&sh.tfull[buf], tphase, abort));
+                ok = __all_sync(0xffffffffu, ok && mm_wait(&sh.tfull[par * 2 + half], tphase, abort));
                 if (!ok) break;
                 tc_fence_after();
-                const float f = scales[slot * (WD_SCALES / 4) + (2 * i + part / 2) * 128 + q * 32 + lane];
+                const float f = scales[slot * (WD_SCALES / 4) + (2 * i + half) * 128 + q * 32 + lane];
 #pragma unroll
                 for (int c = 0; c < WD_COLS; c += 16) {
                     float d[16];
-                    tmem_ld16w(taddr + buf * WD_BN + c, d);
+                    tmem_ld16w(taddr + par * 256 + c, d);
                     if (c + 16 == WD_COLS) {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(cluster_addr(&sh.tempty[buf], 0));
+                        if (lane == 0) mbar_arrive(&sh.tempty[par * 2 + half]);
                     }
 #pragma unroll
                     for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(d[j], f, acc[c + j]);
                 }
-                buf ^= 1;
-                if (buf == 0) tphase ^= 1;
+                par ^= 1;
+                if (par == 0) tphase ^= 1;
                 if (i == WD_GROUP - 1 || kb == KB - 1) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.sempty[slot]);
@@ -383,11 +327,9 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     }
     tc_fence_before();
     __syncthreads();
-    cluster_arrive();                                    // neither CTA leaves while the other may signal it
-    cluster_wait();
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+        tmem_dealloc(tmem, WD_BUFS * 128);
     }
     if (threadIdx.x == 0 && sh.abort) set_status(g.status, ST_TIMEOUT);
 }
@@ -402,20 +344,15 @@ int launch_mm_wide(const MmArgs &g, const void *a, int64_t lda, const void *w, i
         attr = cudaFuncSetAttribute(k_matmul_fp8_wide, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WD_SMEM);
     });
     if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
-    CUtensorMap ta{}, tw{}, ta2{}, tw2{};
-    if (!tmap_bytes(&ta, a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)lda, QBLOCK, 128) ||
-        !tmap_bytes(&tw, w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)ldw, QBLOCK, 128))
-        return XPRESS_ERR_CUDA;
-    // whole K blocks only: past them the rows' padding would be read
-    const uint64_t kbs = g.K / QBLOCK;
-    if (kbs >= WD_SKB && (!tmap_bytes_kblocks(&ta2, a, kbs, (uint64_t)g.M, (uint64_t)lda, 128, WD_SKB) ||
-                          !tmap_bytes_kblocks(&tw2, w, kbs, (uint64_t)g.N, (uint64_t)ldw, 128, WD_SKB)))
+    CUtensorMap ta{}, tw{};
+    if (!tmap_bytes(&ta, a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)lda, QBLOCK, WD_BM) ||
+        !tmap_bytes(&tw, w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)ldw, QBLOCK, WD_BN))
         return XPRESS_ERR_CUDA;
     const int64_t tiles = (int64_t)((g.M + WD_BM - 1) / WD_BM) * ((g.N + WD_BN - 1) / WD_BN);
-    const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
     const int es = g.bf16 ? 2 : 4;
     const int vec = aligned(g.out, 32) && g.ldo * es % 32 == 0;
-    XH_CUDA(launch_head(k_matmul_fp8_wide, dim3((unsigned)(2 * pairs)), WD_THREADS, WD_SMEM, st, 2, g, ta, tw, ta2, tw2, vec));
+    XH_CUDA(launch_head(k_matmul_fp8_wide, dim3((unsigned)(tiles < sms ? tiles : sms)), WD_THREADS, WD_SMEM, st, 1, g, ta,
+                        tw, vec));
     return XPRESS_OK;
 }
 
