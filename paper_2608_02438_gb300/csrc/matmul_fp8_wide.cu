@@ -11,9 +11,11 @@
 // instead of two large ones cover the way from a finished MMA over the epilogue
 // back to the MMA that reuses its buffer.
 //
-// Roles (640 threads): warp 0 TMA producer, warp 1 TMEM allocator and MMA
-// issuer, warps 2-3 stage the products of the scales (128 rows by the tile's 2
-// weight blocks, four K blocks at a time) in shared memory; warps 4-19
+// Roles (640 threads): warp 0 TMA producer; warps 1 and 2 MMA issuers, one for
+// each half tile (warp 1 also allocates TMEM): waiting, issuing 4 MMAs and
+// committing takes a warp longer than the tensor core takes for them; warp 3
+// stages the products of the scales (128 rows by the tile's 2 weight blocks,
+// four K blocks at a time) in shared memory; warps 4-19
 // epilogue (lane quarter warp % 4, 64 columns of a half tile) with the 64 sums
 // of a thread in registers: the first warpgroup hands registers to the others.
 #include <mutex>
@@ -48,7 +50,7 @@ struct WideBars {
     uint64_t full[WD_STAGES], empty[WD_STAGES];
     uint64_t tfull[WD_BUFS], tempty[WD_BUFS];
     uint64_t sfull[2], sempty[2];
-    uint64_t drain;
+    uint64_t drain[2];
     uint32_t tmem_base;
     int abort;
 };
@@ -106,10 +108,10 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     const int64_t tiles = (int64_t)MT * NT, first = blockIdx.x, step = gridDim.x;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < WD_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < WD_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
         for (int i = 0; i < WD_BUFS; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], WD_EPI / 2); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.sfull[i], 2); mbar_init(&sh.sempty[i], WD_EPI); }
-        mbar_init(&sh.drain, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.sfull[i], 1); mbar_init(&sh.sempty[i], WD_EPI); }
+        for (int i = 0; i < 2; ++i) mbar_init(&sh.drain[i], 1);
         sh.abort = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tmap_w);
@@ -152,47 +154,43 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             for (int st = 0; st < WD_STAGES; ++st)
                 if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
         }
-    } else if (warp == 1) {
-        // ---------------------------------------------------- MMA issuer
+    } else if (warp <= 2) {
+        // --------------------------------------------------- MMA issuers
         // the whole warp runs the loop, so that the descriptors stay in uniform
         // registers, and one elected lane issues
+        const int h = warp - 1;
         const uint32_t base_u = __shfl_sync(0xffffffffu, smem_u32(base), 0);
-        const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t d0 = __shfl_sync(0xffffffffu, tmem + h * 128, 0);
         const uint32_t lo0 = (uint32_t)smem_desc_sw128(base_u), hi = (uint32_t)(smem_desc_sw128(base_u) >> 32);
+        const uint32_t w0 = __shfl_sync(0xffffffffu, lo0 + (1 + h) * (WD_HALF >> 4), 0);
         int stage = 0;
-        uint32_t phase = 0, par = 0, tphase = 0;               // par: K block parity, which names the TMEM buffers
+        uint32_t phase = 0, par = 0, tphase = 0;               // par: K block parity, which names the TMEM buffer
         bool ok = true;
         for (int64_t t = first; t < tiles && ok; t += step) {
-            for (int kb = 0; kb < KB && ok; ++kb) {
-                ok = __all_sync(0xffffffffu, mm_wait(&sh.full[stage], phase, abort));
+            for (int kb = 0; kb < KB; ++kb) {
+                ok = mm_wait(&sh.full[stage], phase, abort) && mm_wait(&sh.tempty[par * 2 + h], tphase ^ 1, abort);
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const uint32_t a_lo = lo0 + stage * (WD_STAGE >> 4);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int buf = par * 2 + h;
-                    ok = __all_sync(0xffffffffu, mm_wait(&sh.tempty[buf], tphase ^ 1, abort));
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        tc_mma_fp8_kblock(tmem_u + buf * 128, a_lo, a_lo + (1 + h) * (WD_HALF >> 4), hi, WD_IDESC);
-                        tc_commit(&sh.tfull[buf]);
-                        if (h == 1) tc_commit(&sh.empty[stage]);
-                    }
-                    __syncwarp();
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t off = stage * (WD_STAGE >> 4);
+                    tc_mma_fp8_kblock(d0 + par * 256, lo0 + off, w0 + off, hi, WD_IDESC);
+                    tc_commit(&sh.tfull[par * 2 + h]);
+                    tc_commit(&sh.empty[stage]);
                 }
+                __syncwarp();
                 if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
                 par ^= 1;
                 if (par == 0) tphase ^= 1;
             }
         }
-        if (elect_one()) tc_commit(&sh.drain);
+        if (elect_one()) tc_commit(&sh.drain[h]);
         __syncwarp();
         int dummy = 0;
-        mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
+        mm_wait(&sh.drain[h], 0, &dummy, MM_WAIT_CYCLES / 20);
         __syncwarp();
-    } else if (warp >= 2) {
+    } else {
         // -------------------------------------------------- scale products
-        const int r0 = (warp - 2) * 32 + lane;               // rows r0 and r0 + 64 of this CTA's 128
         const bool vec4 = aligned_dev(g.sa, 16) && g.ldsa % 4 == 0;
         int slot = 0;
         uint32_t phase = 0;
@@ -200,37 +198,37 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
         for (int64_t t = first; t < tiles && ok; t += step) {
             int row, col;
             tile_at(t, MT, NT, row, col);
-            const int m = row + r0, wb = col / QBLOCK, wl = (g.N - 1) / QBLOCK;
-            const float *s0 = g.sa + (int64_t)min(m, g.M - 1) * g.ldsa, *s1 = g.sa + (int64_t)min(m + 64, g.M - 1) * g.ldsa;
+            const int wb = col / QBLOCK, wl = (g.N - 1) / QBLOCK;
             const float *w0 = g.sw + (int64_t)min(wb, wl) * g.ldsw, *w1 = g.sw + (int64_t)min(wb + 1, wl) * g.ldsw;
+            const float *s[4];                                  // rows lane, lane + 32, ...
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[r] = g.sa + (int64_t)min(row + r * 32 + lane, g.M - 1) * g.ldsa;
             for (int kb = 0; kb < KB; kb += WD_GROUP) {
-                float a0[WD_GROUP], a1[WD_GROUP], b0[WD_GROUP], b1[WD_GROUP];
-                if (vec4 && kb + WD_GROUP <= KB) {
-                    const float4 x = *reinterpret_cast<const float4 *>(s0 + kb), y = *reinterpret_cast<const float4 *>(s1 + kb);
-                    a0[0] = x.x; a0[1] = x.y; a0[2] = x.z; a0[3] = x.w;
-                    a1[0] = y.x; a1[1] = y.y; a1[2] = y.z; a1[3] = y.w;
-                } else
+                float a[4][WD_GROUP], b[2][WD_GROUP];
 #pragma unroll
-                    for (int i = 0; i < WD_GROUP; ++i) {
-                        a0[i] = kb + i < KB ? s0[kb + i] : 0.0f;
-                        a1[i] = kb + i < KB ? s1[kb + i] : 0.0f;
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    if (vec4 && kb + WD_GROUP <= KB) {
+                        const float4 x = *reinterpret_cast<const float4 *>(s[r] + kb);
+                        a[r][0] = x.x; a[r][1] = x.y; a[r][2] = x.z; a[r][3] = x.w;
+                    } else
+#pragma unroll
+                        for (int i = 0; i < WD_GROUP; ++i) a[r][i] = kb + i < KB ? s[r][kb + i] : 0.0f;
+                }
 #pragma unroll
                 for (int i = 0; i < WD_GROUP; ++i) {
-                    b0[i] = kb + i < KB ? w0[kb + i] : 0.0f;
-                    b1[i] = kb + i < KB ? w1[kb + i] : 0.0f;
+                    b[0][i] = kb + i < KB ? w0[kb + i] : 0.0f;
+                    b[1][i] = kb + i < KB ? w1[kb + i] : 0.0f;
                 }
-                if (ok) ok = mm_wait(&sh.sempty[slot], phase ^ 1, abort);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = __all_sync(0xffffffffu, mm_wait(&sh.sempty[slot], phase ^ 1, abort));
                 if (!ok) break;
-                float *f = scales + slot * (WD_SCALES / 4) + r0;
+                float *f = scales + slot * (WD_SCALES / 4) + lane;
 #pragma unroll
-                for (int i = 0; i < WD_GROUP; ++i) {
-                    f[(2 * i) * 128] = a0[i] * b0[i];
-                    f[(2 * i) * 128 + 64] = a1[i] * b0[i];
-                    f[(2 * i + 1) * 128] = a0[i] * b1[i];
-                    f[(2 * i + 1) * 128 + 64] = a1[i] * b1[i];
-                }
+                for (int i = 0; i < WD_GROUP; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        f[(2 * i) * 128 + r * 32] = a[r][i] * b[0][i];
+                        f[(2 * i + 1) * 128 + r * 32] = a[r][i] * b[1][i];
+                    }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.sfull[slot]);
                 slot ^= 1;
