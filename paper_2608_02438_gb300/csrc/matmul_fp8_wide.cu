@@ -55,20 +55,30 @@ struct WideBars {
     int abort;
 };
 
+// (x[0], x[1]) += (d[0], d[1]) * f, as one packed FMA.
+__device__ __forceinline__ void fma2(float *x, const float *d, float f)
+{
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %4};\n\t"
+        "mov.b64 c, {%0, %1};\n\t"
+        "fma.rn.f32x2 c, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, c;\n\t}"
+        : "+f"(x[0]), "+f"(x[1])
+        : "f"(d[0]), "f"(d[1]), "f"(f));
+}
+
 // 16 TMEM columns of this warp's lane quarter.
 __device__ __forceinline__ void tmem_ld16w(uint32_t taddr, float (&v)[16])
 {
-    uint32_t r[16];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
         "%14, %15}, [%16];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
         : "r"(taddr)
         : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
@@ -269,7 +279,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                         if (lane == 0) mbar_arrive(&sh.tempty[par * 2 + half]);
                     }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(d[j], f, acc[c + j]);
+                    for (int j = 0; j < 16; j += 2) fma2(acc + c + j, d + j, f);
                 }
                 par ^= 1;
                 if (par == 0) tphase ^= 1;
