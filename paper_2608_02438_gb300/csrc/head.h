@@ -136,4 +136,10 @@ int current_sms();
 // swizzle, zero fill out of bounds (base 16-byte aligned, pitch a multiple of 16).
 bool tmap_bytes(CUtensorMap *m, const void *base, uint64_t inner, uint64_t rows, uint64_t pitch, uint32_t box_inner,
                 uint32_t box_rows);
+// Byte matrix [rows][128 kblocks] as (128 columns, rows, K blocks): a box of
+// 128 x box_rows x box_kblocks lands as the K blocks' tiles of 2-D boxes, back
+// to back, with the same 128-byte swizzle.
+bool tmap_bytes_kblocks(CUtensorMap *m, const void *base, uint64_t kblocks, uint64_t rows, uint64_t pitch,
+                        uint32_t box_rows, uint32_t box_kblocks);
+
 }  // namespace xp

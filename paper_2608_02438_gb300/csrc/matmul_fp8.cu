@@ -17,9 +17,11 @@
 // travel through a lane each, 32 K blocks at a time.
 //
 // Work items are (128 weight rows, NT rows of a), dealt round-robin to
-// clusters of S CTAs.  The CTAs of a cluster split K; each leaves its sums in
-// its shared memory, and every CTA adds a share of the rows of a over the
-// cluster in rank order, so that the result does not depend on timing.
+// clusters of S CTAs.  The CTAs of a cluster split K; each sends every CTA its
+// sums of that CTA's share of the rows of a (asynchronous stores into the
+// other's shared memory, which its mbarrier counts: no cluster barrier, and a
+// sender may leave), which adds them in rank order, so that the result does not
+// depend on timing.
 #include <mutex>
 
 #include "matmul_fp8.h"
@@ -32,12 +34,13 @@ constexpr int MM_BN = 128;                             // weight rows per tile
 constexpr int MM_EPI = 4;                              // epilogue warps
 constexpr int MM_THREADS = 32 * (2 + MM_EPI);
 constexpr uint32_t MM_W_STAGE = MM_BN * QBLOCK;        // 16 KB
-constexpr int MM_MAX_STAGES = 12;
+constexpr int MM_SKB = 2;                              // K blocks of a stage
+constexpr int MM_MAX_STAGES = 6;
 
 template <int NT>
 struct MmShape {
     static constexpr uint32_t A_STAGE = NT * QBLOCK;
-    static constexpr uint32_t STAGE = MM_W_STAGE + A_STAGE;
+    static constexpr uint32_t STAGE = MM_SKB * (MM_W_STAGE + A_STAGE);   // w's K blocks, then a's
     static constexpr int NBUF = 4;
     static constexpr uint32_t TMEM_COLS = NBUF * NT;   // a power of two from 64 to 256
     static constexpr uint32_t IDESC = idesc_e4m3(MM_BN, NT);
@@ -47,7 +50,7 @@ struct MmShape {
 struct MmBars {
     uint64_t full[MM_MAX_STAGES], empty[MM_MAX_STAGES];
     uint64_t tfull[4], tempty[4];
-    uint64_t drain;
+    uint64_t drain, joined;
     uint32_t tmem_base;
     int abort;
 };
@@ -67,12 +70,27 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *v)
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// A float of CTA `rank`'s shared memory at this CTA's address `p`.
-__device__ __forceinline__ float ld_cluster(const float *p, uint32_t rank)
+// Floats to a shared::cluster address (aligned to their size), counted in bytes
+// by the mbarrier `bar` of the same CTA once they are there.
+__device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, const float *v)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr(p, rank)) : "memory");
-    return v;
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%2, %3}, [%1];" ::"r"(addr), "r"(bar),
+                 "f"(v[0]), "f"(v[1])
+                 : "memory");
+}
+__device__ __forceinline__ void st_async4(uint32_t addr, uint32_t bar, const float *v)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
+                 "r"(bar), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3])
+                 : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
 }
 
 __device__ __forceinline__ void mm_epi_bar() { asm volatile("bar.sync 1, %0;" ::"n"(MM_EPI * 32) : "memory"); }
@@ -86,7 +104,7 @@ __device__ __forceinline__ void mm_store(const MmArgs &g, int m, int n, float v)
 
 // grid: clusters of S CTAs; MM_THREADS threads.
 template <int NT>
-__global__ void __launch_bounds__(MM_THREADS, 1)
+__global__ void __launch_bounds__(MM_THREADS, 2)
     k_matmul_fp8(const __grid_constant__ MmArgs g, const __grid_constant__ CUtensorMap tmap_w,
                  const __grid_constant__ CUtensorMap tmap_a)
 {
@@ -96,12 +114,14 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
     const int stages = g.stages;
     uint8_t *after = base + stages * Sh::STAGE;
     float *table = reinterpret_cast<float *>(after);                       // [K blocks of this CTA][NT]
-    float *part = reinterpret_cast<float *>(after + g.table_bytes);        // [NT][128] (S > 1)
+    float *part = reinterpret_cast<float *>(after + g.table_bytes);        // [S][groups of vw rows of a][128][vw] (S > 1)
     __shared__ MmBars sh;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int S = g.S, rank = S > 1 ? (int)cluster_rank() : 0;
     const int KB = (g.K + QBLOCK - 1) / QBLOCK;
-    const int kb0 = (int)((int64_t)KB * rank / S), kb1 = (int)((int64_t)KB * (rank + 1) / S);
+    const int KP = (KB + MM_SKB - 1) / MM_SKB;             // stages of K, split over the cluster
+    const int kb0 = KP * rank / S * MM_SKB, kb1 = min(KB, KP * (rank + 1) / S * MM_SKB);
+    const bool whole = g.K % QBLOCK == 0;                  // the maps: (128 columns, rows, K blocks), else (K, rows)
     const int NRB = (g.N + MM_BN - 1) / MM_BN, NC = (g.M + NT - 1) / NT;
     const int64_t items = (int64_t)NRB * NC;               // item i: weight rows 128 (i / NC), rows of a NT (i % NC)
     const int64_t first = blockIdx.x / S, step = gridDim.x / S;
@@ -110,6 +130,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
         for (int i = 0; i < stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
         for (int i = 0; i < Sh::NBUF; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], MM_EPI); }
         mbar_init(&sh.drain, 1);
+        mbar_init(&sh.joined, 1);
         sh.abort = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tmap_w);
@@ -121,6 +142,7 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
     volatile int *abort = &sh.abort;
+    if (S > 1) cluster_arrive();                            // waited for before the first access to another CTA
     pdl_trigger();
     pdl_wait();
 
@@ -132,12 +154,23 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
             bool ok = true;
             for (int64_t it = first; it < items && ok; it += step) {
                 const int rb = (int)(it / NC), mc = (int)(it % NC);
-                for (int kb = kb0; kb < kb1; ++kb) {
+                for (int kb = kb0; kb < kb1; kb += MM_SKB) {
                     if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
-                    uint8_t *dst = base + stage * Sh::STAGE;
-                    mbar_expect_tx(&sh.full[stage], Sh::STAGE);
-                    tma_load_2d(dst, &tmap_w, &sh.full[stage], kb * QBLOCK, rb * MM_BN);
-                    tma_load_2d(dst + MM_W_STAGE, &tmap_a, &sh.full[stage], kb * QBLOCK, mc * NT);
+                    uint8_t *dw = base + stage * Sh::STAGE, *da = dw + MM_SKB * MM_W_STAGE;
+                    if (whole) {
+                        // one copy per operand (a copy takes the same time at 16 and
+                        // at 32 KB); a K block past the end reads as zero
+                        mbar_expect_tx(&sh.full[stage], Sh::STAGE);
+                        tma_load_3d(dw, &tmap_w, &sh.full[stage], 0, rb * MM_BN, kb);
+                        tma_load_3d(da, &tmap_a, &sh.full[stage], 0, mc * NT, kb);
+                    } else {
+                        const int n = min(MM_SKB, kb1 - kb);
+                        mbar_expect_tx(&sh.full[stage], n * (MM_W_STAGE + Sh::A_STAGE));
+                        for (int i = 0; i < n; ++i) {
+                            tma_load_2d(dw + i * MM_W_STAGE, &tmap_w, &sh.full[stage], (kb + i) * QBLOCK, rb * MM_BN);
+                            tma_load_2d(da + i * Sh::A_STAGE, &tmap_a, &sh.full[stage], (kb + i) * QBLOCK, mc * NT);
+                        }
+                    }
                     pending |= 1u << stage;
                     pend_par = (pend_par & ~(1u << stage)) | (phase << stage);
                     if (++stage == stages) { stage = 0; phase ^= 1; }
@@ -159,20 +192,23 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
         uint32_t phase = 0, tphase = 0;
         bool ok = true;
         for (int64_t it = first; it < items && ok; it += step) {
-            for (int kb = kb0; kb < kb1; ++kb) {
-                ok = mm_wait(&sh.tempty[buf], tphase ^ 1, abort) && mm_wait(&sh.full[stage], phase, abort);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t w_lo = lo0 + stage * (Sh::STAGE >> 4);
-                    tc_mma_fp8_kblock(tmem_u + buf * NT, w_lo, w_lo + (MM_W_STAGE >> 4), hi, Sh::IDESC);
-                    tc_commit(&sh.empty[stage]);
-                    tc_commit(&sh.tfull[buf]);
+            for (int kb = kb0; kb < kb1 && ok; kb += MM_SKB) {
+                ok = __all_sync(0xffffffffu, mm_wait(&sh.full[stage], phase, abort));
+                const uint32_t w_lo = lo0 + stage * (Sh::STAGE >> 4), a_lo = w_lo + (MM_SKB * MM_W_STAGE >> 4);
+                for (int i = 0; i < MM_SKB && kb + i < kb1 && ok; ++i) {
+                    ok = __all_sync(0xffffffffu, mm_wait(&sh.tempty[buf], tphase ^ 1, abort));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        tc_mma_fp8_kblock(tmem_u + buf * NT, w_lo + i * (MM_W_STAGE >> 4), a_lo + i * (Sh::A_STAGE >> 4), hi,
+                                          Sh::IDESC);
+                        tc_commit(&sh.tfull[buf]);
+                        if (i + 1 == MM_SKB || kb + i + 1 == kb1) tc_commit(&sh.empty[stage]);
+                    }
+                    __syncwarp();
+                    if (++buf == Sh::NBUF) { buf = 0; tphase ^= 1; }
                 }
-                __syncwarp();
                 if (++stage == stages) { stage = 0; phase ^= 1; }
-                if (++buf == Sh::NBUF) { buf = 0; tphase ^= 1; }
             }
         }
         if (elect_one()) tc_commit(&sh.drain);
@@ -237,30 +273,43 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
                     for (int j = 0; j < NT; ++j)
                         if (mc * NT + j < g.M) mm_store(g, mc * NT + j, n, acc[j]);
             } else {
-                // S > 1: one item per cluster (the host's grid), joined below
+                // S > 1: one item per cluster (the host's grid), joined below; rows
+                // of a travel in groups of 4 (2 where a share has no more)
+                const int share = NT / S;
+                __syncwarp();
+                cluster_wait();
+                if (share >= 4) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) part[j * MM_BN + row] = acc[j];
+                    for (int j = 0; j < NT; j += 4)
+                        if (mc * NT + j < g.M)
+                            st_async4(cluster_addr(part + ((rank * share + j % share) * MM_BN + row * 4), j / share),
+                                      cluster_addr(&sh.joined, j / share), acc + j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NT; j += 2)
+                        if (mc * NT + j < g.M)
+                            st_async2(cluster_addr(part + (rank * share * MM_BN + row * 2), j / share),
+                                      cluster_addr(&sh.joined, j / share), acc + j);
+                }
             }
         }
     }
     if (S > 1) {
-        // every thread of every CTA of the cluster comes here, whatever its role saw
         __syncwarp();
-        cluster_arrive();
-        cluster_wait();
-        const int rb = (int)(first / NC), mc = (int)(first % NC);
-        for (int i = threadIdx.x; i < (NT / S) * MM_BN; i += MM_THREADS) {
-            const int j = rank * (NT / S) + i / MM_BN, row = i % MM_BN;
-            const int m = mc * NT + j, n = rb * MM_BN + row;
-            if (m < g.M && n < g.N) {
-                float v = 0.0f;
-                for (int s = 0; s < S; ++s) v += ld_cluster(part + j * MM_BN + row, s);
-                mm_store(g, m, n, v);
-            }
+        if (warp < 2) cluster_wait();
+        const int rb = (int)(first / NC), mc = (int)(first % NC), share = NT / S, vw = share >= 4 ? 4 : 2;
+        const int m0 = mc * NT + rank * share;                 // this CTA's rows of a: m0 .. m0 + rows - 1
+        const int rows = max(0, min(share, g.M - m0)), sent = (rows + vw - 1) / vw * vw;
+        if (sent > 0) {
+            if (threadIdx.x == 0) mbar_expect_tx(&sh.joined, S * sent * MM_BN * 4);
+            if (mm_wait(&sh.joined, 0, abort))
+                for (int i = threadIdx.x; i < rows * MM_BN; i += MM_THREADS) {
+                    const int j = i / MM_BN, row = i % MM_BN, n = rb * MM_BN + row;
+                    float v = 0.0f;
+                    for (int s = 0; s < S; ++s) v += part[(s * share + j / vw * vw) * MM_BN + row * vw + j % vw];
+                    if (n < g.N) mm_store(g, m0 + j, n, v);
+                }
         }
-        __syncwarp();
-        cluster_arrive();
-        cluster_wait();
     }
     tc_fence_before();
     __syncthreads();
@@ -271,21 +320,108 @@ __global__ void __launch_bounds__(MM_THREADS, 1)
     if (threadIdx.x == 0 && sh.abort) set_status(g.status, ST_TIMEOUT);
 }
 
+// A launch's shape and its estimated time in us beyond what every launch costs
+// (about 3), from times measured on GB300:
+//   few rows   a stage (two K blocks) takes a CTA 0.58 us (NT = 16) or 0.66 (32)
+//              (16 x 4096 x 4096 without a split: 12.4 us, with S = 4: 6.0);
+//              joining a split costs about 0.6 us and 0.075 for each row of a
+//              (16 x 4096 x 512 with S = 2: 5.3 us, 4.1 without); with two CTAs
+//              on an SM a stage takes 1.43 times as long and an item 1.5 stages
+//              more; the weights stream at 6.3 TB/s
+//   many rows  0.5 us for a K block of a 128 x 256 tile, 1 to start, 2 between
+//              tiles (16 x 4096 x 4096: 18.2, 64 x 151936 x 256: 15.9); the
+//              weights stream at 5.9 TB/s
+// At 24 x 151936 x 4096 the choice is NT = 32 (96 us; 16: 102, many rows: 118),
+// at 64 x 151936 x 4096 many rows (103; 126 and 177), at 300 x 2048 x 1024
+// NT = 16 (6.1; 32: 10.3, many rows: 9.1).
+struct MmPlan {
+    int NT, S;
+    float us;
+};
+
+// Clusters of 2, 4 or 8 CTAs with an SM each that the GPU runs at a time.
+int resident_clusters(int S)
+{
+    static std::once_flag once;
+    static int n[3];
+    std::call_once(once, [] {
+        for (int i = 0; i < 3; ++i) {
+            cudaLaunchAttribute a[1];
+            a[0].id = cudaLaunchAttributeClusterDimension;
+            a[0].val.clusterDim.x = 2u << i;
+            a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
+            cudaLaunchConfig_t cfg{};
+            cfg.gridDim = dim3(2u << i);
+            cfg.blockDim = dim3(MM_THREADS);
+            cfg.dynamicSmemBytes = MM_SMEM_LIMIT - 1024;
+            cfg.attrs = a;
+            cfg.numAttrs = 1;
+            if (cudaFuncSetAttribute(k_matmul_fp8<16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)MM_SMEM_LIMIT - 1024) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n[i], k_matmul_fp8<16>, &cfg) != cudaSuccess) {
+                (void)cudaGetLastError();
+                n[i] = 0;
+            }
+        }
+    });
+    return n[S == 2 ? 0 : S == 4 ? 1 : 2];
+}
+
+MmPlan plan_few(int M, int N, int KB, int NT, int sms)
+{
+    const int KP = (KB + MM_SKB - 1) / MM_SKB;
+    const int64_t items = (int64_t)((N + MM_BN - 1) / MM_BN) * ((M + NT - 1) / NT);
+    const float stage = NT == 16 ? 0.58f : 0.66f, join = 0.6f + 0.075f * (M < NT ? M : NT);
+    if (items >= 2 * sms) {
+        const int slots = 2 * sms;
+        const float rounds = 0.5f * ((float)items / slots + (float)((items + slots - 1) / slots));
+        const float stream = (float)N * KB * QBLOCK / 6.3e6f, work = rounds * (KP + 1.5f) * stage * 1.43f;
+        return {NT, 1, stream > work ? stream : work};
+    }
+    MmPlan best{NT, 1, (float)((items + sms - 1) / sms) * KP * stage};
+    for (int S = 2; S <= 8 && S <= KP && items <= resident_clusters(S); S *= 2) {
+        const float us = (KP + S - 1) / S * stage + join;
+        if (us < best.us) best = {NT, S, us};
+    }
+    return best;
+}
+
+MmPlan plan_mm(int M, int N, int KB, int sms)
+{
+    MmPlan best = plan_few(M, N, KB, 16, sms);
+    if (M > 16) {
+        const MmPlan b = plan_few(M, N, KB, 32, sms);
+        if (b.us < best.us) best = b;
+        const int64_t tiles = (int64_t)((M + 127) / 128) * ((N + 255) / 256);
+        const float stream = (float)N * KB * QBLOCK / 5.9e6f;
+        const float work = 1.0f + 0.5f * KB + (0.5f * KB + 2.0f) * ((tiles - 1) / sms);
+        const float us = stream > work ? stream : work;
+        if (us < best.us) best = {0, 1, us};             // NT = 0: the kernel for many rows
+    }
+    return best;
+}
+
 template <int NT>
-int launch_mm(MmArgs g, const void *a, int64_t lda, const void *w, int64_t ldw, int sms, cudaStream_t st)
+int launch_mm(MmArgs g, int S, const void *a, int64_t lda, const void *w, int64_t ldw, int sms, cudaStream_t st)
 {
     using Sh = MmShape<NT>;
-    const int KB = (g.K + QBLOCK - 1) / QBLOCK;
+    const int KB = (g.K + QBLOCK - 1) / QBLOCK, KP = (KB + MM_SKB - 1) / MM_SKB;
     const int64_t items = (int64_t)((g.N + MM_BN - 1) / MM_BN) * ((g.M + NT - 1) / NT);
-    // few tiles: split K over the CTAs of a cluster, at least two K blocks each
-    int S = 1;
-    while (S < 8 && items * S * 2 <= sms && KB >= S * 4) S *= 2;
     g.S = S;
-    const size_t table = (((size_t)((KB + S - 1) / S + 1) * NT * 4) + 127) & ~size_t(127);
+    // many items: two CTAs per SM, so that one streams while the other starts,
+    // drains or stores (1 x 151936 x 256: 11.2 -> 7.8 us, 16 x 151936 x 4096: 98
+    // -> 96); a cluster has one item and takes as many stages as it has K blocks
+    // for
+    const size_t table = (size_t)((KP + S - 1) / S) * MM_SKB * NT * 4;        // a multiple of 128
     const size_t fixed = 1024 + table + (S > 1 ? Sh::PART : 0) + 1024;
-    if (fixed + 3 * Sh::STAGE > MM_SMEM_LIMIT) return XPRESS_ERR_UNSUPPORTED;
-    g.stages = (int)((MM_SMEM_LIMIT - fixed) / Sh::STAGE);
+    const int want = (KP + S - 1) / S;
+    int per_sm = items >= 2 * sms ? 2 : 1;
+    size_t limit = MM_SMEM_LIMIT / per_sm;
+    if (fixed + 2 * Sh::STAGE > limit) { limit = MM_SMEM_LIMIT; per_sm = 1; }
+    if (fixed + 2 * Sh::STAGE > limit) return XPRESS_ERR_UNSUPPORTED;
+    g.stages = (int)((limit - fixed) / Sh::STAGE);
     if (g.stages > MM_MAX_STAGES) g.stages = MM_MAX_STAGES;
+    if (S > 1 && g.stages > want) g.stages = want;
     g.table_bytes = (uint32_t)table;
     const size_t smem = fixed - 1024 + (size_t)g.stages * Sh::STAGE;
     static std::once_flag once;
@@ -294,11 +430,16 @@ int launch_mm(MmArgs g, const void *a, int64_t lda, const void *w, int64_t ldw, 
         attr = cudaFuncSetAttribute(k_matmul_fp8<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MM_SMEM_LIMIT - 1024);
     });
     if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
+    // by K blocks only where they are whole: past the last one the rows'
+    // padding would be read
     CUtensorMap tw{}, ta{};
-    if (!tmap_bytes(&tw, w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)ldw, QBLOCK, MM_BN) ||
-        !tmap_bytes(&ta, a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)lda, QBLOCK, NT))
-        return XPRESS_ERR_CUDA;
-    const int64_t grid = S > 1 ? items * S : items < sms ? items : sms;
+    const bool ok = g.K % QBLOCK == 0
+                        ? tmap_bytes_kblocks(&tw, w, (uint64_t)KB, (uint64_t)g.N, (uint64_t)ldw, MM_BN, MM_SKB) &&
+                              tmap_bytes_kblocks(&ta, a, (uint64_t)KB, (uint64_t)g.M, (uint64_t)lda, NT, MM_SKB)
+                        : tmap_bytes(&tw, w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)ldw, QBLOCK, MM_BN) &&
+                              tmap_bytes(&ta, a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)lda, QBLOCK, NT);
+    if (!ok) return XPRESS_ERR_CUDA;
+    const int64_t grid = S > 1 ? items * S : items < per_sm * sms ? items : per_sm * sms;
     XH_CUDA(launch_head(k_matmul_fp8<NT>, dim3((unsigned)grid), MM_THREADS, smem, st, (unsigned)S, g, tw, ta));
     return XPRESS_OK;
 }
@@ -334,7 +475,8 @@ extern "C" int xpress_matmul_fp8(const xpress_matmul_args *in, void *ws, size_t 
     g.bf16 = in->out_dtype == XPRESS_BF16;
     g.status = static_cast<int32_t *>(ws);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (in->M > 64) return launch_mm_wide(g, in->a, in->lda, in->w, in->ldw, sms, st);
-    if (in->M <= 16) return launch_mm<16>(g, in->a, in->lda, in->w, in->ldw, sms, st);
-    return launch_mm<32>(g, in->a, in->lda, in->w, in->ldw, sms, st);
+    const MmPlan p = plan_mm(in->M, in->N, KB, sms);
+    if (p.NT == 16) return launch_mm<16>(g, p.S, in->a, in->lda, in->w, in->ldw, sms, st);
+    if (p.NT == 32) return launch_mm<32>(g, p.S, in->a, in->lda, in->w, in->ldw, sms, st);
+    return launch_mm_wide(g, in->a, in->lda, in->w, in->ldw, sms, st);
 }

@@ -1035,6 +1035,20 @@ bool tmap_bytes(CUtensorMap *m, const void *base, uint64_t inner, uint64_t rows,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool tmap_bytes_kblocks(CUtensorMap *m, const void *base, uint64_t kblocks, uint64_t rows, uint64_t pitch,
+                        uint32_t box_rows, uint32_t box_kblocks)
+{
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {128, rows, kblocks};
+    cuuint64_t strides[2] = {pitch, 128};
+    cuuint32_t box[3] = {128, box_rows, box_kblocks};
+    cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int current_sms()
 {
     constexpr int MAX_DEVICES = 64;
