@@ -67,6 +67,71 @@ __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ float load1(const uint16_t *p) { return bf2f(*p); }
 __device__ __forceinline__ float load1(const float *p) { return *p; }
 
+// 8 elements as they are stored.
+template <typename T> struct Raw8;
+template <> struct Raw8<uint16_t> { uint4 a; };
+template <> struct Raw8<float> { float4 a, b; };
+
+__device__ __forceinline__ void unpack(const Raw8<uint16_t> &r, float (&v)[8])
+{
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const Raw8<float> &r, float (&v)[8])
+{
+    v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
+    v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+}
+// 8 elements from p (`n` of them exist); VEC: p is 16-byte aligned.
+template <bool VEC>
+__device__ __forceinline__ Raw8<uint16_t> load_raw(const uint16_t *p, int n)
+{
+    if (VEC && n >= 8) return {*reinterpret_cast<const uint4 *>(p)};
+    uint32_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : 0u;
+    return {make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16)};
+}
+template <bool VEC>
+__device__ __forceinline__ Raw8<float> load_raw(const float *p, int n)
+{
+    if (VEC && n >= 8) return {*reinterpret_cast<const float4 *>(p), *reinterpret_cast<const float4 *>(p + 4)};
+    float e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : 0.0f;
+    return {make_float4(e[0], e[1], e[2], e[3]), make_float4(e[4], e[5], e[6], e[7])};
+}
+__device__ __forceinline__ void pack(const float (&v)[8], Raw8<uint16_t> &r)
+{
+    r.a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void pack(const float (&v)[8], Raw8<float> &r)
+{
+    r.a = make_float4(v[0], v[1], v[2], v[3]);
+    r.b = make_float4(v[4], v[5], v[6], v[7]);
+}
+// The bits of the largest magnitude as fp32 (a NaN's are above all others).
+__device__ __forceinline__ uint32_t amax8(const Raw8<uint16_t> &r)
+{
+    // two bf16 magnitudes per word, compared as 16-bit unsigned integers
+    const uint32_t m = __vmaxu2(__vmaxu2(r.a.x & 0x7fff7fffu, r.a.y & 0x7fff7fffu),
+                                __vmaxu2(r.a.z & 0x7fff7fffu, r.a.w & 0x7fff7fffu));
+    return max(m << 16, m & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t amax8(const Raw8<float> &r)
+{
+    float v[8];
+    unpack(r, v);
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+    return m;
+}
+
 // Division by a group's scale.  x / s as x times 1 / s with the remainder put
 // back, q + (x - q s) / s, which rounds as the division does (ties between
 // e4m3 values are common: inputs of few bits over a scale made of one of them)

@@ -11,14 +11,22 @@
 // that the result does not depend on the compiler), one rounding to the
 // storage type at the end.
 //
-// A CTA takes a range of the vocabulary for all rows of one sequence.  It
-// counts the history's tokens that fall into its range in shared memory (every
-// CTA of a sequence reads the whole history, from L2), then streams the rows.
-// A thread owns the same ids in every row, so the block's tokens are added to
-// the counts by their owners without a barrier, and a register holds one bit
-// per owned id that has a count or a bias: the others pass through untouched.
-// HBM bound for many rows (each logit read and written once); for one row
-// bound by the latency of offsets -> history -> counts.
+// A CTA takes a share of the vocabulary for all rows of one sequence: every
+// G-th segment of 256 ids, so that the frequent tokens, which vocabularies keep
+// together, are spread over the CTAs.  Ids with a count or a bias are few, and
+// their arithmetic (a division among it) would run in nearly every warp if it
+// sat in the stream of the rows, so the work is split:
+//   counts  the history's tokens that fall into the share, in shared memory
+//           (every CTA of a sequence reads the whole history, from L2), and a
+//           list of the ids that have a count, a bias or a place in the block
+//   stream  rows in 16-byte pieces, each read while the one before it is worked
+//           on: the mask, the copy and the packed maximum of the ids that are
+//           not listed; listed ids pass unchanged
+//   patch   after every 4 rows, while they are in L2, their listed ids, read
+//           once more and rewritten, with their own maximum (after all rows of a
+//           large batch they would come from and go to HBM, 32 bytes each)
+// Each warp leaves its argmax keys; a second kernel takes the largest of a
+// row's.
 #include "head.h"
 
 namespace xp {
@@ -46,58 +54,17 @@ struct LogitsArgs {
     int mask_rows;
     const int32_t *mask_row;
     float mask_value;
-    unsigned long long *part;      // [n_seq * rows][8 gridDim.x] argmax keys (0: none), or NULL
+    int patch;                     // a rule on single ids is given
+    uint32_t magic;                // ceil(2^32 / gridDim.x)
+    unsigned long long *part;      // [n_seq * rows][gridDim.x][8 (1 + patch)] argmax keys (0: none), or NULL
 };
 
 constexpr int LT = 256;            // threads: 8 warps
+constexpr int64_t MAX_ENTRIES = 1 << 30;     // of history and bias
+constexpr int MAX_V = 1 << 24;     // so that Share's division by multiplication is exact ((V / 256) (V / 2048) < 2^32)
 constexpr int LWARPS = LT / 32;
-constexpr uint32_t IN_PROMPT = 1u << 31;
+constexpr uint32_t IN_PROMPT = 1u << 31, IN_BLOCK = 1u << 30, TIMES = IN_BLOCK - 1;   // of a count
 
-template <typename T> struct Raw8;
-template <> struct Raw8<uint16_t> { uint4 a; };
-template <> struct Raw8<float> { float4 a, b; };
-
-__device__ __forceinline__ void unpack(const Raw8<uint16_t> &r, float (&v)[8])
-{
-    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void unpack(const Raw8<float> &r, float (&v)[8])
-{
-    v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
-    v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
-}
-__device__ __forceinline__ Raw8<uint16_t> repack(const float (&v)[8], uint16_t)
-{
-    return {make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]))};
-}
-__device__ __forceinline__ Raw8<float> repack(const float (&v)[8], float)
-{
-    return {make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7])};
-}
-// 8 elements from p (`n` of them exist); VEC: p is 16-byte aligned.
-template <bool VEC>
-__device__ __forceinline__ Raw8<uint16_t> load_raw(const uint16_t *p, int n)
-{
-    if (VEC && n >= 8) return {*reinterpret_cast<const uint4 *>(p)};
-    uint32_t e[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : 0u;
-    return {make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16)};
-}
-template <bool VEC>
-__device__ __forceinline__ Raw8<float> load_raw(const float *p, int n)
-{
-    if (VEC && n >= 8) return {*reinterpret_cast<const float4 *>(p), *reinterpret_cast<const float4 *>(p + 4)};
-    float e[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : 0.0f;
-    return {make_float4(e[0], e[1], e[2], e[3]), make_float4(e[4], e[5], e[6], e[7])};
-}
 template <bool VEC>
 __device__ __forceinline__ void store_raw(uint16_t *p, int n, const Raw8<uint16_t> &r)
 {
@@ -122,215 +89,366 @@ __device__ __forceinline__ void store_raw(float *p, int n, const Raw8<float> &r)
         if (j < n) p[j] = v[j];
 }
 
-// Sequence q's entries o0 .. o0 + n - 1 of an array of `total` (offsets cut to it).
-__device__ __forceinline__ void range_of(const int64_t *off, int q, int64_t total, int64_t &o0, int64_t &n)
+// The elements of r whose bit in `keep` is clear become `other`.
+__device__ __forceinline__ void select8(Raw8<uint16_t> &r, uint32_t keep, float other)
 {
-    o0 = min(max(off[q], (int64_t)0), total);
-    n = max(min(off[q + 1], total) - o0, (int64_t)0);
+    const uint32_t o = f2bf(other), oo = o | o << 16;
+    uint32_t *w = reinterpret_cast<uint32_t *>(&r.a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t b = keep >> (2 * i);
+        const uint32_t m = ((b & 1u) ? 0xffffu : 0u) | ((b & 2u) ? 0xffff0000u : 0u);
+        w[i] = (w[i] & m) | (oo & ~m);
+    }
+}
+__device__ __forceinline__ void select8(Raw8<float> &r, uint32_t keep, float other)
+{
+    float *v = reinterpret_cast<float *>(&r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (keep >> i & 1u) ? v[i] : other;
+}
+// The largest element, NaNs apart.
+__device__ __forceinline__ float max8(const Raw8<uint16_t> &r)
+{
+    const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&r.a);
+    const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float max8(const Raw8<float> &r)
+{
+    return fmaxf(fmaxf(fmaxf(r.a.x, r.a.y), fmaxf(r.a.z, r.a.w)), fmaxf(fmaxf(r.b.x, r.b.y), fmaxf(r.b.z, r.b.w)));
 }
 
-// Counts one history token of position `pos` that falls into [c0, c0 + C).
-template <int C>
-__device__ __forceinline__ void count_token(uint32_t *cnt, int c0, int t, bool prompt)
+// The order-preserving word of argmax_key, -0 as 0.
+__device__ __forceinline__ uint32_t order_word(float v)
 {
-    const uint32_t i = (uint32_t)t - (uint32_t)c0;
-    if (t >= 0 && i < (uint32_t)C) {
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+// The warp's argmax key: the lanes' largest `top` words, the smallest id among them.
+__device__ __forceinline__ unsigned long long warp_key(uint32_t mine, uint32_t top, uint32_t id)
+{
+    id = __reduce_min_sync(0xffffffffu, mine == top ? id : 0xffffffffu);
+    return id == 0xffffffffu ? 0ull : ((unsigned long long)top << 32) | (0xffffffffu - id);
+}
+
+// Sequence q's entries o0 .. o0 + n - 1 of an array of `total` < 2^31 (offsets cut to it).
+__device__ __forceinline__ void range_of(const int64_t *off, int q, int64_t total, int64_t &o0, int &n)
+{
+    o0 = min(max(off[q], (int64_t)0), total);
+    n = (int)max(min(off[q + 1], total) - o0, (int64_t)0);
+}
+
+// Where a CTA of G keeps its ids: id SEG (G i + blockIdx.x) + r is its element
+// SEG i + r.
+constexpr int SEG_BITS = 8, SEG = 1 << SEG_BITS;
+struct Share {
+    uint32_t G, blk, magic;
+    __device__ __forceinline__ int id(int at) const
+    {
+        return (int)((((uint32_t)at >> SEG_BITS) * G + blk) << SEG_BITS | (at & (SEG - 1)));
+    }
+    // the element of id t, or a number of no element of any share
+    __device__ __forceinline__ uint32_t at(int t) const
+    {
+        // (negative ids end up past every share's elements)
+        const uint32_t seg = (uint32_t)t >> SEG_BITS, i = G == 1 ? seg : __umulhi(seg, magic);
+        return i * G + blk == seg ? i << SEG_BITS | (t & (SEG - 1)) : 0xffffffffu;
+    }
+};
+
+// Counts one history token.
+__device__ __forceinline__ void count_token(uint32_t *cnt, const Share &sh, int size, int t, bool prompt)
+{
+    const uint32_t i = sh.at(t);
+    if (i < (uint32_t)size) {
         if (prompt) atomicOr(cnt + i, IN_PROMPT);
         else atomicAdd(cnt + i, 1u);
     }
 }
 
-// grid (vocabulary ranges of 2048 U ids, sequences); shared memory: counts and,
-// with a bias, as many floats.
-template <typename T, bool VEC, int U>
-__global__ void __launch_bounds__(LT) k_logits(const __grid_constant__ LogitsArgs a)
+// grid (shares of 2048 U ids, sequences); shared memory with patch: counts [C],
+// with a bias as many floats, the list [C] (16 bits).  MULTI: several rows.
+template <typename T, bool VEC, int U, bool MULTI>
+__global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __grid_constant__ LogitsArgs a)
 {
     constexpr int C = LT * 8 * U;
-    extern __shared__ uint32_t cnt[];              // [C]: IN_PROMPT | times answered
-    uint32_t *bias = cnt + C;                      // [C]: the bias as fp32 bits (while being built: entry + 1)
+    constexpr int PR = MULTI ? 4 : 1;              // rows patched together
+    __shared__ int listed;
+    extern __shared__ uint32_t cnt[];              // [C]: IN_PROMPT | IN_BLOCK | times answered
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const int q = blockIdx.y, c0 = blockIdx.x * C, V = a.V, R = a.rows;
+    const int q = blockIdx.y, V = a.V, R = a.rows;
+    const Share sh{gridDim.x, blockIdx.x, a.magic};
     const bool has_bias = a.bias_ids != nullptr;
+    uint32_t *bias = cnt + C;                      // [C]: the bias as fp32 bits (while being built: entry + 1)
+    uint16_t *list = reinterpret_cast<uint16_t *>(has_bias ? bias + C : bias);
     pdl_trigger();
-    for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
-    if (has_bias)
-        for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(bias)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) listed = 0;
+    if (a.patch) {
+        for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
+        if (has_bias)
+            for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(bias)[i] = make_uint4(0, 0, 0, 0);
+    }
     pdl_wait();
-
-    const float rep = a.rep ? a.rep[q] : 1.0f, freq = a.freq ? a.freq[q] : 0.0f, pres = a.pres ? a.pres[q] : 0.0f;
-    const bool penal = rep != 1.0f || freq != 0.0f || pres != 0.0f;
-    __syncthreads();
-    if (penal && a.hist) {
-        int64_t o0, n;
-        range_of(a.hist_off, q, a.n_hist, o0, n);
-        const int64_t plen = a.prompt_len ? a.prompt_len[q] : 0;
-        const int32_t *h = a.hist + o0;
-        int64_t head = (int64_t)((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4;
-        if (head > n) head = n;
-        if (tid < head) count_token<C>(cnt, c0, h[tid], tid < plen);
-        const int4 *h4 = reinterpret_cast<const int4 *>(h + head);
-        const int64_t n4 = n > head ? (n - head) / 4 : 0;
-        constexpr int UN = 4;
-        for (int64_t i0 = tid; i0 < n4; i0 += UN * LT) {
-            int4 t[UN];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) t[u] = i0 + u * LT < n4 ? h4[i0 + u * LT] : make_int4(-1, -1, -1, -1);
-#pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                const int64_t p = head + 4 * (i0 + u * LT);
-                count_token<C>(cnt, c0, t[u].x, p < plen);
-                count_token<C>(cnt, c0, t[u].y, p + 1 < plen);
-                count_token<C>(cnt, c0, t[u].z, p + 2 < plen);
-                count_token<C>(cnt, c0, t[u].w, p + 3 < plen);
-            }
-        }
-        const int64_t tail = head + 4 * n4 + tid;
-        if (tid < 4 && tail < n) count_token<C>(cnt, c0, h[tail], tail < plen);
-    }
-    int64_t b0 = 0;
-    if (has_bias) {
-        // of several entries for one id the last one counts
-        int64_t n;
-        range_of(a.bias_off, q, a.n_bias, b0, n);
-        for (int64_t i = tid; i < n; i += LT) {
-            const int t = a.bias_ids[b0 + i];
-            const uint32_t k = (uint32_t)t - (uint32_t)c0;
-            if (t >= 0 && k < (uint32_t)C) atomicMax(bias + k, (uint32_t)i + 1);
-        }
-    }
-    __syncthreads();
-
-    // slot u of this thread: ids c0 + 2048 u + 8 tid + 0 .. 7; bit 8 u + k of
-    // `special`: id k of slot u has a count or a bias
-    uint32_t special = 0;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int s = u * LT * 8 + tid * 8;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            bool on = cnt[s + k] != 0;
-            if (has_bias && bias[s + k]) {
-                bias[s + k] = __float_as_uint(a.bias_val[b0 + bias[s + k] - 1]);
-                on = true;
-            }
-            if (on) special |= 1u << (8 * u + k);
-        }
-    }
 
     const int64_t n0 = (int64_t)q * R;
     const T *in = static_cast<const T *>(a.in) + n0 * a.ld;
     T *out = a.out ? static_cast<T *>(a.out) + n0 * a.ldo : nullptr;
     const bool in_place = a.out == a.in && a.ld == a.ldo;
-    const int id0 = c0 + tid * 8;
+    // slot u of this thread: its elements 2048 u + 8 tid + 0 .. 7, with the ids
+    // id0 + u id_step + 0 .. 7; their bits are 8 u + k
+    const int id0 = sh.id(tid * 8), id_step = LT * 8 * (int)gridDim.x;
+    uint32_t inside = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int n = min(max(V - id0 - u * id_step, 0), 8);
+        inside |= ((1u << n) - 1u) << (8 * u);
+    }
 
-    auto load_row = [&](int j, Raw8<T> (&x)[U], uint32_t &allow) {
-        allow = 0xffffffffu;
-        if (j >= R) return;
+    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
+    int64_t b0 = 0;
+    uint32_t special = 0;
+    if (a.patch) {
+        // all that does not depend on one another is asked for at once
+        int64_t o0 = 0;
+        int n = 0, bn = 0, plen = 0;
+        if (a.hist) range_of(a.hist_off, q, a.n_hist, o0, n);
+        if (a.hist && a.prompt_len) plen = a.prompt_len[q];
+        if (has_bias) range_of(a.bias_off, q, a.n_bias, b0, bn);
+        if (a.rep) rep = a.rep[q];
+        if (a.freq) freq = a.freq[q];
+        if (a.pres) pres = a.pres[q];
+        const int32_t *h = a.hist + o0;
+        const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4, n);
+        const int4 *h4 = reinterpret_cast<const int4 *>(h + head);
+        const int n4 = (n - head) / 4;
+        constexpr int UN = 4;
+        auto fetch = [&](int i0, int4 (&t)[UN]) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int id = id0 + u * LT * 8;
-            if (id < V) x[u] = load_raw<VEC>(in + j * a.ld + id, V - id);
-        }
-        if (a.mask) {
-            const int64_t mr = a.mask_row ? (int64_t)a.mask_row[n0 + j] : n0 + j;
-            if (mr >= 0 && mr < a.mask_rows) {
-                const uint8_t *m = reinterpret_cast<const uint8_t *>(a.mask + mr * a.ld_mask);
-                allow = 0;
+            for (int u = 0; u < UN; ++u) t[u] = i0 + u * LT < n4 ? h4[i0 + u * LT] : make_int4(-1, -1, -1, -1);
+        };
+        int4 nt[UN];
+        fetch(tid, nt);
+        const bool penal = rep != 1.0f || freq != 0.0f || pres != 0.0f;
+        __syncthreads();
+        if (penal) {
+            if (tid < head) count_token(cnt, sh, C, h[tid], tid < plen);
+            for (int i0 = tid; i0 < n4; i0 += UN * LT) {
+                int4 t[UN];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int id = id0 + u * LT * 8;
-                    if (id < V) allow |= (uint32_t)m[id / 8] << (8 * u);
+                for (int u = 0; u < UN; ++u) t[u] = nt[u];
+                fetch(i0 + UN * LT, nt);           // under way while this piece is counted
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                    const int p = head + 4 * (i0 + u * LT);
+                    count_token(cnt, sh, C, t[u].x, p < plen);
+                    count_token(cnt, sh, C, t[u].y, p + 1 < plen);
+                    count_token(cnt, sh, C, t[u].z, p + 2 < plen);
+                    count_token(cnt, sh, C, t[u].w, p + 3 < plen);
                 }
             }
+            const int tail = head + 4 * n4 + tid;
+            if (tid < 4 && tail < n) count_token(cnt, sh, C, h[tail], tail < plen);
+            if (a.draft)
+                for (int i = tid; i < R - 1; i += LT) {
+                    const uint32_t k = sh.at(a.draft[q * a.ld_draft + i]);
+                    if (k < (uint32_t)C) atomicOr(cnt + k, IN_BLOCK);
+                }
+        }
+        // of several bias entries for one id the last one counts
+        for (int i = tid; i < bn; i += LT) {
+            const uint32_t k = sh.at(a.bias_ids[b0 + i]);
+            if (k < (uint32_t)C) atomicMax(bias + k, (uint32_t)i + 1);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = u * LT * 8 + tid * 8;
+            const uint4 lo = *reinterpret_cast<const uint4 *>(cnt + s), hi = *reinterpret_cast<const uint4 *>(cnt + s + 4);
+            const uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c[k]) special |= 1u << (8 * u + k);
+            if (has_bias) {
+                const uint4 bl = *reinterpret_cast<const uint4 *>(bias + s), bh = *reinterpret_cast<const uint4 *>(bias + s + 4);
+                const uint32_t e[8] = {bl.x, bl.y, bl.z, bl.w, bh.x, bh.y, bh.z, bh.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (e[k]) {
+                        bias[s + k] = __float_as_uint(a.bias_val[b0 + e[k] - 1]);
+                        special |= 1u << (8 * u + k);
+                    }
+            }
+        }
+        special &= inside;
+        if (special) {
+            int at = atomicAdd(&listed, __popc(special));
+            for (uint32_t b = special; b; b &= b - 1) {
+                const int i = __ffs(b) - 1;
+                list[at++] = (uint16_t)(i / 8 * LT * 8 + tid * 8 + i % 8);
+            }
+        }
+    }
+
+    const int slots = LWARPS * (1 + a.patch);
+    unsigned long long *part = a.part ? a.part + (n0 * gridDim.x + blockIdx.x) * slots + warp : nullptr;
+    auto mask_of = [&](int j) -> const uint8_t * {
+        if (!a.mask || j >= R) return nullptr;
+        const int64_t mr = a.mask_row ? (int64_t)a.mask_row[n0 + j] : n0 + j;
+        return mr >= 0 && mr < a.mask_rows ? reinterpret_cast<const uint8_t *>(a.mask + mr * a.ld_mask) : nullptr;
+    };
+    auto fetch_row = [&](int j, Raw8<T> (&x)[U]) {
+        if (j >= R) return;
+        const T *row = in + (int64_t)j * a.ld;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = id0 + u * id_step;
+            if (id < V) x[u] = load_raw<VEC>(row + id, V - id);
+        }
+    };
+    // bytes of a row's mask, as they are stored: arithmetic on them here would
+    // wait for them here
+    auto fetch_bits = [&](const uint8_t *mask, uint32_t (&bits)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = id0 + u * id_step;
+            if (mask && id < V) bits[u] = mask[id / 8];
         }
     };
 
     Raw8<T> nx[U];
-    uint32_t nallow = 0;
-    load_row(0, nx, nallow);
+    uint32_t nbits[U];
+    const uint8_t *mask = nullptr, *mask1 = mask_of(0), *mask2 = MULTI ? mask_of(1) : nullptr;   // of rows j, j + 1, j + 2
+    fetch_bits(mask1, nbits);
+    fetch_row(0, nx);
+    const uint8_t *pmask = nullptr;                // of the row that this thread patches
     for (int j = 0; j < R; ++j) {
-        Raw8<T> x[U];
-        const uint32_t allow = nallow;
+        struct { Raw8<T> x[U]; } cur;
+        uint32_t bits[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = nx[u];
-        load_row(j + 1, nx, nallow);
-        if (j > 0 && a.draft && penal) {
-            const int t = a.draft[q * a.ld_draft + j - 1];
-            const uint32_t i = (uint32_t)t - (uint32_t)c0;
-            if (t >= 0 && i < (uint32_t)C && (i / 8) % LT == (uint32_t)tid) {
-                cnt[i] += 1;
-                special |= 1u << (8 * (i / (8 * LT)) + i % 8);
-            }
+        for (int u = 0; u < U; ++u) { cur.x[u] = nx[u]; bits[u] = nbits[u]; }
+        mask = mask1;
+        mask1 = mask2;
+        if (MULTI) {
+            mask2 = mask_of(j + 2);
+            fetch_bits(mask1, nbits);
+            fetch_row(j + 1, nx);
         }
-        float best = -INFINITY;
-        int best_id = -1;
+        if (a.patch && j % PR == 0) pmask = mask_of(j + tid % PR);
+        T *orow = out + (int64_t)j * a.ldo;
+        uint32_t allow = 0xffffffffu;
+        if (mask) {
+            allow = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) allow |= bits[u] << (8 * u);
+        }
+        const uint32_t use = allow & inside & ~special;
+        float mx[U], m = -INFINITY;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int id = id0 + u * LT * 8;
+            const int id = id0 + u * id_step;
+            mx[u] = -INFINITY;
             if (id >= V) continue;
-            const uint32_t al = (allow >> (8 * u)) & 0xffu, sp = (special >> (8 * u)) & 0xffu;
-            float v[8];
-            unpack(x[u], v);
-            const bool touched = sp != 0 || al != 0xffu;
-            if (touched) {
+            const uint32_t keep = (allow | special) >> (8 * u) & 0xffu;
+            if (keep != 0xffu) select8(cur.x[u], keep, a.mask_value);
+            if (out && !(in_place && keep == 0xffu)) store_raw<VEC>(orow + id, V - id, cur.x[u]);
+            if (part) {
+                const uint32_t us = use >> (8 * u) & 0xffu;
+                Raw8<T> y = cur.x[u];
+                if (us != 0xffu) select8(y, us, -INFINITY);
+                mx[u] = max8(y);
+                m = fmaxf(m, mx[u]);
+            }
+        }
+        if (part) {
+            const uint32_t mine = order_word(m), top = __reduce_max_sync(0xffffffffu, mine);
+            uint32_t id = 0xffffffffu;
+            if (mine == top) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (sp >> k & 1) {
-                        const int s = u * LT * 8 + tid * 8 + k;
-                        const uint32_t c = cnt[s], times = c & ~IN_PROMPT;
-                        if (c) v[k] = v[k] > 0.0f ? __fdiv_rn(v[k], rep) : __fmul_rn(v[k], rep);
-                        if (times) {
-                            v[k] = __fsub_rn(v[k], __fmul_rn(freq, (float)times));
-                            v[k] = __fsub_rn(v[k], pres);
-                        }
-                        if (has_bias) v[k] = __fadd_rn(v[k], __uint_as_float(bias[s]));
+                for (int u = U - 1; u >= 0; --u)
+                    if (mx[u] == m) {
+                        float v[8];
+                        unpack(cur.x[u], v);
+#pragma unroll
+                        for (int k = 7; k >= 0; --k)
+                            if ((use >> (8 * u + k) & 1u) && v[k] == m) id = id0 + u * id_step + k;
                     }
-                    if (!(al >> k & 1)) v[k] = a.mask_value;
+            }
+            const unsigned long long key = warp_key(mine, top, id);
+            if (lane == 0) part[(int64_t)j * gridDim.x * slots] = key;
+        }
+        if (a.patch && (j % PR == PR - 1 || j == R - 1)) {
+            __syncthreads();                       // the list, and the rows as they were copied
+            const int j0 = j - j % PR, jr = j0 + tid % PR, n = jr <= j ? listed : 0;
+            const T *row = in + (int64_t)jr * a.ld;
+            uint32_t word = 0, pid = 0xffffffffu;
+            constexpr int EU = 4, ES = LT / PR;    // ids in flight, threads of a row
+            for (int e0 = tid / PR; e0 < n; e0 += EU * ES) {
+                T raw[EU];
+                uint32_t mb[EU];
+                int at[EU];
+#pragma unroll
+                for (int i = 0; i < EU; ++i) {
+                    const int e = e0 + i * ES;
+                    at[i] = list[e < n ? e : e0];
+                    const int v = sh.id(at[i]);
+                    raw[i] = row[v];
+                    mb[i] = pmask ? pmask[v / 8] : 0xffu;
                 }
-                x[u] = repack(v, T{});
-                unpack(x[u], v);
-            }
-            if (out && !(in_place && !touched)) store_raw<VEC>(out + j * a.ldo + id, V - id, x[u]);
-            if (a.part) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if ((al >> k & 1) && id + k < V && (v[k] > best || (best_id < 0 && v[k] == v[k]))) {
-                        best = v[k];
-                        best_id = id + k;
+                for (int i = 0; i < EU; ++i) {
+                    if (e0 + i * ES >= n) continue;
+                    const int v = sh.id(at[i]);
+                    const bool ok = mb[i] >> (v % 8) & 1u;
+                    const uint32_t c = cnt[at[i]];
+                    uint32_t times = c & TIMES;
+                    if (c & IN_BLOCK)
+                        for (int t = 0; t < jr; ++t) times += a.draft[q * a.ld_draft + t] == v;
+                    float y = load1(&raw[i]);
+                    if (times || (c & IN_PROMPT)) y = y > 0.0f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+                    if (times) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, (float)times)), pres);
+                    if (has_bias) y = __fadd_rn(y, __uint_as_float(bias[at[i]]));
+                    if (!ok) y = a.mask_value;
+                    if (sizeof(T) == 2) y = bf2f(f2bf(y));
+                    if (out) store1(out + (int64_t)jr * a.ldo + v, y);
+                    if (ok && y == y) {
+                        const uint32_t w = order_word(y);
+                        if (w > word || (w == word && (uint32_t)v < pid)) { word = w; pid = v; }
                     }
+                }
             }
+            if (part)
+#pragma unroll
+                for (int r = 0; r < PR; ++r) {
+                    const bool mine = tid % PR == r;
+                    const uint32_t w = mine ? word : 0, top = __reduce_max_sync(0xffffffffu, w);
+                    const unsigned long long key = warp_key(w, top, mine ? pid : 0xffffffffu);
+                    if (lane == 0 && j0 + r <= j) part[(int64_t)(j0 + r) * gridDim.x * slots + LWARPS] = key;
+                }
         }
-        if (a.part) {
-            // the warp's first maximum: the largest value, then the smallest id (-0 counts as 0)
-            const unsigned long long key = best_id < 0 ? 0ull : argmax_key(best + 0.0f, best_id);
-            const uint32_t hi = (uint32_t)(key >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-            const uint32_t lo = __reduce_max_sync(0xffffffffu, hi == top ? (uint32_t)key : 0u);
-            if (lane == 0)
-                a.part[(n0 + j) * (gridDim.x * LWARPS) + blockIdx.x * LWARPS + warp] =
-                    ((unsigned long long)top << 32) | lo;
-        }
+        if (!MULTI) break;
     }
 }
 
-// grid ceil(rows / 8), 256 threads: warp w combines the n keys of row 8 blockIdx.x + w.
-__global__ void __launch_bounds__(256) k_logits_argmax(const unsigned long long *part, int n, int64_t rows,
-                                                        int32_t *argmax)
+// grid: rows; 256 threads: the largest of a row's n keys.
+__global__ void __launch_bounds__(256) k_logits_argmax(const unsigned long long *part, int n, int32_t *argmax)
 {
-    const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    __shared__ unsigned long long best_of[8];
+    const int64_t row = blockIdx.x;
     const int lane = threadIdx.x % 32;
     pdl_trigger();
     pdl_wait();
-    if (row >= rows) return;
     unsigned long long best = 0;
-    for (int i = lane; i < n; i += 32) {
-        const unsigned long long k = part[row * n + i];
-        if (k > best) best = k;
-    }
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 256) best = max(best, part[row * n + i]);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const unsigned long long k = __shfl_xor_sync(0xffffffffu, best, o);
-        if (k > best) best = k;
-    }
+    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (lane == 0) best_of[threadIdx.x / 32] = best;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    best = best_of[lane % 8];
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
     if (lane == 0) {
         float v;
         int id = -1;
@@ -339,27 +457,36 @@ __global__ void __launch_bounds__(256) k_logits_argmax(const unsigned long long 
     }
 }
 
-// Slots per thread: ranges of 2048, 4096 or 8192 ids, the largest that still
-// gives every SM two CTAs.
+// Slots per thread: shares of 2048, 4096 or 8192 ids, the largest that still
+// gives every SM four CTAs.
 int logits_slots(int n_seq, int V, int sms)
 {
     int U = 4;
-    while (U > 1 && (int64_t)n_seq * ((V + LT * 8 * U - 1) / (LT * 8 * U)) < 2 * sms) U /= 2;
+    while (U > 1 && (int64_t)n_seq * ((V + LT * 8 * U - 1) / (LT * 8 * U)) < 4 * sms) U /= 2;
     return U;
+}
+
+template <typename T, bool VEC, int U, bool MULTI>
+cudaError_t launch_logits_u(LogitsArgs a, int n_seq, cudaStream_t st)
+{
+    constexpr int C = LT * 8 * U;
+    static const cudaError_t attr =
+        cudaFuncSetAttribute(k_logits<T, VEC, U, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, C * 10);
+    if (attr != cudaSuccess) { (void)cudaGetLastError(); return attr; }
+    const size_t smem = a.patch ? (size_t)C * (a.bias_ids ? 10 : 6) : 0;
+    const unsigned G = (a.V + C - 1) / C;
+    a.magic = (uint32_t)(((1ull << 32) + G - 1) / G);
+    return launch_head(k_logits<T, VEC, U, MULTI>, dim3(G, n_seq), LT, smem, st, 1, a);
 }
 
 template <typename T, bool VEC>
 cudaError_t launch_logits(const LogitsArgs &a, int n_seq, int U, cudaStream_t st)
 {
-    const int C = LT * 8 * U;
-    const dim3 grid((a.V + C - 1) / C, n_seq);
-    const size_t smem = (size_t)C * 4 * (a.bias_ids ? 2 : 1);
-    auto *k = U == 1 ? k_logits<T, VEC, 1> : U == 2 ? k_logits<T, VEC, 2> : k_logits<T, VEC, 4>;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
-    }
-    return launch_head(k, grid, LT, smem, st, 1, a);
+    if (a.rows > 1)
+        return U == 1 ? launch_logits_u<T, VEC, 1, true>(a, n_seq, st)
+             : U == 2 ? launch_logits_u<T, VEC, 2, true>(a, n_seq, st) : launch_logits_u<T, VEC, 4, true>(a, n_seq, st);
+    return U == 1 ? launch_logits_u<T, VEC, 1, false>(a, n_seq, st)
+         : U == 2 ? launch_logits_u<T, VEC, 2, false>(a, n_seq, st) : launch_logits_u<T, VEC, 4, false>(a, n_seq, st);
 }
 
 }  // namespace
@@ -370,7 +497,7 @@ using namespace xp;
 extern "C" size_t xpress_process_logits_workspace_size(int n_seq, int rows, int V)
 {
     if (n_seq < 1 || rows < 1 || V < 1) return 0;
-    return (size_t)n_seq * rows * ((V + LT * 8 - 1) / (LT * 8)) * LWARPS * 8;
+    return (size_t)n_seq * rows * ((V + LT * 8 - 1) / (LT * 8)) * 2 * LWARPS * 8;
 }
 
 extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, size_t ws_bytes, void *stream)
@@ -378,7 +505,8 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
     if (!in || in->n_seq < 0 || in->rows < 1 || in->V < 1 || !in->logits || (!in->out && !in->argmax) ||
         in->ld < in->V || (in->out && in->ldo < in->V))
         return XPRESS_ERR_INVALID_ARG;
-    if ((in->dtype != XPRESS_F32 && in->dtype != XPRESS_BF16) || in->n_seq > 65535 || in->V > MAX_DIM)
+    if ((in->dtype != XPRESS_F32 && in->dtype != XPRESS_BF16) || in->n_seq > 65535 || in->V > MAX_V ||
+        (int64_t)in->n_seq * in->rows > 0x7fffffff || in->n_history > MAX_ENTRIES || in->n_bias > MAX_ENTRIES)
         return XPRESS_ERR_UNSUPPORTED;
     if ((in->history && (!in->history_offsets || in->n_history < 0)) ||
         (in->bias_ids && (!in->bias_values || !in->bias_offsets || in->n_bias < 0)) ||
@@ -407,6 +535,7 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
     a.bias_ids = in->bias_ids; a.bias_val = in->bias_values; a.n_bias = in->n_bias; a.bias_off = in->bias_offsets;
     a.mask = in->mask; a.ld_mask = in->ld_mask; a.mask_rows = in->mask_rows; a.mask_row = in->mask_row;
     a.mask_value = in->mask_value;
+    a.patch = in->repetition || in->frequency || in->presence || in->bias_ids;
     a.part = in->argmax ? static_cast<unsigned long long *>(ws) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int U = logits_slots(in->n_seq, in->V, sms);
@@ -418,10 +547,9 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
                 : (vec ? launch_logits<float, true>(a, in->n_seq, U, st)
                        : launch_logits<float, false>(a, in->n_seq, U, st)));
     if (in->argmax) {
-        const int64_t rows = (int64_t)in->n_seq * in->rows;
-        const int n = (in->V + LT * 8 * U - 1) / (LT * 8 * U) * LWARPS;
-        XH_CUDA(launch_head(k_logits_argmax, dim3((unsigned)((rows + 7) / 8)), 256, 0, st, 1,
-                            (const unsigned long long *)ws, n, rows, in->argmax));
+        const int n = (in->V + LT * 8 * U - 1) / (LT * 8 * U) * LWARPS * (1 + a.patch);
+        XH_CUDA(launch_head(k_logits_argmax, dim3((unsigned)(in->n_seq * in->rows)), 256, 0, st, 1,
+                            (const unsigned long long *)ws, n, in->argmax));
     }
     return XPRESS_OK;
 }

@@ -91,6 +91,8 @@ def _logits(**kw):
     (dict(n_history=-1), BAD), (dict(bias_values=None), BAD), (dict(bias_offsets=None), BAD), (dict(n_bias=-1), BAD),
     (dict(ld_draft=1), BAD), (dict(ld_mask=31), BAD), (dict(mask_rows=-1), BAD), (dict(logits=4097), BAD),
     (dict(history_offsets=4100), BAD), (dict(mask_row=4098), BAD), (dict(dtype=3), UNS), (dict(n_seq=65536), UNS),
+    (dict(V=(1 << 24) + 1, ld=1 << 25, ldo=1 << 25, ld_mask=1 << 20), UNS), (dict(n_history=(1 << 30) + 1), UNS),
+    (dict(n_bias=(1 << 30) + 1), UNS),
     (dict(n_seq=0), OK)])
 def test_logits_refusals(lib, kw, want):
     size = 1 << 24
