@@ -457,8 +457,10 @@ int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws
  *           set = allowed; row n is masked by mask row mask_row[n] (mask_row
  *           NULL: by row n), and not at all where that is not in
  *           [0, mask_rows)
- * xpress_refine_block takes rows with a finite mask_value (e.g. -1e30), so
- * that a row that its mask left empty still has a token.
+ * For rows that go on to xpress_refine_block or xpress_accept give a finite
+ * mask_value that is far below every logit but of moderate size, e.g. -8192: a
+ * row of -inf alone has no softmax, and their exponentials carry the rounding of
+ * l / T, which must stay far below 1.
  * out may be logits (same pitch) or NULL (argmax only).  workspace: >=
  * xpress_process_logits_workspace_size bytes, 256-byte aligned, needed for
  * argmax only (else it may be NULL).

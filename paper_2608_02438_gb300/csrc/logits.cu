@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
     const bool has_bias = a.bias_ids != nullptr;
     uint32_t *bias = cnt + C;                      // [C]: the bias as fp32 bits (while being built: entry + 1)
     uint16_t *list = reinterpret_cast<uint16_t *>(has_bias ? bias + C : bias);
-    pdl_trigger();
+    if (a.part) pdl_trigger();                     // k_logits_argmax may start and wait
     if (tid == 0) listed = 0;
     if (a.patch) {
         for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
@@ -436,7 +436,6 @@ __global__ void __launch_bounds__(256) k_logits_argmax(const unsigned long long 
     __shared__ unsigned long long best_of[8];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x % 32;
-    pdl_trigger();
     pdl_wait();
     unsigned long long best = 0;
 #pragma unroll 4

@@ -143,7 +143,6 @@ __global__ void __launch_bounds__(MM_THREADS, 2)
     const uint32_t tmem = sh.tmem_base;
     volatile int *abort = &sh.abort;
     if (S > 1) cluster_arrive();                            // waited for before the first access to another CTA
-    pdl_trigger();
     pdl_wait();
 
     if (warp == 0) {

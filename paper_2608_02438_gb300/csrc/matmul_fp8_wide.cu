@@ -134,7 +134,6 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     const uint32_t tmem = sh.tmem_base;
     volatile int *abort = &sh.abort;
     float *scales = reinterpret_cast<float *>(base + WD_STAGES * WD_STAGE + WD_EPI * WD_TILE);
-    pdl_trigger();
     pdl_wait();
 
     if (warp < 4) {

@@ -25,7 +25,6 @@ __global__ void __launch_bounds__(QT, sizeof(T) == 2 ? 4 : 2)
     __shared__ uint32_t part[QT / 32];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rb = blockIdx.x / ncb, c0 = blockIdx.x % ncb * QBLOCK;
-    pdl_trigger();
     pdl_wait();
     // VEC: slot i is row 32 i + thread / 16, columns 8 (thread % 16) + j;
     // else slot i holds rows 32 i + 2 warp + (j / 4), columns 32 (j % 4) + lane

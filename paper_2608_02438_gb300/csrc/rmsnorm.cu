@@ -110,7 +110,6 @@ __global__ void __launch_bounds__(THREADS, FEW ? 1 : 2048 / THREADS) k_rmsnorm(c
     constexpr int WARPS = THREADS / 32;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, H = a.H;
     const int64_t r = blockIdx.x;
-    pdl_trigger();
     pdl_wait();
     const T *x = static_cast<const T *>(a.x) + r * a.ldx;
     const T *res = a.residual ? static_cast<const T *>(a.residual) + r * a.ldr : nullptr;
