@@ -11,7 +11,7 @@
 // that the result does not depend on the compiler), one rounding to the
 // storage type at the end.
 //
-// A CTA takes a share of the vocabulary for all rows of one sequence: every
+// A CTA takes a share of the vocabulary for the rows of one sequence: every
 // G-th segment of 256 ids, so that the frequent tokens, which vocabularies keep
 // together, are spread over the CTAs.  Ids with a count or a bias are few, and
 // their arithmetic (a division among it) would run in nearly every warp if it
@@ -38,6 +38,7 @@ struct LogitsArgs {
     void *out;
     int64_t ld, ldo;
     int rows, V;
+    int rows_each;                 // rows of a CTA
     const float *rep, *freq, *pres;
     const int32_t *hist;
     int64_t n_hist;
@@ -56,7 +57,7 @@ struct LogitsArgs {
     float mask_value;
     int patch;                     // a rule on single ids is given
     uint32_t magic;                // ceil(2^32 / gridDim.x)
-    unsigned long long *part;      // [n_seq * rows][gridDim.x][8 (1 + patch)] argmax keys (0: none), or NULL
+    unsigned long long *part;      // [n_seq * rows][gridDim.x][8, with patch NT / 32 more] argmax keys (0: none), or NULL
 };
 
 constexpr int LT = 256;            // threads: 8 warps
@@ -167,10 +168,11 @@ __device__ __forceinline__ void count_token(uint32_t *cnt, const Share &sh, int 
     }
 }
 
-// grid (shares of 2048 U ids, sequences); shared memory with patch: counts [C],
+// grid (shares of 2048 U ids, sequences, parts of the rows); shared memory with patch: counts [C],
 // with a bias as many floats, the list [C] (16 bits).  MULTI: several rows.
-template <typename T, bool VEC, int U, bool MULTI>
-__global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __grid_constant__ LogitsArgs a)
+// NT: LT threads, or more, of which those past LT count and patch only.
+template <typename T, bool VEC, int U, bool MULTI, int NT>
+__global__ void __launch_bounds__(NT, NT > LT ? 1 : MULTI && U == 4 ? 2 : 4) k_logits(const __grid_constant__ LogitsArgs a)
 {
     constexpr int C = LT * 8 * U;
     constexpr int PR = MULTI ? 4 : 1;              // rows patched together
@@ -178,16 +180,18 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
     extern __shared__ uint32_t cnt[];              // [C]: IN_PROMPT | IN_BLOCK | times answered
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int q = blockIdx.y, V = a.V, R = a.rows;
+    const int jb = blockIdx.z * a.rows_each, je = min(jb + a.rows_each, R);     // this CTA's rows
     const Share sh{gridDim.x, blockIdx.x, a.magic};
+    const bool streams = NT == LT || tid < LT;
     const bool has_bias = a.bias_ids != nullptr;
     uint32_t *bias = cnt + C;                      // [C]: the bias as fp32 bits (while being built: entry + 1)
     uint16_t *list = reinterpret_cast<uint16_t *>(has_bias ? bias + C : bias);
     if (a.part) pdl_trigger();                     // k_logits_argmax may start and wait
     if (tid == 0) listed = 0;
     if (a.patch) {
-        for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < C / 4; i += NT) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0, 0, 0, 0);
         if (has_bias)
-            for (int i = tid; i < C / 4; i += LT) reinterpret_cast<uint4 *>(bias)[i] = make_uint4(0, 0, 0, 0);
+            for (int i = tid; i < C / 4; i += NT) reinterpret_cast<uint4 *>(bias)[i] = make_uint4(0, 0, 0, 0);
     }
     pdl_wait();
 
@@ -195,7 +199,7 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
     const T *in = static_cast<const T *>(a.in) + n0 * a.ld;
     T *out = a.out ? static_cast<T *>(a.out) + n0 * a.ldo : nullptr;
     const bool in_place = a.out == a.in && a.ld == a.ldo;
-    // slot u of this thread: its elements 2048 u + 8 tid + 0 .. 7, with the ids
+    // slot u of a thread that streams: its elements 2048 u + 8 tid + 0 .. 7, with the ids
     // id0 + u id_step + 0 .. 7; their bits are 8 u + k
     const int id0 = sh.id(tid * 8), id_step = LT * 8 * (int)gridDim.x;
     uint32_t inside = 0;
@@ -225,7 +229,7 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
         constexpr int UN = 4;
         auto fetch = [&](int i0, int4 (&t)[UN]) {
 #pragma unroll
-            for (int u = 0; u < UN; ++u) t[u] = i0 + u * LT < n4 ? h4[i0 + u * LT] : make_int4(-1, -1, -1, -1);
+            for (int u = 0; u < UN; ++u) t[u] = i0 + u * NT < n4 ? h4[i0 + u * NT] : make_int4(-1, -1, -1, -1);
         };
         int4 nt[UN];
         fetch(tid, nt);
@@ -233,14 +237,14 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
         __syncthreads();
         if (penal) {
             if (tid < head) count_token(cnt, sh, C, h[tid], tid < plen);
-            for (int i0 = tid; i0 < n4; i0 += UN * LT) {
+            for (int i0 = tid; i0 < n4; i0 += UN * NT) {
                 int4 t[UN];
 #pragma unroll
                 for (int u = 0; u < UN; ++u) t[u] = nt[u];
-                fetch(i0 + UN * LT, nt);           // under way while this piece is counted
+                fetch(i0 + UN * NT, nt);           // under way while this piece is counted
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
-                    const int p = head + 4 * (i0 + u * LT);
+                    const int p = head + 4 * (i0 + u * NT);
                     count_token(cnt, sh, C, t[u].x, p < plen);
                     count_token(cnt, sh, C, t[u].y, p + 1 < plen);
                     count_token(cnt, sh, C, t[u].z, p + 2 < plen);
@@ -250,19 +254,20 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
             const int tail = head + 4 * n4 + tid;
             if (tid < 4 && tail < n) count_token(cnt, sh, C, h[tail], tail < plen);
             if (a.draft)
-                for (int i = tid; i < R - 1; i += LT) {
+                for (int i = tid; i < R - 1; i += NT) {
                     const uint32_t k = sh.at(a.draft[q * a.ld_draft + i]);
                     if (k < (uint32_t)C) atomicOr(cnt + k, IN_BLOCK);
                 }
         }
         // of several bias entries for one id the last one counts
-        for (int i = tid; i < bn; i += LT) {
+        for (int i = tid; i < bn; i += NT) {
             const uint32_t k = sh.at(a.bias_ids[b0 + i]);
             if (k < (uint32_t)C) atomicMax(bias + k, (uint32_t)i + 1);
         }
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (!streams) break;
             const int s = u * LT * 8 + tid * 8;
             const uint4 lo = *reinterpret_cast<const uint4 *>(cnt + s), hi = *reinterpret_cast<const uint4 *>(cnt + s + 4);
             const uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
@@ -290,15 +295,15 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
         }
     }
 
-    const int slots = LWARPS * (1 + a.patch);
+    const int slots = LWARPS + a.patch * (NT / 32);
     unsigned long long *part = a.part ? a.part + (n0 * gridDim.x + blockIdx.x) * slots + warp : nullptr;
     auto mask_of = [&](int j) -> const uint8_t * {
-        if (!a.mask || j >= R) return nullptr;
+        if (!a.mask || j >= je) return nullptr;
         const int64_t mr = a.mask_row ? (int64_t)a.mask_row[n0 + j] : n0 + j;
         return mr >= 0 && mr < a.mask_rows ? reinterpret_cast<const uint8_t *>(a.mask + mr * a.ld_mask) : nullptr;
     };
     auto fetch_row = [&](int j, Raw8<T> (&x)[U]) {
-        if (j >= R) return;
+        if (j >= je) return;
         const T *row = in + (int64_t)j * a.ld;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -318,71 +323,76 @@ __global__ void __launch_bounds__(LT, MULTI && U == 4 ? 2 : 4) k_logits(const __
 
     Raw8<T> nx[U];
     uint32_t nbits[U];
-    const uint8_t *mask = nullptr, *mask1 = mask_of(0), *mask2 = MULTI ? mask_of(1) : nullptr;   // of rows j, j + 1, j + 2
-    fetch_bits(mask1, nbits);
-    fetch_row(0, nx);
+    const uint8_t *mask = nullptr, *mask1 = mask_of(jb), *mask2 = MULTI ? mask_of(jb + 1) : nullptr;   // of rows j, j + 1, j + 2
+    if (streams) {
+        fetch_bits(mask1, nbits);
+        fetch_row(jb, nx);
+    }
     const uint8_t *pmask = nullptr;                // of the row that this thread patches
-    for (int j = 0; j < R; ++j) {
-        struct { Raw8<T> x[U]; } cur;
-        uint32_t bits[U];
+    for (int j = jb; j < je; ++j) {
+        const int in_group = (j - jb) % PR;
+        if (a.patch && in_group == 0) pmask = mask_of(j + tid % PR);
+        if (streams) {
+            struct { Raw8<T> x[U]; } cur;
+            uint32_t bits[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) { cur.x[u] = nx[u]; bits[u] = nbits[u]; }
-        mask = mask1;
-        mask1 = mask2;
-        if (MULTI) {
-            mask2 = mask_of(j + 2);
-            fetch_bits(mask1, nbits);
-            fetch_row(j + 1, nx);
-        }
-        if (a.patch && j % PR == 0) pmask = mask_of(j + tid % PR);
-        T *orow = out + (int64_t)j * a.ldo;
-        uint32_t allow = 0xffffffffu;
-        if (mask) {
-            allow = 0;
+            for (int u = 0; u < U; ++u) { cur.x[u] = nx[u]; bits[u] = nbits[u]; }
+            mask = mask1;
+            mask1 = mask2;
+            if (MULTI) {
+                mask2 = mask_of(j + 2);
+                fetch_bits(mask1, nbits);
+                fetch_row(j + 1, nx);
+            }
+            T *orow = out + (int64_t)j * a.ldo;
+            uint32_t allow = 0xffffffffu;
+            if (mask) {
+                allow = 0;
 #pragma unroll
-            for (int u = 0; u < U; ++u) allow |= bits[u] << (8 * u);
-        }
-        const uint32_t use = allow & inside & ~special;
-        float mx[U], m = -INFINITY;
+                for (int u = 0; u < U; ++u) allow |= bits[u] << (8 * u);
+            }
+            const uint32_t use = allow & inside & ~special;
+            float mx[U], m = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int id = id0 + u * id_step;
-            mx[u] = -INFINITY;
-            if (id >= V) continue;
-            const uint32_t keep = (allow | special) >> (8 * u) & 0xffu;
-            if (keep != 0xffu) select8(cur.x[u], keep, a.mask_value);
-            if (out && !(in_place && keep == 0xffu)) store_raw<VEC>(orow + id, V - id, cur.x[u]);
+            for (int u = 0; u < U; ++u) {
+                const int id = id0 + u * id_step;
+                mx[u] = -INFINITY;
+                if (id >= V) continue;
+                const uint32_t keep = (allow | special) >> (8 * u) & 0xffu;
+                if (keep != 0xffu) select8(cur.x[u], keep, a.mask_value);
+                if (out && !(in_place && keep == 0xffu)) store_raw<VEC>(orow + id, V - id, cur.x[u]);
+                if (part) {
+                    const uint32_t us = use >> (8 * u) & 0xffu;
+                    Raw8<T> y = cur.x[u];
+                    if (us != 0xffu) select8(y, us, -INFINITY);
+                    mx[u] = max8(y);
+                    m = fmaxf(m, mx[u]);
+                }
+            }
             if (part) {
-                const uint32_t us = use >> (8 * u) & 0xffu;
-                Raw8<T> y = cur.x[u];
-                if (us != 0xffu) select8(y, us, -INFINITY);
-                mx[u] = max8(y);
-                m = fmaxf(m, mx[u]);
+                const uint32_t mine = order_word(m), top = __reduce_max_sync(0xffffffffu, mine);
+                uint32_t id = 0xffffffffu;
+                if (mine == top) {
+#pragma unroll
+                    for (int u = U - 1; u >= 0; --u)
+                        if (mx[u] == m) {
+                            float v[8];
+                            unpack(cur.x[u], v);
+#pragma unroll
+                            for (int k = 7; k >= 0; --k)
+                                if ((use >> (8 * u + k) & 1u) && v[k] == m) id = id0 + u * id_step + k;
+                        }
+                }
+                const unsigned long long key = warp_key(mine, top, id);
+                if (lane == 0) part[(int64_t)j * gridDim.x * slots] = key;
             }
         }
-        if (part) {
-            const uint32_t mine = order_word(m), top = __reduce_max_sync(0xffffffffu, mine);
-            uint32_t id = 0xffffffffu;
-            if (mine == top) {
-#pragma unroll
-                for (int u = U - 1; u >= 0; --u)
-                    if (mx[u] == m) {
-                        float v[8];
-                        unpack(cur.x[u], v);
-#pragma unroll
-                        for (int k = 7; k >= 0; --k)
-                            if ((use >> (8 * u + k) & 1u) && v[k] == m) id = id0 + u * id_step + k;
-                    }
-            }
-            const unsigned long long key = warp_key(mine, top, id);
-            if (lane == 0) part[(int64_t)j * gridDim.x * slots] = key;
-        }
-        if (a.patch && (j % PR == PR - 1 || j == R - 1)) {
+        if (a.patch && (in_group == PR - 1 || j == je - 1)) {
             __syncthreads();                       // the list, and the rows as they were copied
-            const int j0 = j - j % PR, jr = j0 + tid % PR, n = jr <= j ? listed : 0;
+            const int j0 = j - in_group, jr = j0 + tid % PR, n = jr <= j ? listed : 0;
             const T *row = in + (int64_t)jr * a.ld;
             uint32_t word = 0, pid = 0xffffffffu;
-            constexpr int EU = 4, ES = LT / PR;    // ids in flight, threads of a row
+            constexpr int EU = 4, ES = NT / PR;    // ids in flight, threads of a row
             for (int e0 = tid / PR; e0 < n; e0 += EU * ES) {
                 T raw[EU];
                 uint32_t mb[EU];
@@ -456,36 +466,56 @@ __global__ void __launch_bounds__(256) k_logits_argmax(const unsigned long long 
     }
 }
 
+constexpr int LT_FEW = 512;        // threads of a CTA that has an SM for itself and a long history
+
+struct LogitsPlan {
+    int U, threads, rows_each;
+};
+
 // Slots per thread: shares of 2048, 4096 or 8192 ids, the largest that still
-// gives every SM four CTAs.
-int logits_slots(int n_seq, int V, int sms)
+// gives every SM four CTAs.  Few CTAs: a sequence's rows are split over several
+// (each counts for itself) until there are two per SM.  Where not even every SM
+// gets one and histories are long, a CTA takes 512 threads for the counts and the
+// patch (6 sequences of 30000 tokens, V = 32003, 5 rows: 32 -> 21 us; a short
+// history gains nothing).
+LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, int sms)
 {
-    int U = 4;
-    while (U > 1 && (int64_t)n_seq * ((V + LT * 8 * U - 1) / (LT * 8 * U)) < 4 * sms) U /= 2;
-    return U;
+    LogitsPlan p{4, LT, a.rows};
+    auto ctas = [&] { return (int64_t)n_seq * ((a.V + LT * 8 * p.U - 1) / (LT * 8 * p.U)); };
+    while (p.U > 1 && ctas() < 4 * sms) p.U /= 2;
+    if (p.U == 1 && a.patch && ctas() <= sms && a.n_hist >= 8192 * (int64_t)n_seq) p.threads = LT_FEW;
+    else if (p.U == 1)
+        while (p.rows_each > 4 && ctas() * ((a.rows + p.rows_each - 1) / p.rows_each) < 2 * sms)
+            p.rows_each = (p.rows_each + 1) / 2;
+    return p;
 }
 
-template <typename T, bool VEC, int U, bool MULTI>
+template <typename T, bool VEC, int U, bool MULTI, int NT>
 cudaError_t launch_logits_u(LogitsArgs a, int n_seq, cudaStream_t st)
 {
     constexpr int C = LT * 8 * U;
     static const cudaError_t attr =
-        cudaFuncSetAttribute(k_logits<T, VEC, U, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, C * 10);
+        cudaFuncSetAttribute(k_logits<T, VEC, U, MULTI, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C * 10);
     if (attr != cudaSuccess) { (void)cudaGetLastError(); return attr; }
     const size_t smem = a.patch ? (size_t)C * (a.bias_ids ? 10 : 6) : 0;
     const unsigned G = (a.V + C - 1) / C;
     a.magic = (uint32_t)(((1ull << 32) + G - 1) / G);
-    return launch_head(k_logits<T, VEC, U, MULTI>, dim3(G, n_seq), LT, smem, st, 1, a);
+    return launch_head(k_logits<T, VEC, U, MULTI, NT>, dim3(G, n_seq, (a.rows + a.rows_each - 1) / a.rows_each), NT, smem, st, 1, a);
+}
+
+template <typename T, bool VEC, bool MULTI>
+cudaError_t launch_logits_r(const LogitsArgs &a, int n_seq, const LogitsPlan &p, cudaStream_t st)
+{
+    return p.threads == LT_FEW ? launch_logits_u<T, VEC, 1, MULTI, LT_FEW>(a, n_seq, st)
+         : p.U == 1 ? launch_logits_u<T, VEC, 1, MULTI, LT>(a, n_seq, st)
+         : p.U == 2 ? launch_logits_u<T, VEC, 2, MULTI, LT>(a, n_seq, st)
+                    : launch_logits_u<T, VEC, 4, MULTI, LT>(a, n_seq, st);
 }
 
 template <typename T, bool VEC>
-cudaError_t launch_logits(const LogitsArgs &a, int n_seq, int U, cudaStream_t st)
+cudaError_t launch_logits(const LogitsArgs &a, int n_seq, const LogitsPlan &p, cudaStream_t st)
 {
-    if (a.rows > 1)
-        return U == 1 ? launch_logits_u<T, VEC, 1, true>(a, n_seq, st)
-             : U == 2 ? launch_logits_u<T, VEC, 2, true>(a, n_seq, st) : launch_logits_u<T, VEC, 4, true>(a, n_seq, st);
-    return U == 1 ? launch_logits_u<T, VEC, 1, false>(a, n_seq, st)
-         : U == 2 ? launch_logits_u<T, VEC, 2, false>(a, n_seq, st) : launch_logits_u<T, VEC, 4, false>(a, n_seq, st);
+    return a.rows > 1 ? launch_logits_r<T, VEC, true>(a, n_seq, p, st) : launch_logits_r<T, VEC, false>(a, n_seq, p, st);
 }
 
 }  // namespace
@@ -496,7 +526,7 @@ using namespace xp;
 extern "C" size_t xpress_process_logits_workspace_size(int n_seq, int rows, int V)
 {
     if (n_seq < 1 || rows < 1 || V < 1) return 0;
-    return (size_t)n_seq * rows * ((V + LT * 8 - 1) / (LT * 8)) * 2 * LWARPS * 8;
+    return (size_t)n_seq * rows * ((V + LT * 8 - 1) / (LT * 8)) * (LWARPS + LT_FEW / 32) * 8;
 }
 
 extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, size_t ws_bytes, void *stream)
@@ -537,16 +567,17 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
     a.patch = in->repetition || in->frequency || in->presence || in->bias_ids;
     a.part = in->argmax ? static_cast<unsigned long long *>(ws) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int U = logits_slots(in->n_seq, in->V, sms);
+    const LogitsPlan plan = logits_plan(a, in->n_seq, sms);
+    a.rows_each = plan.rows_each;
     const bool vec = aligned(in->logits, 16) && in->ld * es % 16 == 0 &&
                      (!in->out || (aligned(in->out, 16) && in->ldo * es % 16 == 0));
     XH_CUDA(in->dtype == XPRESS_BF16
-                ? (vec ? launch_logits<uint16_t, true>(a, in->n_seq, U, st)
-                       : launch_logits<uint16_t, false>(a, in->n_seq, U, st))
-                : (vec ? launch_logits<float, true>(a, in->n_seq, U, st)
-                       : launch_logits<float, false>(a, in->n_seq, U, st)));
+                ? (vec ? launch_logits<uint16_t, true>(a, in->n_seq, plan, st)
+                       : launch_logits<uint16_t, false>(a, in->n_seq, plan, st))
+                : (vec ? launch_logits<float, true>(a, in->n_seq, plan, st)
+                       : launch_logits<float, false>(a, in->n_seq, plan, st)));
     if (in->argmax) {
-        const int n = (in->V + LT * 8 * U - 1) / (LT * 8 * U) * LWARPS * (1 + a.patch);
+        const int C = LT * 8 * plan.U, n = (in->V + C - 1) / C * (LWARPS + a.patch * (plan.threads / 32));
         XH_CUDA(launch_head(k_logits_argmax, dim3((unsigned)(in->n_seq * in->rows)), 256, 0, st, 1,
                             (const unsigned long long *)ws, n, in->argmax));
     }
