@@ -369,7 +369,8 @@ def matmul_fp8(a, a_scale, w, w_scale, out, stream=None) -> int:
     """out [M, N] (bf16 or fp32) = a w^T for e4m3 a [M, K] with a_scale fp32
     [M, ceil(K / 128)] and e4m3 w [N, K] with w_scale fp32 [ceil(N / 128),
     ceil(K / 128)] (see xpress_matmul_fp8).  Asynchronous; returns XPRESS_OK;
-    matmul_fp8_status() reads the device status of the calls so far."""
+    matmul_fp8_status() reads the device status of the calls so far.  The first
+    call on a device makes the status word: not inside a graph capture."""
     return _call("matmul_fp8", stream, a, a_scale, w, w_scale, out)
 
 

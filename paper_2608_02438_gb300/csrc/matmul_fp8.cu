@@ -10,9 +10,9 @@
 // registers with its scales, sum[n, m] += (sa sw) d[n, m], while the MMAs of
 // the next K blocks fill the other buffers.
 //
-// Roles (192 threads): warp 0 TMA producer (a 128 x 128 box of w and an
-// NT x 128 box of a per K block into a ring), warp 1 TMEM allocator and MMA
-// issuer, warps 2-5 epilogue (one TMEM lane quarter each).  The scales of the
+// Roles (192 threads): warp 0 TMA producer (two K blocks of 128 rows of w and of
+// NT rows of a at a time into a ring), warp 1 TMEM allocator and MMA issuer,
+// warps 2-5 epilogue (one TMEM lane quarter each).  The scales of the
 // NT rows of a over the CTA's K range stay in shared memory; those of w
 // travel through a lane each, 32 K blocks at a time.
 //
@@ -22,6 +22,10 @@
 // other's shared memory, which its mbarrier counts: no cluster barrier, and a
 // sender may leave), which adds them in rank order, so that the result does not
 // depend on timing.
+//
+// Bound by the weights' stream for large w (16 x 151936 x 4096: 96 us, 6.5 TB/s
+// of w alone), by the chain first copy - MMAs - join - store for small ones
+// (1 x 4096 x 4096: 5.9 us).
 #include <mutex>
 
 #include "matmul_fp8.h"
@@ -54,21 +58,6 @@ struct MmBars {
     uint32_t tmem_base;
     int abort;
 };
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *v)
-{
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
-        "%14, %15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
 
 // Floats to a shared::cluster address (aligned to their size), counted in bytes
 // by the mbarrier `bar` of the same CTA once they are there.
@@ -301,7 +290,8 @@ __global__ void __launch_bounds__(MM_THREADS, 2)
         const int rows = max(0, min(share, g.M - m0)), sent = (rows + vw - 1) / vw * vw;
         if (sent > 0) {
             if (threadIdx.x == 0) mbar_expect_tx(&sh.joined, S * sent * MM_BN * 4);
-            if (mm_wait(&sh.joined, 0, abort))
+            // (longer than any sender's own waits, which end in its stores)
+            if (mm_wait(&sh.joined, 0, abort, 3 * MM_WAIT_CYCLES))
                 for (int i = threadIdx.x; i < rows * MM_BN; i += MM_THREADS) {
                     const int j = i / MM_BN, row = i % MM_BN, n = rb * MM_BN + row;
                     float v = 0.0f;

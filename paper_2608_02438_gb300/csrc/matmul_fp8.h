@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank)
 }
 
 // Bounded wait for a phase of `bar`.  It polls (a wait with a sleep hint wakes
-// up later: 2048 x 38912 x 4096 took 739 us against 683) and bounds itself by
+// up later: an earlier form at 2048 x 38912 x 4096 took 739 us against 683) and bounds itself by
 // the SM's cycle counter, read once in 64 polls: the global timer's latency
 // would sit in every hand-off of a K block.
 constexpr long long MM_WAIT_CYCLES = 4000000000ll;       // about 2 s
@@ -92,6 +92,19 @@ __device__ __forceinline__ void tc_mma_fp8_kblock(uint32_t d_tmem, uint32_t a_lo
         "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %10, t;}"
         ::"r"(d_tmem), "r"(a_lo), "r"(a_lo + 2), "r"(a_lo + 4), "r"(a_lo + 6), "r"(b_lo), "r"(b_lo + 2), "r"(b_lo + 4),
         "r"(b_lo + 6), "r"(hi), "r"(idesc)
+        : "memory");
+}
+
+// 16 TMEM columns of this warp's lane quarter.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *v)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(taddr)
         : "memory");
 }
 

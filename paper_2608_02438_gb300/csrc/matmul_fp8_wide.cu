@@ -15,9 +15,17 @@
 // each half tile (warp 1 also allocates TMEM): waiting, issuing 4 MMAs and
 // committing takes a warp longer than the tensor core takes for them; warp 3
 // stages the products of the scales (128 rows by the tile's 2 weight blocks,
-// four K blocks at a time) in shared memory; warps 4-19
-// epilogue (lane quarter warp % 4, 64 columns of a half tile) with the 64 sums
-// of a thread in registers: the first warpgroup hands registers to the others.
+// four K blocks at a time) in shared memory; warps 4-19 epilogue (lane quarter
+// warp % 4, 64 columns of a half tile) with the 64 sums of a thread in
+// registers: the first warpgroup hands registers to the others.
+//
+// Measured at 2048 x 38912 x 4096: 284 us, 2.3 PFLOP/s; the MMAs and their
+// hand-offs alone take 191 us, with the operands' copies 224, with the TMEM loads
+// 210.  What binds is the epilogue: 64 FMAs (32 packed) and 4 TMEM loads per
+// thread and K block on 16 warps.  One issuer warp took 379 us, unpacked FMAs
+// 321, a pair of CTAs on a 256 x 256 tile with two TMEM buffers 568 (each K block
+// waited for the other CTA's epilogue); sharing copies in clusters of 2 or 4 CTAs
+// by multicast gained nothing.
 #include <mutex>
 
 #include "matmul_fp8.h"
@@ -40,9 +48,9 @@ constexpr int WD_STAGES = 4;
 constexpr uint32_t WD_IDESC = idesc_e4m3(128, 128);
 constexpr int WD_BUFS = 4;                              // TMEM buffers: K block parity, half
 constexpr int WD_TCOLS = 8;                             // columns of a transpose
-constexpr size_t WD_TILE = 32 * (WD_TCOLS + 1) * 4;
+constexpr size_t WD_TILE = 32 * (WD_TCOLS + 1) * 4;     // a warp's transpose
 constexpr int WD_GROUP = 4;                             // K blocks whose scales are staged together
-constexpr size_t WD_SCALES = WD_GROUP * 2 * 128 * 4;    // [K block][weight block][row]                 // a warp's transpose
+constexpr size_t WD_SCALES = WD_GROUP * 2 * 128 * 4;    // [K block][weight block][row]
 constexpr size_t WD_SMEM = 1024 + WD_STAGES * WD_STAGE + WD_EPI * WD_TILE + 2 * WD_SCALES;
 constexpr int WD_BAND = 32;                             // row tiles that share the weights while they are in L2
 
@@ -66,19 +74,6 @@ __device__ __forceinline__ void fma2(float *x, const float *d, float f)
         "mov.b64 {%0, %1}, c;\n\t}"
         : "+f"(x[0]), "+f"(x[1])
         : "f"(d[0]), "f"(d[1]), "f"(f));
-}
-
-// 16 TMEM columns of this warp's lane quarter.
-__device__ __forceinline__ void tmem_ld16w(uint32_t taddr, float (&v)[16])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
-        "%14, %15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
-          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-        : "r"(taddr)
-        : "memory");
 }
 
 __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
@@ -138,113 +133,113 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(WD_REGS_FEW));
-    if (warp == 0) {
-        // ------------------------------------------------------- producer
-        if (lane == 0) {
+        if (warp == 0) {
+            // ------------------------------------------------------- producer
+            if (lane == 0) {
+                int stage = 0;
+                uint32_t phase = 0, pending = 0, pend_par = 0;
+                bool ok = true;
+                for (int64_t t = first; t < tiles && ok; t += step) {
+                    int row, col;
+                    tile_at(t, MT, NT, row, col);
+                    for (int kb = 0; kb < KB; ++kb) {
+                        if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
+                        uint8_t *dst = base + stage * WD_STAGE;
+                        mbar_expect_tx(&sh.full[stage], WD_STAGE);
+                        tma_load_2d(dst, &tmap_a, &sh.full[stage], kb * QBLOCK, row);
+                        tma_load_2d(dst + WD_HALF, &tmap_w, &sh.full[stage], kb * QBLOCK, col);
+                        pending |= 1u << stage;
+                        pend_par = (pend_par & ~(1u << stage)) | (phase << stage);
+                        if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
+                    }
+                }
+                // no copy may still be landing when the CTA leaves
+                int dummy = 0;
+                for (int st = 0; st < WD_STAGES; ++st)
+                    if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
+            }
+        } else if (warp <= 2) {
+            // --------------------------------------------------- MMA issuers
+            // the whole warp runs the loop, so that the descriptors stay in uniform
+            // registers, and one elected lane issues
+            const int h = warp - 1;
+            const uint32_t base_u = __shfl_sync(0xffffffffu, smem_u32(base), 0);
+            const uint32_t d0 = __shfl_sync(0xffffffffu, tmem + h * 128, 0);
+            const uint32_t lo0 = (uint32_t)smem_desc_sw128(base_u), hi = (uint32_t)(smem_desc_sw128(base_u) >> 32);
+            const uint32_t w0 = __shfl_sync(0xffffffffu, lo0 + (1 + h) * (WD_HALF >> 4), 0);
             int stage = 0;
-            uint32_t phase = 0, pending = 0, pend_par = 0;
+            uint32_t phase = 0, par = 0, tphase = 0;               // par: K block parity, which names the TMEM buffer
+            bool ok = true;
+            for (int64_t t = first; t < tiles && ok; t += step) {
+                for (int kb = 0; kb < KB; ++kb) {
+                    ok = mm_wait(&sh.full[stage], phase, abort) && mm_wait(&sh.tempty[par * 2 + h], tphase ^ 1, abort);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t off = stage * (WD_STAGE >> 4);
+                        tc_mma_fp8_kblock(d0 + par * 256, lo0 + off, w0 + off, hi, WD_IDESC);
+                        tc_commit(&sh.tfull[par * 2 + h]);
+                        tc_commit(&sh.empty[stage]);
+                    }
+                    __syncwarp();
+                    if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
+                    par ^= 1;
+                    if (par == 0) tphase ^= 1;
+                }
+            }
+            if (elect_one()) tc_commit(&sh.drain[h]);
+            __syncwarp();
+            int dummy = 0;
+            mm_wait(&sh.drain[h], 0, &dummy, MM_WAIT_CYCLES / 20);
+            __syncwarp();
+        } else {
+            // -------------------------------------------------- scale products
+            const bool vec4 = aligned_dev(g.sa, 16) && g.ldsa % 4 == 0;
+            int slot = 0;
+            uint32_t phase = 0;
             bool ok = true;
             for (int64_t t = first; t < tiles && ok; t += step) {
                 int row, col;
                 tile_at(t, MT, NT, row, col);
-                for (int kb = 0; kb < KB; ++kb) {
-                    if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
-                    uint8_t *dst = base + stage * WD_STAGE;
-                    mbar_expect_tx(&sh.full[stage], WD_STAGE);
-                    tma_load_2d(dst, &tmap_a, &sh.full[stage], kb * QBLOCK, row);
-                    tma_load_2d(dst + WD_HALF, &tmap_w, &sh.full[stage], kb * QBLOCK, col);
-                    pending |= 1u << stage;
-                    pend_par = (pend_par & ~(1u << stage)) | (phase << stage);
-                    if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
-                }
-            }
-            // no copy may still be landing when the CTA leaves
-            int dummy = 0;
-            for (int st = 0; st < WD_STAGES; ++st)
-                if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
-        }
-    } else if (warp <= 2) {
-        // --------------------------------------------------- MMA issuers
-        // the whole warp runs the loop, so that the descriptors stay in uniform
-        // registers, and one elected lane issues
-        const int h = warp - 1;
-        const uint32_t base_u = __shfl_sync(0xffffffffu, smem_u32(base), 0);
-        const uint32_t d0 = __shfl_sync(0xffffffffu, tmem + h * 128, 0);
-        const uint32_t lo0 = (uint32_t)smem_desc_sw128(base_u), hi = (uint32_t)(smem_desc_sw128(base_u) >> 32);
-        const uint32_t w0 = __shfl_sync(0xffffffffu, lo0 + (1 + h) * (WD_HALF >> 4), 0);
-        int stage = 0;
-        uint32_t phase = 0, par = 0, tphase = 0;               // par: K block parity, which names the TMEM buffer
-        bool ok = true;
-        for (int64_t t = first; t < tiles && ok; t += step) {
-            for (int kb = 0; kb < KB; ++kb) {
-                ok = mm_wait(&sh.full[stage], phase, abort) && mm_wait(&sh.tempty[par * 2 + h], tphase ^ 1, abort);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t off = stage * (WD_STAGE >> 4);
-                    tc_mma_fp8_kblock(d0 + par * 256, lo0 + off, w0 + off, hi, WD_IDESC);
-                    tc_commit(&sh.tfull[par * 2 + h]);
-                    tc_commit(&sh.empty[stage]);
-                }
-                __syncwarp();
-                if (++stage == WD_STAGES) { stage = 0; phase ^= 1; }
-                par ^= 1;
-                if (par == 0) tphase ^= 1;
-            }
-        }
-        if (elect_one()) tc_commit(&sh.drain[h]);
-        __syncwarp();
-        int dummy = 0;
-        mm_wait(&sh.drain[h], 0, &dummy, MM_WAIT_CYCLES / 20);
-        __syncwarp();
-    } else {
-        // -------------------------------------------------- scale products
-        const bool vec4 = aligned_dev(g.sa, 16) && g.ldsa % 4 == 0;
-        int slot = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int64_t t = first; t < tiles && ok; t += step) {
-            int row, col;
-            tile_at(t, MT, NT, row, col);
-            const int wb = col / QBLOCK, wl = (g.N - 1) / QBLOCK;
-            const float *w0 = g.sw + (int64_t)min(wb, wl) * g.ldsw, *w1 = g.sw + (int64_t)min(wb + 1, wl) * g.ldsw;
-            const float *s[4];                                  // rows lane, lane + 32, ...
+                const int wb = col / QBLOCK, wl = (g.N - 1) / QBLOCK;
+                const float *w0 = g.sw + (int64_t)min(wb, wl) * g.ldsw, *w1 = g.sw + (int64_t)min(wb + 1, wl) * g.ldsw;
+                const float *s[4];                                  // rows lane, lane + 32, ...
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[r] = g.sa + (int64_t)min(row + r * 32 + lane, g.M - 1) * g.ldsa;
-            for (int kb = 0; kb < KB; kb += WD_GROUP) {
-                float a[4][WD_GROUP], b[2][WD_GROUP];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (vec4 && kb + WD_GROUP <= KB) {
-                        const float4 x = *reinterpret_cast<const float4 *>(s[r] + kb);
-                        a[r][0] = x.x; a[r][1] = x.y; a[r][2] = x.z; a[r][3] = x.w;
-                    } else
-#pragma unroll
-                        for (int i = 0; i < WD_GROUP; ++i) a[r][i] = kb + i < KB ? s[r][kb + i] : 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < WD_GROUP; ++i) {
-                    b[0][i] = kb + i < KB ? w0[kb + i] : 0.0f;
-                    b[1][i] = kb + i < KB ? w1[kb + i] : 0.0f;
-                }
-                ok = __all_sync(0xffffffffu, mm_wait(&sh.sempty[slot], phase ^ 1, abort));
-                if (!ok) break;
-                float *f = scales + slot * (WD_SCALES / 4) + lane;
-#pragma unroll
-                for (int i = 0; i < WD_GROUP; ++i)
+                for (int r = 0; r < 4; ++r) s[r] = g.sa + (int64_t)min(row + r * 32 + lane, g.M - 1) * g.ldsa;
+                for (int kb = 0; kb < KB; kb += WD_GROUP) {
+                    float a[4][WD_GROUP], b[2][WD_GROUP];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        f[(2 * i) * 128 + r * 32] = a[r][i] * b[0][i];
-                        f[(2 * i + 1) * 128 + r * 32] = a[r][i] * b[1][i];
+                        if (vec4 && kb + WD_GROUP <= KB) {
+                            const float4 x = *reinterpret_cast<const float4 *>(s[r] + kb);
+                            a[r][0] = x.x; a[r][1] = x.y; a[r][2] = x.z; a[r][3] = x.w;
+                        } else
+#pragma unroll
+                            for (int i = 0; i < WD_GROUP; ++i) a[r][i] = kb + i < KB ? s[r][kb + i] : 0.0f;
                     }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.sfull[slot]);
-                slot ^= 1;
-                if (slot == 0) phase ^= 1;
+#pragma unroll
+                    for (int i = 0; i < WD_GROUP; ++i) {
+                        b[0][i] = kb + i < KB ? w0[kb + i] : 0.0f;
+                        b[1][i] = kb + i < KB ? w1[kb + i] : 0.0f;
+                    }
+                    ok = __all_sync(0xffffffffu, mm_wait(&sh.sempty[slot], phase ^ 1, abort));
+                    if (!ok) break;
+                    float *f = scales + slot * (WD_SCALES / 4) + lane;
+#pragma unroll
+                    for (int i = 0; i < WD_GROUP; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            f[(2 * i) * 128 + r * 32] = a[r][i] * b[0][i];
+                            f[(2 * i + 1) * 128 + r * 32] = a[r][i] * b[1][i];
+                        }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.sfull[slot]);
+                    slot ^= 1;
+                    if (slot == 0) phase ^= 1;
+                }
             }
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WD_REGS_MANY));
         // ------------------------------------------------------ epilogue
@@ -271,7 +266,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
 #pragma unroll
                 for (int c = 0; c < WD_COLS; c += 16) {
                     float d[16];
-                    tmem_ld16w(taddr + par * 256 + c, d);
+                    tmem_ld16(taddr + par * 256 + c, d);
                     if (c + 16 == WD_COLS) {
                         tc_fence_before();
                         __syncwarp();

@@ -20,7 +20,7 @@ using namespace xp;
 
 namespace {
 
-constexpr int XPRESS_VERSION = 2;
+constexpr int XPRESS_VERSION = 3;
 constexpr int CACHE_SLOTS = 8;
 
 PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder()
