@@ -274,6 +274,22 @@ def test_matmul_shapes(X, M, N, K):
     _mm(X, M, N, K, BF16)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M, N, K", [(600, 3330, 1000), (1025, 3001, 1544), (640, 4096, 2048), (1000, 12001, 100),
+                                     (130, 60000, 648), (4097, 4100, 16)])
+def test_matmul_many_rows_ragged(X, M, N, K, dtype):
+    """Shapes that the kernel for many rows takes, none a multiple of its tile."""
+    _mm(X, M, N, K, dtype, pad=8, off=16, out_pad=5)
+    _mm(X, M, N, K, dtype)
+
+
+@pytest.mark.parametrize("M, N, K", [(1, 100, 8192), (9, 1000, 8192), (16, 130, 16384), (30, 260, 8192), (32, 100, 4096),
+                                     (5, 4096, 1024), (17, 4100, 4104), (24, 4096, 4096)])
+def test_matmul_split_k(X, M, N, K):
+    """K split over clusters of 2, 4 and 8, rows of a that fill no share."""
+    _mm(X, M, N, K, F32, out_pad=1)
+
+
 def test_matmul_reproducible(X):
     for M, N, K in ((5, 512, 4096), (64, 4096, 2048), (300, 1000, 1000)):
         assert torch.equal(_mm(X, M, N, K, F32), _mm(X, M, N, K, F32))
@@ -283,12 +299,12 @@ def test_matmul_empty_and_nan_rows(X):
     q = lambda r, k: X.alloc_e4m3(r, k)  # noqa: E731
     assert X.matmul_fp8(q(0, 64), torch.empty((0, 1), device="cuda"), q(5, 64), torch.empty((1, 1), device="cuda"),
                         torch.empty((0, 5), device="cuda")) == X.XPRESS_OK
-    for M in (3, 200, 300):
-        a, w = _operand(M, 256, 1), _operand(260, 256, 2)
+    for M, N in ((3, 260), (200, 260), (300, 260), (700, 5000)):
+        a, w = _operand(M, 256, 1), _operand(N, 256, 2)
         a[1, 130] = float("nan")
         w[258, 3] = float("nan")
-        out = torch.empty((M, 260), device="cuda")
-        X.matmul_fp8(a, torch.ones((M, 2), device="cuda"), w, torch.ones((3, 2), device="cuda"), out)
+        out = torch.empty((M, N), device="cuda")
+        X.matmul_fp8(a, torch.ones((M, 2), device="cuda"), w, torch.ones((-(-N // 128), 2), device="cuda"), out)
         nan = torch.isnan(out)
         assert nan[1].all() and nan[:, 258].all()
         nan[1] = False
@@ -297,12 +313,12 @@ def test_matmul_empty_and_nan_rows(X):
 
 
 def test_matmul_infinite_scale(X):
-    for M in (2, 150):
-        a, w = _operand(M, 256, 1), _operand(130, 256, 2)
-        sa, sw = torch.ones((M, 2), device="cuda"), torch.ones((2, 2), device="cuda")
+    for M, N in ((2, 130), (150, 130), (700, 5000)):
+        a, w = _operand(M, 256, 1), _operand(N, 256, 2)
+        sa, sw = torch.ones((M, 2), device="cuda"), torch.ones((-(-N // 128), 2), device="cuda")
         sa[0, 1] = float("inf")
-        sw[1, 0] = float("nan")
-        out = torch.empty((M, 130), device="cuda")
+        sw[1:, 0] = float("nan")
+        out = torch.empty((M, N), device="cuda")
         X.matmul_fp8(a, sa, w, sw, out)
         assert not torch.isfinite(out[0]).any() and torch.isnan(out[:, 128:]).all() and torch.isfinite(out[1:, :128]).all()
 

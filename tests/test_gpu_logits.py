@@ -121,7 +121,7 @@ def _check(c, logits, out, argmax, mask_value=float("-inf")):
         bound = 6 * 2.0 ** -24 * mag + 1e-37
         if logits.dtype is BF16:                                    # half the spacing of the stored value
             bound = bound + 2.0 ** (np.floor(np.log2(np.where(fin, np.abs(o64), 0.0) + bound)) - 8)
-        assert (np.abs(g - o64)[fin] <= bound[fin]).all()
+        assert (np.abs(g[fin] - o64[fin]) <= bound[fin]).all()
     if argmax is not None:
         stored = (_bf16_bits(o32).float().numpy() if logits.dtype is BF16 else o32).copy()
         use = ok & ~np.isnan(stored)
@@ -146,7 +146,8 @@ SHAPES = [  # b, R, V, history lengths, bias entries
     (1, 1, 1, [1], 1), (1, 1, 31, [0], 0), (1, 1, 32, [5], 3), (2, 1, 33, [7, 0], 40), (1, 4, 1000, [100], 10),
     (3, 2, 2047, [3, 1025, 1], 5), (2, 3, 2048, [4096, 33], 0), (2, 17, 2049, [0, 9000], 300),
     (5, 5, 4099, [50, 51, 52, 53, 54], 1), (1, 33, 8192, [30000], 100), (2, 1, 151936, [700, 5], 20),
-    (40, 3, 20000, list(range(0, 400, 10)), 7)]
+    (40, 3, 20000, list(range(0, 400, 10)), 7), (1, 1, 9000, [20000], 5), (2, 3, 5001, [9000, 9001], 0),
+    (1, 18, 30000, [50], 3), (70, 1, 60000, [3] * 70, 1)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
