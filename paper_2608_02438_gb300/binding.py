@@ -314,22 +314,16 @@ def _load_ext():
     return _ext
 
 
-def _call(name, stream, *args):
-    """One call of the extension, on `stream` if given (memory used there is
-    kept from torch's allocator until that stream is done with it)."""
-    f = getattr(_ext or _load_ext(), name)
-    if stream is None:
-        code = f(*args)
-    else:
-        import torch
-        with torch.cuda.stream(stream):
-            code = f(*args)
-            for t in args:
-                if isinstance(t, torch.Tensor):
-                    t.record_stream(stream)
-    if code:
-        _check("xpress_" + name, code)
-    return XPRESS_OK
+def _on_stream(stream, call, args) -> int:
+    """One call of the extension on `stream`; memory used there is kept from
+    torch's allocator until that stream is done with it."""
+    import torch
+    with torch.cuda.stream(stream):
+        code = call(*args)
+        for t in args:
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+    return code
 
 
 def alloc_e4m3(rows: int, cols: int, device="cuda"):
@@ -345,13 +339,18 @@ def rmsnorm(x, weight, eps: float = 1e-6, residual=None, sum_out=None, y_out=Non
     x [rows, H], weight [H]; see xpress_rmsnorm): writes those of sum_out, y_out
     (like x), q_out (e4m3 [rows, H], with scale_out fp32 [rows, ceil(H / 128)])
     that are given.  Asynchronous; returns XPRESS_OK."""
-    return _call("rmsnorm", stream, x, weight, eps, residual, sum_out, y_out, q_out, scale_out)
+    call = (_ext or _load_ext()).rmsnorm
+    args = (x, weight, eps, residual, sum_out, y_out, q_out, scale_out)
+    code = call(*args) if stream is None else _on_stream(stream, call, args)
+    if code:
+        _check("xpress_rmsnorm", code)
+    return XPRESS_OK
 
 
 def quantize_weight(W, q_out=None, scale_out=None, stream=None):
     """e4m3 weights with a scale per 128 x 128 block from W [rows, cols] (bf16 or
     fp32): returns (q, scale), allocated where not given."""
-    if W.dim() == 2 and (q_out is None or scale_out is None):
+    if (q_out is None or scale_out is None) and W.dim() == 2:
         import contextlib
 
         import torch
@@ -361,7 +360,10 @@ def quantize_weight(W, q_out=None, scale_out=None, stream=None):
                 q_out = alloc_e4m3(rows, cols, W.device)
             if scale_out is None:
                 scale_out = torch.empty(((rows + 127) // 128, (cols + 127) // 128), dtype=torch.float32, device=W.device)
-    _call("quantize_weight", stream, W, q_out, scale_out)
+    call, args = (_ext or _load_ext()).quantize_weight, (W, q_out, scale_out)
+    code = call(*args) if stream is None else _on_stream(stream, call, args)
+    if code:
+        _check("xpress_quantize_weight", code)
     return q_out, scale_out
 
 
@@ -371,7 +373,11 @@ def matmul_fp8(a, a_scale, w, w_scale, out, stream=None) -> int:
     ceil(K / 128)] (see xpress_matmul_fp8).  Asynchronous; returns XPRESS_OK;
     matmul_fp8_status() reads the device status of the calls so far.  The first
     call on a device makes the status word: not inside a graph capture."""
-    return _call("matmul_fp8", stream, a, a_scale, w, w_scale, out)
+    call, args = (_ext or _load_ext()).matmul_fp8, (a, a_scale, w, w_scale, out)
+    code = call(*args) if stream is None else _on_stream(stream, call, args)
+    if code:
+        _check("xpress_matmul_fp8", code)
+    return XPRESS_OK
 
 
 def matmul_fp8_status(stream=None) -> int:
@@ -393,8 +399,13 @@ def process_logits(logits, out=None, argmax_out=None, rows: int = 1, repetition=
     [n_seq + 1]; prompt_len int32 [n_seq]; draft int32 [n_seq, >= rows - 1];
     mask int32 [mask rows, ceil(V / 32)]; mask_row int32 [n_seq * rows].
     Asynchronous; returns XPRESS_OK."""
-    return _call("process_logits", stream, logits, out, argmax_out, rows, repetition, frequency, presence, history,
-                 history_offsets, prompt_len, draft, bias_ids, bias_values, bias_offsets, mask, mask_row, mask_value)
+    call = (_ext or _load_ext()).process_logits
+    args = (logits, out, argmax_out, rows, repetition, frequency, presence, history, history_offsets, prompt_len, draft,
+            bias_ids, bias_values, bias_offsets, mask, mask_row, mask_value)
+    code = call(*args) if stream is None else _on_stream(stream, call, args)
+    if code:
+        _check("xpress_process_logits", code)
+    return XPRESS_OK
 
 
 # ------------------------------------------------------------ torch helper

