@@ -183,8 +183,8 @@ __device__ __forceinline__ void count_token(uint32_t *cnt, const Share &sh, int 
 }
 
 // grid (shares of 2048 U ids, sequences, parts of the rows); shared memory with patch: counts [C],
-// with a bias as many floats, the list [C] (16 bits).  MULTI: several rows.
-// NT: LT threads, or more, of which those past LT count and patch only.
+// with a bias as many floats, the list [C] (16 bits).
+// MULTI: several rows of a CTA.  NT: LT threads, or more, of which those past LT count and patch only.
 template <typename T, bool VEC, int U, bool MULTI, int NT>
 __global__ void __launch_bounds__(NT, NT > LT ? 1 : MULTI && U == 4 ? 2 : 4) k_logits(const __grid_constant__ LogitsArgs a)
 {
@@ -498,18 +498,25 @@ int logits_slots(int n_seq, int V, int sms)
     return U;
 }
 
-// Few CTAs: a sequence's rows are split over several (each counts for itself)
-// until there are two per SM.  Where not even every SM gets one and histories
-// are long, a CTA takes 512 threads for the counts and the patch (6 sequences of
-// 30000 tokens, V = 32003, 5 rows: 32 -> 21 us; a short history gains nothing).
+// Few CTAs: a sequence's rows are split over as many as an SM takes, four (17
+// rows of 10000 bf16, 3 requests: 11.7 us with parts of 4 rows, 8.8 with one row
+// each).  Each part counts the history for itself, so that from 4096 tokens on
+// there are two per SM (16 rows of 32000, 4 requests of 8000 tokens: 18 us,
+// 22 with four).  Where not even every SM gets one and histories are longer yet,
+// a CTA takes 512 threads for the counts and the patch (6 sequences of 30000
+// tokens, V = 32003, 5 rows: 32 -> 21 us; a short history gains nothing), and
+// there is one per SM (17 rows of 5000, one request of 20000 tokens: 11 us, 43
+// with all rows in one CTA).
 LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, int sms)
 {
     LogitsPlan p{logits_slots(n_seq, a.V, sms), LT, a.rows};
     const int64_t ctas = (int64_t)n_seq * ((a.V + LT * 8 - 1) / (LT * 8));
-    if (p.U == 1 && a.patch && ctas <= sms && a.n_hist >= 8192 * (int64_t)n_seq) p.threads = LT_FEW;
-    else if (p.U == 1)
-        while (p.rows_each > 4 && ctas * ((a.rows + p.rows_each - 1) / p.rows_each) < 2 * sms)
-            p.rows_each = (p.rows_each + 1) / 2;
+    if (p.U != 1) return p;
+    const int64_t each = a.patch ? a.n_hist / n_seq : 0;
+    if (ctas <= sms && each >= 8192) p.threads = LT_FEW;
+    const int64_t room = (int64_t)sms * (p.threads == LT_FEW ? 1 : each >= 4096 ? 2 : 4);
+    const int64_t parts = room > ctas ? room / ctas : 1;
+    p.rows_each = (int)((a.rows + parts - 1) / parts);
     return p;
 }
 
@@ -538,7 +545,7 @@ cudaError_t launch_logits_r(const LogitsArgs &a, int n_seq, const LogitsPlan &p,
 template <typename T, bool VEC>
 cudaError_t launch_logits(const LogitsArgs &a, int n_seq, const LogitsPlan &p, cudaStream_t st)
 {
-    return a.rows > 1 ? launch_logits_r<T, VEC, true>(a, n_seq, p, st) : launch_logits_r<T, VEC, false>(a, n_seq, p, st);
+    return a.rows_each > 1 ? launch_logits_r<T, VEC, true>(a, n_seq, p, st) : launch_logits_r<T, VEC, false>(a, n_seq, p, st);
 }
 
 }  // namespace

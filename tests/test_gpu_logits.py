@@ -242,6 +242,28 @@ def test_rules_infinities_nans_and_empty_rows(X, dtype, mask_value):
     assert (out[1] == stored).all() and (out[4] == stored).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("b, R, V, hist", [(40, 17, 4200, 300), (90, 17, 4000, 5), (3, 17, 30000, 10000), (4, 16, 9001, 6000),
+                                           (65, 9, 4096, 700), (30, 5, 44000, 20)])
+def test_rules_groups_of_rows(X, b, R, V, hist, dtype):
+    """Batches that leave a CTA several rows, whole groups and parts of one, with
+    infinities, NaNs, rows that allow nothing, and in place."""
+    c = _case(b, R, V, [hist + q for q in range(b)], 25, seed=V)
+    x = _logits(c, dtype, V, pad=8 - V % 8)
+    for j in range(R):                                               # each place of a group
+        x[(b - 1) * R + j, 3 * j], x[j, 7 * j], x[R + j, 5 * j + 1] = float("inf"), float("-inf"), float("nan")
+    x[2 * R] = float("nan")
+    x[2 * R + 1] = float("-inf")
+    c["mask_row"][2 * R:2 * R + 2] = -1
+    c["mask_row"][1::7] = 1                                          # a grammar state without a token
+    out, am = torch.empty_like(x), torch.full((b * R,), -9, dtype=torch.int32, device="cuda")
+    _call(X, c, x, out, am)
+    _check(c, x, out, am)
+    y, am2 = x.clone(), torch.empty_like(am)
+    _call(X, c, y, y, am2)
+    assert torch.equal(am2, am) and ((y == out) | (y.isnan() & out.isnan())).all()
+
+
 def test_rules_ties_go_to_the_lowest_id(X):
     for V, at in ((151936, (5, 70000, 151935)), (2500, (2047, 2048, 2499))):
         x = torch.zeros((3, V), dtype=BF16, device="cuda")
