@@ -59,21 +59,6 @@ struct MmBars {
     int abort;
 };
 
-// Floats to a shared::cluster address (aligned to their size), counted in bytes
-// by the mbarrier `bar` of the same CTA once they are there.
-__device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, const float *v)
-{
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%2, %3}, [%1];" ::"r"(addr), "r"(bar),
-                 "f"(v[0]), "f"(v[1])
-                 : "memory");
-}
-__device__ __forceinline__ void st_async4(uint32_t addr, uint32_t bar, const float *v)
-{
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
-                 "r"(bar), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3])
-                 : "memory");
-}
-
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z)
 {
     asm volatile(
@@ -316,13 +301,20 @@ __global__ void __launch_bounds__(MM_THREADS, 2)
 //              joining a split costs about 0.6 us and 0.075 for each row of a
 //              (16 x 4096 x 512 with S = 2: 5.3 us, 4.1 without); with two CTAs
 //              on an SM a stage takes 1.43 times as long and an item 1.5 stages
-//              more; the weights stream at 6.3 TB/s
-//   many rows  0.5 us for a K block of a 128 x 256 tile, 1 to start, 2 between
-//              tiles (16 x 4096 x 4096: 18.2, 64 x 151936 x 256: 15.9); the
-//              weights stream at 5.9 TB/s
+//              more, and so it has where a CTA takes several; the weights stream
+//              at 6.3 TB/s
+//   many rows  0.41 us for a K block of a 128 x 256 tile, 0.6 to start and 2 for
+//              the epilogue of 128 rows (512 x 1024 x 1024: 9.2 us, 300 x 4096 x
+//              4096: 19), with K split over 2, 4 and 8 CTAs 1.7 and 1.9, 2.7, 3.1
+//              (300 x 600 x 8192: 33 us, 18.4, 13.8, 11.4), 1.5 and 0.7 more where
+//              out's rows start anywhere, two fifths of the weights' stream at
+//              5.9 TB/s (512 x 4096 x 4096 with S = 2: 14.9).  Where a CTA takes
+//              several tiles, 0.5 us for a K block, 1 to start, 2 between tiles,
+//              or the stream (64 x 151936 x 256: 15.9)
 // At 24 x 151936 x 4096 the choice is NT = 32 (96 us; 16: 102, many rows: 118),
 // at 64 x 151936 x 4096 many rows (103; 126 and 177), at 300 x 2048 x 1024
-// NT = 16 (6.1; 32: 10.3, many rows: 9.1).
+// NT = 16 (6.1; 32: 10.3, many rows: 9.1), at 512 x 4096 x 4096 many rows with
+// S = 2 (14.9; without a split 19.7, few rows 31.6).
 struct MmPlan {
     int NT, S;
     float us;
@@ -367,7 +359,7 @@ MmPlan plan_few(int M, int N, int KB, int NT, int sms)
         const float stream = (float)N * KB * QBLOCK / 6.3e6f, work = rounds * (KP + 1.5f) * stage * 1.43f;
         return {NT, 1, stream > work ? stream : work};
     }
-    MmPlan best{NT, 1, (float)((items + sms - 1) / sms) * KP * stage};
+    MmPlan best{NT, 1, items <= sms ? KP * stage : (float)((items + sms - 1) / sms) * (KP + 1.5f) * stage};
     for (int S = 2; S <= 8 && S <= KP && items <= resident_clusters(S); S *= 2) {
         const float us = (KP + S - 1) / S * stage + join;
         if (us < best.us) best = {NT, S, us};
@@ -375,17 +367,28 @@ MmPlan plan_few(int M, int N, int KB, int NT, int sms)
     return best;
 }
 
-MmPlan plan_mm(int M, int N, int KB, int sms)
+// ragged: out's rows do not all start on 32 bytes.
+MmPlan plan_mm(int M, int N, int KB, bool ragged, int sms)
 {
     MmPlan best = plan_few(M, N, KB, 16, sms);
     if (M > 16) {
         const MmPlan b = plan_few(M, N, KB, 32, sms);
         if (b.us < best.us) best = b;
+        // NT = 0: the kernel for many rows
         const int64_t tiles = (int64_t)((M + 127) / 128) * ((N + 255) / 256);
         const float stream = (float)N * KB * QBLOCK / 5.9e6f;
-        const float work = 1.0f + 0.5f * KB + (0.5f * KB + 2.0f) * ((tiles - 1) / sms);
-        const float us = stream > work ? stream : work;
-        if (us < best.us) best = {0, 1, us};             // NT = 0: the kernel for many rows
+        if (tiles > sms) {
+            const float work = 1.0f + 0.5f * KB + (0.5f * KB + 2.0f) * ((tiles - 1) / sms);
+            const float us = stream > work ? stream : work;
+            if (us < best.us) best = {0, 1, us};
+        }
+        const float full = M < 128 ? (M + 31) / 32 / 4.0f : 1.0f;                   // part of the epilogue that has rows
+        const float epilogue[4] = {2.0f, 1.9f, 2.7f, 3.1f};
+        for (int i = 0, S = 1; S <= 8 && S <= KB && tiles <= (S == 1 ? sms : resident_clusters(S)); ++i, S *= 2) {
+            const float us = (S == 1 ? 0.6f : 1.7f) + epilogue[i] * full + 0.41f * ((KB + S - 1) / S) + 0.4f * stream +
+                             (ragged ? S == 1 ? 1.5f : 0.7f : 0.0f);
+            if (us < best.us) best = {0, S, us};
+        }
     }
     return best;
 }
@@ -464,8 +467,9 @@ extern "C" int xpress_matmul_fp8(const xpress_matmul_args *in, void *ws, size_t 
     g.bf16 = in->out_dtype == XPRESS_BF16;
     g.status = static_cast<int32_t *>(ws);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const MmPlan p = plan_mm(in->M, in->N, KB, sms);
+    const MmPlan p = plan_mm(in->M, in->N, KB, !mm_out_vec(g), sms);
     if (p.NT == 16) return launch_mm<16>(g, p.S, in->a, in->lda, in->w, in->ldw, sms, st);
     if (p.NT == 32) return launch_mm<32>(g, p.S, in->a, in->lda, in->w, in->ldw, sms, st);
+    g.S = p.S;
     return launch_mm_wide(g, in->a, in->lda, in->w, in->ldw, sms, st);
 }

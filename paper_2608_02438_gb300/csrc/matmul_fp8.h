@@ -35,6 +35,21 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank)
     return a;
 }
 
+// Floats to a shared::cluster address (aligned to their size), counted in bytes
+// by the mbarrier `bar` of the same CTA once they are there.
+__device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, const float *v)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%2, %3}, [%1];" ::"r"(addr), "r"(bar),
+                 "f"(v[0]), "f"(v[1])
+                 : "memory");
+}
+__device__ __forceinline__ void st_async4(uint32_t addr, uint32_t bar, const float *v)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
+                 "r"(bar), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3])
+                 : "memory");
+}
+
 // Bounded wait for a phase of `bar`.  It polls (a wait with a sleep hint wakes
 // up later: an earlier form at 2048 x 38912 x 4096 took 739 us against 683) and bounds itself by
 // the SM's cycle counter, read once in 64 polls: the global timer's latency
@@ -107,6 +122,9 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *v)
         : "r"(taddr)
         : "memory");
 }
+
+// out's rows start on 32 bytes
+inline bool mm_out_vec(const MmArgs &g) { return aligned(g.out, 32) && g.ldo * (g.bf16 ? 2 : 4) % 32 == 0; }
 
 // many rows of a (matmul_fp8_wide.cu)
 int launch_mm_wide(const MmArgs &g, const void *a, int64_t lda, const void *w, int64_t ldw, int sms, cudaStream_t st);

@@ -11,6 +11,18 @@
 // instead of two large ones cover the way from a finished MMA over the epilogue
 // back to the MMA that reuses its buffer.
 //
+// Where the tiles are fewer than the SMs, the CTAs of a cluster of S split K.
+// Every thread of the epilogue sends its sums to its counterparts, each of which
+// gets 64 / S columns and adds them in rank order, so that the result does not
+// depend on timing.  The sums land where the operands' stages were, so all
+// CTAs of the cluster meet once before them.  Each CTA starts with the next one
+// in rank: with all of them sending to the same CTA first, joining 4 took 1.5 us
+// longer.  From there a warp stores whole rows of its columns, which is also
+// how a single tile goes out whose rows start anywhere (700 x 3000 x 256: 9.1 ->
+// 7.3 us; rows on 32 bytes leave from the registers, 0.6 us faster than through
+// shared memory).  512 x 4096 x 4096: 19.8 us, 14.9 with S = 2; 300 x 600 x 8192:
+// 33 us, 11.4 with S = 8.
+//
 // Roles (640 threads): warp 0 TMA producer; warps 1 and 2 MMA issuers, one for
 // each half tile (warp 1 also allocates TMEM): waiting, issuing 4 MMAs and
 // committing takes a warp longer than the tensor core takes for them; warp 3
@@ -48,6 +60,9 @@ constexpr int WD_STAGES = 4;
 constexpr uint32_t WD_IDESC = idesc_e4m3(128, 128);
 constexpr int WD_BUFS = 4;                              // TMEM buffers: K block parity, half
 constexpr int WD_TCOLS = 8;                             // columns of a transpose
+// Sums of a CTA's only tile: 4 columns of each of the 512 threads, then the next
+// 4, four banks on.
+constexpr int WD_GROUP4 = WD_EPI * 32 * 4 + 4;
 constexpr size_t WD_TILE = 32 * (WD_TCOLS + 1) * 4;     // a warp's transpose
 constexpr int WD_GROUP = 4;                             // K blocks whose scales are staged together
 constexpr size_t WD_SCALES = WD_GROUP * 2 * 128 * 4;    // [K block][weight block][row]
@@ -59,6 +74,7 @@ struct WideBars {
     uint64_t tfull[WD_BUFS], tempty[WD_BUFS];
     uint64_t sfull[2], sempty[2];
     uint64_t drain[2];
+    uint64_t joined[WD_EPI];
     uint32_t tmem_base;
     int abort;
 };
@@ -88,6 +104,24 @@ __device__ __forceinline__ bool aligned_dev(const void *p, uintptr_t a)
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }
 
+// Eight columns of the warp's 32 rows, v of row `lane`, to rows m0 .. and columns
+// n .. of out through a transpose, so that 8 lanes store consecutive elements.
+__device__ __forceinline__ void store_cols8(const MmArgs &g, int m0, int n, const float *v, float (*tp)[WD_TCOLS + 1])
+{
+    const int lane = threadIdx.x % 32;
+    const int rows = min(32, g.M - m0), cl = lane % WD_TCOLS;
+#pragma unroll
+    for (int j = 0; j < WD_TCOLS; ++j) tp[lane][j] = v[j];
+    __syncwarp();
+    if (n + cl < g.N)
+        for (int r = lane / WD_TCOLS; r < rows; r += 32 / WD_TCOLS) {
+            const int64_t at = (int64_t)(m0 + r) * g.ldo + n + cl;
+            if (g.bf16) static_cast<uint16_t *>(g.out)[at] = f2bf(tp[r][cl]);
+            else static_cast<float *>(g.out)[at] = tp[r][cl];
+        }
+    __syncwarp();
+}
+
 // First row and column of tile t, in the order of bands of WD_BAND row tiles,
 // within a band the row tiles of one column tile after another.
 __device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &row, int &col)
@@ -99,10 +133,13 @@ __device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &row, int
     col = (int)(in / rows) * WD_BN;
 }
 
-// grid: any; WD_THREADS threads, WD_SMEM bytes; vec: out's rows start on 32 bytes.
+// grid: a cluster of S CTAs for each tile, or with S = 0 any number of CTAs that
+// take tile after tile; WD_THREADS threads, WD_SMEM bytes; vec: out's rows start
+// on 32 bytes, pairs: on two elements.
+template <int S>
 __global__ void __launch_bounds__(WD_THREADS, 1)
     k_matmul_fp8_wide(const __grid_constant__ MmArgs g, const __grid_constant__ CUtensorMap tmap_a,
-                      const __grid_constant__ CUtensorMap tmap_w, int vec)
+                      const __grid_constant__ CUtensorMap tmap_w, int vec, int pairs)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -110,13 +147,17 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int KB = (g.K + QBLOCK - 1) / QBLOCK;
     const int MT = (g.M + WD_BM - 1) / WD_BM, NT = (g.N + WD_BN - 1) / WD_BN;
-    const int64_t tiles = (int64_t)MT * NT, first = blockIdx.x, step = gridDim.x;
+    constexpr int CS = S ? S : 1;
+    const int rank = S > 1 ? (int)cluster_rank() : 0;
+    const int kb0 = S > 1 ? KB * rank / CS : 0, kb1 = S > 1 ? KB * (rank + 1) / CS : KB;
+    const int64_t first = blockIdx.x / CS, tiles = S ? first + 1 : (int64_t)MT * NT, step = S ? 1 : gridDim.x;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < WD_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 2); }
         for (int i = 0; i < WD_BUFS; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], WD_EPI / 2); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.sfull[i], 1); mbar_init(&sh.sempty[i], WD_EPI); }
         for (int i = 0; i < 2; ++i) mbar_init(&sh.drain[i], 1);
+        for (int i = 0; i < WD_EPI; ++i) mbar_init(&sh.joined[i], 1);
         sh.abort = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tmap_w);
@@ -142,7 +183,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                 for (int64_t t = first; t < tiles && ok; t += step) {
                     int row, col;
                     tile_at(t, MT, NT, row, col);
-                    for (int kb = 0; kb < KB; ++kb) {
+                    for (int kb = kb0; kb < kb1; ++kb) {
                         if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
                         uint8_t *dst = base + stage * WD_STAGE;
                         mbar_expect_tx(&sh.full[stage], WD_STAGE);
@@ -171,7 +212,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             uint32_t phase = 0, par = 0, tphase = 0;               // par: K block parity, which names the TMEM buffer
             bool ok = true;
             for (int64_t t = first; t < tiles && ok; t += step) {
-                for (int kb = 0; kb < KB; ++kb) {
+                for (int kb = kb0; kb < kb1; ++kb) {
                     ok = mm_wait(&sh.full[stage], phase, abort) && mm_wait(&sh.tempty[par * 2 + h], tphase ^ 1, abort);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
@@ -195,7 +236,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
             __syncwarp();
         } else {
             // -------------------------------------------------- scale products
-            const bool vec4 = aligned_dev(g.sa, 16) && g.ldsa % 4 == 0;
+            const bool vec4 = aligned_dev(g.sa + kb0, 16) && g.ldsa % 4 == 0;
             int slot = 0;
             uint32_t phase = 0;
             bool ok = true;
@@ -207,21 +248,21 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                 const float *s[4];                                  // rows lane, lane + 32, ...
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[r] = g.sa + (int64_t)min(row + r * 32 + lane, g.M - 1) * g.ldsa;
-                for (int kb = 0; kb < KB; kb += WD_GROUP) {
+                for (int kb = kb0; kb < kb1; kb += WD_GROUP) {
                     float a[4][WD_GROUP], b[2][WD_GROUP];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        if (vec4 && kb + WD_GROUP <= KB) {
+                        if (vec4 && kb + WD_GROUP <= kb1) {
                             const float4 x = *reinterpret_cast<const float4 *>(s[r] + kb);
                             a[r][0] = x.x; a[r][1] = x.y; a[r][2] = x.z; a[r][3] = x.w;
                         } else
 #pragma unroll
-                            for (int i = 0; i < WD_GROUP; ++i) a[r][i] = kb + i < KB ? s[r][kb + i] : 0.0f;
+                            for (int i = 0; i < WD_GROUP; ++i) a[r][i] = kb + i < kb1 ? s[r][kb + i] : 0.0f;
                     }
 #pragma unroll
                     for (int i = 0; i < WD_GROUP; ++i) {
-                        b[0][i] = kb + i < KB ? w0[kb + i] : 0.0f;
-                        b[1][i] = kb + i < KB ? w1[kb + i] : 0.0f;
+                        b[0][i] = kb + i < kb1 ? w0[kb + i] : 0.0f;
+                        b[1][i] = kb + i < kb1 ? w1[kb + i] : 0.0f;
                     }
                     ok = __all_sync(0xffffffffu, mm_wait(&sh.sempty[slot], phase ^ 1, abort));
                     if (!ok) break;
@@ -240,6 +281,8 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                 }
             }
         }
+        __syncwarp();
+        if (S > 1) { cluster_arrive(); cluster_wait(); }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(WD_REGS_MANY));
         // ------------------------------------------------------ epilogue
@@ -249,15 +292,17 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
         int slot = 0;
         uint32_t par = 0, tphase = 0, sphase = 0;
         bool ok = true;
-        for (int64_t t = first; t < tiles && ok; t += step) {
+        int m0 = g.M, n0 = g.N;
+        float acc[WD_COLS];
+        for (int64_t t = first; t < tiles; t += step) {
             int row, col;
             tile_at(t, MT, NT, row, col);
-            const int m0 = row + q * 32, n0 = col + part * WD_COLS;
-            float acc[WD_COLS];
+            m0 = row + q * 32;
+            n0 = col + part * WD_COLS;
 #pragma unroll
             for (int j = 0; j < WD_COLS; ++j) acc[j] = 0.0f;
 #pragma unroll 4
-            for (int kb = 0; kb < KB; ++kb) {
+            for (int kb = 0; kb < kb1 - kb0; ++kb) {
                 const int i = kb % WD_GROUP;
                 if (i == 0) ok = mm_wait(&sh.sfull[slot], sphase, abort);
                 ok = __all_sync(0xffffffffu, ok && mm_wait(&sh.tfull[par * 2 + half], tphase, abort));
@@ -278,14 +323,15 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                 }
                 par ^= 1;
                 if (par == 0) tphase ^= 1;
-                if (i == WD_GROUP - 1 || kb == KB - 1) {
+                if (i == WD_GROUP - 1 || kb == kb1 - kb0 - 1) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.sempty[slot]);
                     slot ^= 1;
                     if (slot == 0) sphase ^= 1;
                 }
             }
-            if (!ok || m0 >= g.M || n0 >= g.N) continue;
+            if (!ok || S) break;
+            if (m0 >= g.M || n0 >= g.N) continue;
             if (vec && n0 + WD_COLS <= g.N) {
                 if (m0 + lane < g.M) {
                     const int64_t at = (int64_t)(m0 + lane) * g.ldo + n0;
@@ -308,22 +354,60 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                     }
                 }
             } else {
-                // rows of out that start anywhere, or a partial tile: transpose 8
-                // columns at a time, so that 8 lanes store consecutive elements
-                const int rows = min(32, g.M - m0), cl = lane % WD_TCOLS;
 #pragma unroll
-                for (int c = 0; c < WD_COLS; c += WD_TCOLS) {
-                    const int n = n0 + c + cl;
+                for (int c = 0; c < WD_COLS; c += WD_TCOLS) store_cols8(g, m0, n0 + c, acc + c, tp);
+            }
+        }
+        // the only tile, when the MMAs have read their operands for good (of all CTAs
+        // of the cluster); a warp outside out neither sends nor waits
+        if (S > 1) { __syncwarp(); cluster_arrive(); cluster_wait(); }
+        else if (S == 1) asm volatile("bar.sync 1, %0;" ::"n"(WD_EPI * 32) : "memory");
+        if (S && m0 < g.M && n0 < g.N && (S > 1 || ok)) {
+            constexpr int share = WD_COLS / CS, LPR = share / 2;     // columns that stay here, lanes of a row
+            const int et = threadIdx.x - 128;
+            float *sums = reinterpret_cast<float *>(base);
+            uint64_t *joined = &sh.joined[warp - 4];
+            if (S > 1 && lane == 0) mbar_expect_tx(joined, (WD_COLS - share) * 32 * 4);
 #pragma unroll
-                    for (int j = 0; j < WD_TCOLS; ++j) tp[lane][j] = acc[c + j];
-                    __syncwarp();
-                    if (n < g.N)
-                        for (int r = lane / WD_TCOLS; r < rows; r += 32 / WD_TCOLS) {
-                            const int64_t at = (int64_t)(m0 + r) * g.ldo + n;
-                            if (g.bf16) static_cast<uint16_t *>(g.out)[at] = f2bf(tp[r][cl]);
-                            else static_cast<float *>(g.out)[at] = tp[r][cl];
+            for (int r = 0; r < CS; ++r)
+                if (r == rank)
+#pragma unroll
+                    for (int k = 1; k <= CS; ++k) {
+                        const int d = (r + k) % CS;
+                        const uint32_t there = cluster_addr(sums, d), bar = cluster_addr(joined, d);
+#pragma unroll
+                        for (int c = 0; c < share; c += 4) {
+                            const int at = (r * share + c) / 4 * WD_GROUP4 + et * 4;
+                            const float *v = acc + d * share + c;
+                            if (k < CS) st_async4(there + at * 4, bar, v);
+                            else *reinterpret_cast<float4 *>(sums + at) = make_float4(v[0], v[1], v[2], v[3]);
                         }
-                    __syncwarp();
+                    }
+            __syncwarp();
+            // (longer than any sender's own waits, which end in its stores)
+            if (S > 1) ok = __all_sync(0xffffffffu, mm_wait(joined, 0, abort, 3 * MM_WAIT_CYCLES)) && ok;
+            const int c = lane % LPR * 2, n = n0 + rank * share + c;
+            const float *from = sums + c / 4 * WD_GROUP4 + (et - lane) * 4 + c % 4;
+#pragma unroll 2
+            for (int i = lane / LPR; i < 32 && ok; i += 32 / LPR) {
+                float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+                for (int k = 0; k < S; ++k) {
+                    const float2 x = *reinterpret_cast<const float2 *>(from + k * (share / 4) * WD_GROUP4 + i * 4);
+                    v.x += x.x;
+                    v.y += x.y;
+                }
+                const int64_t at = (int64_t)(m0 + i) * g.ldo + n;
+                if (m0 + i >= g.M || n >= g.N) continue;
+                if (pairs && n + 1 < g.N) {
+                    if (g.bf16) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(g.out) + at) = pack_bf16(v.x, v.y);
+                    else *reinterpret_cast<float2 *>(static_cast<float *>(g.out) + at) = v;
+                } else if (g.bf16) {
+                    static_cast<uint16_t *>(g.out)[at] = f2bf(v.x);
+                    if (n + 1 < g.N) static_cast<uint16_t *>(g.out)[at + 1] = f2bf(v.y);
+                } else {
+                    static_cast<float *>(g.out)[at] = v.x;
+                    if (n + 1 < g.N) static_cast<float *>(g.out)[at + 1] = v.y;
                 }
             }
         }
@@ -337,26 +421,35 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
     if (threadIdx.x == 0 && sh.abort) set_status(g.status, ST_TIMEOUT);
 }
 
-}  // namespace
-
-int launch_mm_wide(const MmArgs &g, const void *a, int64_t lda, const void *w, int64_t ldw, int sms, cudaStream_t st)
+template <int S>
+int launch_wide(const MmArgs &g, const CUtensorMap &ta, const CUtensorMap &tw, int64_t grid, cudaStream_t st)
 {
     static std::once_flag once;
     static cudaError_t attr;
     std::call_once(once, [] {
-        attr = cudaFuncSetAttribute(k_matmul_fp8_wide, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WD_SMEM);
+        attr = cudaFuncSetAttribute(k_matmul_fp8_wide<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WD_SMEM);
     });
     if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
+    const int vec = mm_out_vec(g), pairs = aligned(g.out, g.bf16 ? 4 : 8) && g.ldo % 2 == 0;
+    XH_CUDA(launch_head(k_matmul_fp8_wide<S>, dim3((unsigned)grid), WD_THREADS, WD_SMEM, st, S ? S : 1u, g, ta, tw, vec,
+                        pairs));
+    return XPRESS_OK;
+}
+
+}  // namespace
+
+int launch_mm_wide(const MmArgs &g, const void *a, int64_t lda, const void *w, int64_t ldw, int sms, cudaStream_t st)
+{
     CUtensorMap ta{}, tw{};
     if (!tmap_bytes(&ta, a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)lda, QBLOCK, WD_BM) ||
         !tmap_bytes(&tw, w, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)ldw, QBLOCK, WD_BN))
         return XPRESS_ERR_CUDA;
     const int64_t tiles = (int64_t)((g.M + WD_BM - 1) / WD_BM) * ((g.N + WD_BN - 1) / WD_BN);
-    const int es = g.bf16 ? 2 : 4;
-    const int vec = aligned(g.out, 32) && g.ldo * es % 32 == 0;
-    XH_CUDA(launch_head(k_matmul_fp8_wide, dim3((unsigned)(tiles < sms ? tiles : sms)), WD_THREADS, WD_SMEM, st, 1, g, ta,
-                        tw, vec));
-    return XPRESS_OK;
+    return g.S == 1 && tiles <= sms && !mm_out_vec(g) ? launch_wide<1>(g, ta, tw, tiles, st)
+         : g.S == 8     ? launch_wide<8>(g, ta, tw, tiles * 8, st)
+         : g.S == 4     ? launch_wide<4>(g, ta, tw, tiles * 4, st)
+         : g.S == 2     ? launch_wide<2>(g, ta, tw, tiles * 2, st)
+                        : launch_wide<0>(g, ta, tw, tiles < sms ? tiles : sms, st);
 }
 
 }  // namespace xp

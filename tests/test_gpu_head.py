@@ -290,6 +290,17 @@ def test_matmul_split_k(X, M, N, K):
     _mm(X, M, N, K, F32, out_pad=1)
 
 
+@pytest.mark.parametrize("M, N, K", [(512, 4096, 4096), (300, 600, 8192), (566, 1550, 2048), (200, 4096, 4096),
+                                     (129, 257, 16384), (1000, 2000, 8192), (640, 3001, 1544), (513, 100, 8200),
+                                     (400, 5000, 3000)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_matmul_many_rows_split_k(X, M, N, K, dtype):
+    """K split over clusters of the kernel for many rows, whole and partial tiles."""
+    _mm(X, M, N, K, dtype, pad=8, off=16, out_pad=5)
+    out = _mm(X, M, N, K, dtype)
+    assert torch.equal(out, _mm(X, M, N, K, dtype))
+
+
 def test_matmul_reproducible(X):
     for M, N, K in ((5, 512, 4096), (64, 4096, 2048), (300, 1000, 1000)):
         assert torch.equal(_mm(X, M, N, K, F32), _mm(X, M, N, K, F32))
