@@ -92,8 +92,14 @@ __device__ __forceinline__ void fma2(float *x, const float *d, float f)
         : "f"(d[0]), "f"(d[1]), "f"(f));
 }
 
-__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
+// 32 bytes to an address that is a multiple of 32 (wide) or of 16.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8], bool wide)
 {
+    if (!wide) {
+        static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        return;
+    }
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
                  "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                  : "memory");
@@ -135,7 +141,7 @@ __device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &row, int
 
 // grid: a cluster of S CTAs for each tile, or with S = 0 any number of CTAs that
 // take tile after tile; WD_THREADS threads, WD_SMEM bytes; vec: out's rows start
-// on 32 bytes, pairs: on two elements.
+// on this many bytes (32, 16 or 0: any), pairs: on two elements.
 template <int S>
 __global__ void __launch_bounds__(WD_THREADS, 1)
     k_matmul_fp8_wide(const __grid_constant__ MmArgs g, const __grid_constant__ CUtensorMap tmap_a,
@@ -341,7 +347,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                             uint32_t w[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) w[j] = pack_bf16(acc[c + 2 * j], acc[c + 2 * j + 1]);
-                            store32(static_cast<uint16_t *>(g.out) + at + c, w);
+                            store32(static_cast<uint16_t *>(g.out) + at + c, w, vec == 32);
                         }
                     } else {
 #pragma unroll
@@ -349,7 +355,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                             uint32_t w[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(acc[c + j]);
-                            store32(static_cast<float *>(g.out) + at + c, w);
+                            store32(static_cast<float *>(g.out) + at + c, w, vec == 32);
                         }
                     }
                 }
@@ -430,7 +436,8 @@ int launch_wide(const MmArgs &g, const CUtensorMap &ta, const CUtensorMap &tw, i
         attr = cudaFuncSetAttribute(k_matmul_fp8_wide<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WD_SMEM);
     });
     if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
-    const int vec = mm_out_vec(g), pairs = aligned(g.out, g.bf16 ? 4 : 8) && g.ldo % 2 == 0;
+    const int vec = mm_out_vec(g) ? 32 : aligned(g.out, 16) && g.ldo * (g.bf16 ? 2 : 4) % 16 == 0 ? 16 : 0;
+    const int pairs = aligned(g.out, g.bf16 ? 4 : 8) && g.ldo % 2 == 0;
     XH_CUDA(launch_head(k_matmul_fp8_wide<S>, dim3((unsigned)grid), WD_THREADS, WD_SMEM, st, S ? S : 1u, g, ta, tw, vec,
                         pairs));
     return XPRESS_OK;

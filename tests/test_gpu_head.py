@@ -290,6 +290,13 @@ def test_matmul_split_k(X, M, N, K):
     _mm(X, M, N, K, F32, out_pad=1)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_matmul_many_rows_by_16_bytes(X, dtype):
+    """Rows of out on 16 bytes, but not on 32, in more tiles than SMs."""
+    _mm(X, 2049, 4104 if dtype is BF16 else 4100, 200, dtype)
+    _mm(X, 2049, 4096, 200, dtype, out_pad=8 if dtype is BF16 else 4)
+
+
 @pytest.mark.parametrize("M, N, K", [(512, 4096, 4096), (300, 600, 8192), (566, 1550, 2048), (200, 4096, 4096),
                                      (129, 257, 16384), (1000, 2000, 8192), (640, 3001, 1544), (513, 100, 8200),
                                      (400, 5000, 3000)])
