@@ -11,9 +11,11 @@
 // of 8 elements), so x is read once; the only exchange is the sum of squares.
 // A warp owns segments of 256 elements: lane l holds 8 consecutive ones (a
 // 16-byte load; a group of 128 is half a warp) or, where a row does not start
-// on 16 bytes, the elements l, l + 32, ... (loads of consecutive elements
-// across the warp; a group is 4 of a lane's elements).  Rows longer than the
-// registers hold (V = 0) are read twice, the second time from L2.
+// on 16 bytes, the pairs at 2 l, 2 l + 64, ..., or where it starts on no pair
+// either the elements l, l + 32, ... (loads of consecutive elements across the
+// warp; a group is 4 of a lane's elements).  11853 x 5202 bf16 with rows on 4
+// bytes: 159 us by elements, 110 by pairs.  Rows longer than the registers hold
+// (V = 0) are read twice, the second time from L2.
 #include "head.h"
 
 namespace xp {
@@ -34,14 +36,49 @@ constexpr int SEG = 256;                        // elements a warp takes at a ti
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Element j of this lane in a segment.
-template <bool VEC> __device__ __forceinline__ int elem(int lane, int j) { return VEC ? lane * 8 + j : j * 32 + lane; }
+// Element j of this lane in a segment; VEC: its consecutive elements (8, 2 or 1).
+template <int VEC> __device__ __forceinline__ int elem(int lane, int j)
+{
+    return VEC == 8 ? lane * 8 + j : VEC == 2 ? j / 2 * 64 + lane * 2 + j % 2 : j * 32 + lane;
+}
+// One or two elements, aligned to their number.
+template <int N> __device__ __forceinline__ void load_n(const uint16_t *p, float *v)
+{
+    if (N == 1) { v[0] = bf2f(*p); return; }
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
+    v[0] = __uint_as_float(w << 16);
+    v[1] = __uint_as_float(w & 0xffff0000u);
+}
+template <int N> __device__ __forceinline__ void load_n(const float *p, float *v)
+{
+    if (N == 1) { v[0] = *p; return; }
+    const float2 w = *reinterpret_cast<const float2 *>(p);
+    v[0] = w.x;
+    v[1] = w.y;
+}
+template <int N> __device__ __forceinline__ void store_n(uint16_t *p, const float *v)
+{
+    if (N == 1) *p = f2bf(v[0]);
+    else *reinterpret_cast<uint32_t *>(p) = pack_bf16(v[0], v[1]);
+}
+template <int N> __device__ __forceinline__ void store_n(float *p, const float *v)
+{
+    if (N == 1) *p = v[0];
+    else *reinterpret_cast<float2 *>(p) = make_float2(v[0], v[1]);
+}
 
 // 8 elements of a segment starting at e0 (zero past H).
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ void load_seg(const T *row, int e0, int H, int lane, float (&v)[8])
 {
-    if (VEC && e0 + lane * 8 + 8 <= H) { load8(row + e0 + lane * 8, v); return; }
+    if (VEC == 8 && e0 + lane * 8 + 8 <= H) { load8(row + e0 + lane * 8, v); return; }
+    // (one branch for the whole warp: with one for each piece it would wait for the
+    // piece before)
+    if (VEC < 8 && e0 + SEG <= H) {
+#pragma unroll
+        for (int j = 0; j < 8; j += VEC) load_n<VEC>(row + e0 + elem<VEC>(lane, j), v + j);
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int e = e0 + elem<VEC>(lane, j);
@@ -49,10 +86,15 @@ __device__ __forceinline__ void load_seg(const T *row, int e0, int H, int lane, 
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ void store_seg(T *row, int e0, int H, int lane, const float (&v)[8])
 {
-    if (VEC && e0 + lane * 8 + 8 <= H) { store8(row + e0 + lane * 8, v); return; }
+    if (VEC == 8 && e0 + lane * 8 + 8 <= H) { store8(row + e0 + lane * 8, v); return; }
+    if (VEC < 8 && e0 + SEG <= H) {
+#pragma unroll
+        for (int j = 0; j < 8; j += VEC) store_n<VEC>(row + e0 + elem<VEC>(lane, j), v + j);
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int e = e0 + elem<VEC>(lane, j);
@@ -61,10 +103,10 @@ __device__ __forceinline__ void store_seg(T *row, int e0, int H, int lane, const
 }
 
 // q and the scales of a segment (two groups) of y.
-template <bool VEC>
+template <int VEC>
 __device__ __forceinline__ void quant_seg(uint8_t *qrow, float *srow, int e0, int H, int lane, const float (&y)[8])
 {
-    if (VEC) {
+    if (VEC == 8) {
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max(m, abs_bits(y[j]));
@@ -89,25 +131,33 @@ __device__ __forceinline__ void quant_seg(uint8_t *qrow, float *srow, int e0, in
             const float s = group_scale(m);
             const ScaleDiv div(s);
             if (lane == 0 && e0 + g * QBLOCK < H) srow[e0 / QBLOCK + g] = s;
+            if (VEC == 2 && e0 + SEG <= H) {
+#pragma unroll
+                for (int j = 4 * g; j < 4 * g + 4; j += 2)
+                    *reinterpret_cast<uint16_t *>(qrow + e0 + elem<VEC>(lane, j)) = to_e4m3x2(div(y[j]), div(y[j + 1]));
+                continue;
+            }
 #pragma unroll
             for (int j = 4 * g; j < 4 * g + 4; ++j) {
-                const int e = e0 + j * 32 + lane;
+                const int e = e0 + elem<VEC>(lane, j);
                 if (e < H) qrow[e] = to_e4m3(div(y[j]));
             }
         }
     }
 }
 
-// grid: rows; V > 0: 32 ceil(H / 256 / V) threads or more; V = 0: any.
+// grid: rows; V > 0: 32 ceil(H / 256 / V) threads or more (of THREADS at most);
+// V = 0: any.
 // FEW: the weights are read before the sum of squares is known, which saves
 // their latency; else after it (from L1), and registers are kept for 2048
 // threads on an SM (16384 x 4096 bf16 with a residual and all outputs: 102 us,
-// 5.9 TB/s; 113 with 1536 threads, 163 with the weights held).
-template <typename T, bool VEC, int V, int THREADS, bool FEW>
+// 5.9 TB/s; 113 with 1536 threads, 163 with the weights held, 100 to 110 with CTAs
+// that stay and copy 2 to 4 rows ahead into shared memory).
+template <typename T, int VEC, int V, int THREADS, bool FEW>
 __global__ void __launch_bounds__(THREADS, FEW ? 1 : 2048 / THREADS) k_rmsnorm(const __grid_constant__ NormArgs a)
 {
     __shared__ float part[THREADS / 32];
-    constexpr int WARPS = THREADS / 32;
+    const int WARPS = blockDim.x / 32;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, H = a.H;
     const int64_t r = blockIdx.x;
     pdl_wait();
@@ -191,14 +241,17 @@ __global__ void __launch_bounds__(THREADS, FEW ? 1 : 2048 / THREADS) k_rmsnorm(c
     }
 }
 
-template <typename T, bool VEC, int V, int THREADS>
+template <typename T, int VEC, int V, int THREADS>
 cudaError_t launch_norm(const NormArgs &a, int rows, bool few, cudaStream_t st)
 {
     auto *k = few ? k_rmsnorm<T, VEC, V, THREADS, true> : k_rmsnorm<T, VEC, V, THREADS, false>;
-    return launch_head(k, dim3(rows), THREADS, 0, st, 1, a);
+    // as many warps as have a segment (12779 x 2301 bf16, 9 segments: 64 us with
+    // 8 warps of two slots, 51 with 5)
+    const int segs = (a.H + SEG - 1) / SEG;
+    return launch_head(k, dim3(rows), V ? 32 * ((segs + V - 1) / V) : THREADS, 0, st, 1, a);
 }
 
-template <typename T, bool VEC>
+template <typename T, int VEC>
 cudaError_t launch_norm_h(const NormArgs &a, int rows, bool few, cudaStream_t st)
 {
     const int segs = (a.H + SEG - 1) / SEG;
@@ -207,20 +260,24 @@ cudaError_t launch_norm_h(const NormArgs &a, int rows, bool few, cudaStream_t st
     if (segs <= 16 && !few) return launch_norm<T, VEC, 2, 256>(a, rows, few, st);
     if (segs <= 16) return launch_norm<T, VEC, 1, 512>(a, rows, few, st);
     if (segs <= 32) return launch_norm<T, VEC, 2, 512>(a, rows, few, st);
-    if (segs <= 64) return launch_norm<T, VEC, 2, 1024>(a, rows, true, st);
+    if (segs <= 64) return launch_norm<T, VEC, 2, 1024>(a, rows, few, st);
     return launch_norm<T, VEC, 0, 1024>(a, rows, true, st);
 }
 
 template <typename T>
 cudaError_t launch_norm_t(const NormArgs &a, int rows, cudaStream_t st)
 {
-    // 16-byte loads need every row of every tensor on 16 bytes (q: 8)
+    // n elements at a time need every row of every tensor on n elements
     const int es = sizeof(T);
-    auto on16 = [&](const void *p, int64_t ld) { return !p || (aligned(p, 16) && ld * es % 16 == 0); };
-    const bool vec = on16(a.x, a.ldx) && on16(a.residual, a.ldr) && on16(a.weight, 0) && on16(a.sum, a.lds) &&
-                     on16(a.y, a.ldy) && (!a.q || (aligned(a.q, 8) && a.ldq % 8 == 0));
+    auto on = [&](int bytes, int q_bytes) {
+        auto rows_on = [&](const void *p, int64_t ld) { return !p || (aligned(p, bytes) && ld * es % bytes == 0); };
+        return rows_on(a.x, a.ldx) && rows_on(a.residual, a.ldr) && rows_on(a.weight, 0) && rows_on(a.sum, a.lds) &&
+               rows_on(a.y, a.ldy) && (!a.q || (aligned(a.q, q_bytes) && a.ldq % q_bytes == 0));
+    };
     const bool few = rows <= current_sms();      // a CTA per SM at most: latency counts
-    return vec ? launch_norm_h<T, true>(a, rows, few, st) : launch_norm_h<T, false>(a, rows, few, st);
+    return on(16, 8) ? launch_norm_h<T, 8>(a, rows, few, st)
+         : on(2 * es, 2) ? launch_norm_h<T, 2>(a, rows, few, st)
+                         : launch_norm_h<T, 1>(a, rows, few, st);
 }
 
 }  // namespace

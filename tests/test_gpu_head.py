@@ -108,6 +108,16 @@ def test_norm(X, rows, H, pad, off, dtype):
     assert (qb[:, :off] == 0x5a).all() and (qb[:, off + H:] == 0x5a).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows, H, pad, off", [
+    (1, 2, 0, 0), (3, 126, 4, 2), (5, 129, 5, 2), (700, 130, 0, 0), (200, 1001, 1, 4), (300, 2301, 3, 0), (400, 2302, 0, 0),
+    (160, 3527, 0, 0), (161, 5202, 8, 2), (170, 4354, 0, 2), (2, 8190, 4, 2), (3, 12003, 3, 6), (3, 16386, 0, 0),
+    (2, 40002, 0, 0), (155, 8193, 7, 0)])
+def test_norm_odd_rows(X, rows, H, pad, off, dtype):
+    """Rows that start on a pair but not on 16 bytes, numbers of segments that fill no block."""
+    test_norm(X, rows, H, pad, off, dtype)
+
+
 @pytest.mark.parametrize("H", [256, 1027, 33000])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_norm_single_outputs_and_in_place(X, H, dtype):
