@@ -73,19 +73,18 @@ constexpr int MAX_V = 1 << 24;     // so that Share's division by multiplication
 constexpr int LWARPS = LT / 32;
 constexpr uint32_t IN_PROMPT = 1u << 31, IN_BLOCK = 1u << 30, TIMES = IN_BLOCK - 1;   // of a count
 
-template <bool VEC>
+// The first n elements of r to p, 16-byte aligned.
 __device__ __forceinline__ void store_raw(uint16_t *p, int n, const Raw8<uint16_t> &r)
 {
-    if (VEC && n >= 8) { *reinterpret_cast<uint4 *>(p) = r.a; return; }
+    if (n >= 8) { *reinterpret_cast<uint4 *>(p) = r.a; return; }
     const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (j < n) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
 }
-template <bool VEC>
 __device__ __forceinline__ void store_raw(float *p, int n, const Raw8<float> &r)
 {
-    if (VEC && n >= 8) {
+    if (n >= 8) {
         *reinterpret_cast<float4 *>(p) = r.a;
         *reinterpret_cast<float4 *>(p + 4) = r.b;
         return;
@@ -95,6 +94,21 @@ __device__ __forceinline__ void store_raw(float *p, int n, const Raw8<float> &r)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (j < n) p[j] = v[j];
+}
+
+// The warp's 256 elements, 8 of each lane, to p, where n of them have a place: by
+// way of shared memory, so that the lanes store consecutive elements (each its
+// own 8, they would write every 32-byte sector 8 times or more).
+template <typename T>
+__device__ __forceinline__ void store_turned(T *p, int n, const Raw8<T> &r, Raw8<T> *turn)
+{
+    const int lane = threadIdx.x % 32;
+    turn[lane] = r;
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k * 32 + lane < n) p[k * 32 + lane] = reinterpret_cast<const T *>(turn)[k * 32 + lane];
+    __syncwarp();
 }
 
 // Word masks of the 8 bf16 elements of a piece for every byte of bits (bit k:
@@ -185,13 +199,19 @@ __device__ __forceinline__ void count_token(uint32_t *cnt, const Share &sh, int 
 // grid (shares of 2048 U ids, sequences, parts of the rows); shared memory with patch: counts [C],
 // with a bias as many floats, the list [C] (16 bits).
 // MULTI: several rows of a CTA.  NT: LT threads, or more, of which those past LT count and patch only.
+// The next row's pieces of fp32 want registers: three CTAs per SM (136 rows of
+// 55191: 37 us with four, 24 with three; bf16 takes four, 340 rows of 55192: 45,
+// 56 with three).
+template <typename T, bool MULTI> constexpr int ctas_per_sm() { return MULTI && sizeof(T) == 4 ? 3 : 4; }
+
 template <typename T, bool VEC, int U, bool MULTI, int NT>
-__global__ void __launch_bounds__(NT, NT > LT ? 1 : MULTI && U == 4 ? 2 : 4) k_logits(const __grid_constant__ LogitsArgs a)
+__global__ void __launch_bounds__(NT, NT > LT ? 1 : MULTI && U == 4 ? 2 : ctas_per_sm<T, MULTI>()) k_logits(const __grid_constant__ LogitsArgs a)
 {
     constexpr int C = LT * 8 * U;
     constexpr int PR = MULTI ? 4 : 1;              // rows patched together
     __shared__ int listed;
     __shared__ uint4 masks[sizeof(T) == 2 ? 256 : 1];
+    __shared__ Raw8<T> turn[VEC ? 1 : LT];
     extern __shared__ uint32_t cnt[];              // [C]: IN_PROMPT | IN_BLOCK | times answered
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int q = blockIdx.y, V = a.V, R = a.rows;
@@ -374,10 +394,16 @@ __global__ void __launch_bounds__(NT, NT > LT ? 1 : MULTI && U == 4 ? 2 : 4) k_l
             for (int u = 0; u < U; ++u) {
                 const int id = id0 + u * id_step;
                 mx[u] = -INFINITY;
-                if (id >= V) continue;
+                const int seg = id - lane * 8;     // the warp's first id
+                if ((VEC ? id : seg) >= V) continue;
                 const uint32_t keep = (allow | special) >> (8 * u) & 0xffu;
                 if (keep != 0xffu) select8(cur.x[u], keep, a.mask_value, masks);
-                if (out && !(in_place && keep == 0xffu)) store_raw<VEC>(orow + id, V - id, cur.x[u]);
+                const bool moves = out && !(in_place && keep == 0xffu);
+                if (VEC) {
+                    if (moves) store_raw(orow + id, V - id, cur.x[u]);
+                } else if (__any_sync(0xffffffffu, moves)) {
+                    store_turned(orow + seg, V - seg, cur.x[u], turn + warp * 32);
+                }
                 if (part) {
                     const uint32_t us = use >> (8 * u) & 0xffu;
                     Raw8<T> y = cur.x[u];
@@ -498,23 +524,23 @@ int logits_slots(int n_seq, int V, int sms)
     return U;
 }
 
-// Few CTAs: a sequence's rows are split over as many as an SM takes, four (17
-// rows of 10000 bf16, 3 requests: 11.7 us with parts of 4 rows, 8.8 with one row
-// each).  Each part counts the history for itself, so that from 4096 tokens on
-// there are two per SM (16 rows of 32000, 4 requests of 8000 tokens: 18 us,
+// Few CTAs: a sequence's rows are split over as many as the SMs hold at a time
+// (17 rows of 10000 bf16, 3 requests: 11.7 us with parts of 4 rows, 8.8 with one
+// row each).  Each part counts the history for itself, so that from 4096 tokens
+// on there are two per SM (16 rows of 32000, 4 requests of 8000 tokens: 18 us,
 // 22 with four).  Where not even every SM gets one and histories are longer yet,
 // a CTA takes 512 threads for the counts and the patch (6 sequences of 30000
 // tokens, V = 32003, 5 rows: 32 -> 21 us; a short history gains nothing), and
 // there is one per SM (17 rows of 5000, one request of 20000 tokens: 11 us, 43
 // with all rows in one CTA).
-LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, int sms)
+LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, bool f32, int sms)
 {
     LogitsPlan p{logits_slots(n_seq, a.V, sms), LT, a.rows};
     const int64_t ctas = (int64_t)n_seq * ((a.V + LT * 8 - 1) / (LT * 8));
     if (p.U != 1) return p;
     const int64_t each = a.patch ? a.n_hist / n_seq : 0;
     if (ctas <= sms && each >= 8192) p.threads = LT_FEW;
-    const int64_t room = (int64_t)sms * (p.threads == LT_FEW ? 1 : each >= 4096 ? 2 : 4);
+    const int64_t room = (int64_t)sms * (p.threads == LT_FEW ? 1 : each >= 4096 ? 2 : f32 ? ctas_per_sm<float, true>() : 4);
     const int64_t parts = room > ctas ? room / ctas : 1;
     p.rows_each = (int)((a.rows + parts - 1) / parts);
     return p;
@@ -598,7 +624,7 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
     a.patch = in->repetition || in->frequency || in->presence || in->bias_ids;
     a.part = in->argmax ? static_cast<unsigned long long *>(ws) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const LogitsPlan plan = logits_plan(a, in->n_seq, sms);
+    const LogitsPlan plan = logits_plan(a, in->n_seq, in->dtype == XPRESS_F32, sms);
     a.rows_each = plan.rows_each;
     const bool vec = aligned(in->logits, 16) && in->ld * es % 16 == 0 &&
                      (!in->out || (aligned(in->out, 16) && in->ldo * es % 16 == 0));
