@@ -196,16 +196,22 @@ __device__ __forceinline__ void count_token(uint32_t *cnt, const Share &sh, int 
     }
 }
 
-// grid (shares of 2048 U ids, sequences, parts of the rows); shared memory with patch: counts [C],
-// with a bias as many floats, the list [C] (16 bits).
-// MULTI: several rows of a CTA.  NT: LT threads, or more, of which those past LT count and patch only.
-// The next row's pieces of fp32 want registers: three CTAs per SM (136 rows of
-// 55191: 37 us with four, 24 with three; bf16 takes four, 340 rows of 55192: 45,
-// 56 with three).
-template <typename T, bool MULTI> constexpr int ctas_per_sm() { return MULTI && sizeof(T) == 4 ? 3 : 4; }
+// CTAs of LT threads that an SM takes.  The next row's pieces want registers:
+// three CTAs for several rows of fp32 by two slots (510 rows of 151936: 154 us with
+// four, 135 with three) or element by element (136 rows of 55191: 37 and 24), four
+// where these suffice (225 rows of 25984 fp32: 20 us, 26 with three; 340 rows of
+// 55192 bf16: 45 and 56).
+constexpr int ctas_per_sm(bool f32, bool vec, int U, bool multi)
+{
+    return !multi ? 4 : U == 4 ? 2 : f32 && (U == 2 || !vec) ? 3 : 4;
+}
 
+// grid (shares of 2048 U ids, sequences, parts of the rows); shared memory with
+// patch: counts [C], with a bias as many floats, the list [C] (16 bits).
+// MULTI: several rows of a CTA.  NT: LT threads, or more, of which those past LT
+// count and patch only.
 template <typename T, bool VEC, int U, bool MULTI, int NT>
-__global__ void __launch_bounds__(NT, NT > LT ? 1 : MULTI && U == 4 ? 2 : ctas_per_sm<T, MULTI>()) k_logits(const __grid_constant__ LogitsArgs a)
+__global__ void __launch_bounds__(NT, NT > LT ? 1 : ctas_per_sm(sizeof(T) == 4, VEC, U, MULTI)) k_logits(const __grid_constant__ LogitsArgs a)
 {
     constexpr int C = LT * 8 * U;
     constexpr int PR = MULTI ? 4 : 1;              // rows patched together
@@ -533,14 +539,14 @@ int logits_slots(int n_seq, int V, int sms)
 // tokens, V = 32003, 5 rows: 32 -> 21 us; a short history gains nothing), and
 // there is one per SM (17 rows of 5000, one request of 20000 tokens: 11 us, 43
 // with all rows in one CTA).
-LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, bool f32, int sms)
+LogitsPlan logits_plan(const LogitsArgs &a, int n_seq, bool f32, bool vec, int sms)
 {
     LogitsPlan p{logits_slots(n_seq, a.V, sms), LT, a.rows};
     const int64_t ctas = (int64_t)n_seq * ((a.V + LT * 8 - 1) / (LT * 8));
     if (p.U != 1) return p;
     const int64_t each = a.patch ? a.n_hist / n_seq : 0;
     if (ctas <= sms && each >= 8192) p.threads = LT_FEW;
-    const int64_t room = (int64_t)sms * (p.threads == LT_FEW ? 1 : each >= 4096 ? 2 : f32 ? ctas_per_sm<float, true>() : 4);
+    const int64_t room = (int64_t)sms * (p.threads == LT_FEW ? 1 : each >= 4096 ? 2 : ctas_per_sm(f32, vec, 1, true));
     const int64_t parts = room > ctas ? room / ctas : 1;
     p.rows_each = (int)((a.rows + parts - 1) / parts);
     return p;
@@ -624,10 +630,10 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
     a.patch = in->repetition || in->frequency || in->presence || in->bias_ids;
     a.part = in->argmax ? static_cast<unsigned long long *>(ws) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const LogitsPlan plan = logits_plan(a, in->n_seq, in->dtype == XPRESS_F32, sms);
-    a.rows_each = plan.rows_each;
     const bool vec = aligned(in->logits, 16) && in->ld * es % 16 == 0 &&
                      (!in->out || (aligned(in->out, 16) && in->ldo * es % 16 == 0));
+    const LogitsPlan plan = logits_plan(a, in->n_seq, in->dtype == XPRESS_F32, vec, sms);
+    a.rows_each = plan.rows_each;
     XH_CUDA(in->dtype == XPRESS_BF16
                 ? (vec ? launch_logits<uint16_t, true>(a, in->n_seq, plan, st)
                        : launch_logits<uint16_t, false>(a, in->n_seq, plan, st))
