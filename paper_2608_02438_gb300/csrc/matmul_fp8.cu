@@ -55,6 +55,7 @@ struct MmBars {
     uint64_t full[MM_MAX_STAGES], empty[MM_MAX_STAGES];
     uint64_t tfull[4], tempty[4];
     uint64_t drain, joined;
+    long long since;
     uint32_t tmem_base;
     int abort;
 };
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(MM_THREADS, 2)
         mbar_init(&sh.drain, 1);
         mbar_init(&sh.joined, 1);
         sh.abort = 0;
+        sh.since = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tmap_w);
         tma_prefetch_desc(&tmap_a);
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(MM_THREADS, 2)
                 const int i = kb - kb0;
                 if ((i & 31) == 0) sw32 = kb + lane < kb1 ? swr[kb + lane] : 0.0f;
                 const float sw = __shfl_sync(0xffffffffu, sw32, i & 31);
-                if (ok) ok = mm_wait(&sh.tfull[buf], tphase, abort);
+                if (ok) ok = mm_wait(&sh.tfull[buf], tphase, abort, MM_WAIT_CYCLES, S > 1 ? &sh.since : nullptr);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -275,8 +277,7 @@ __global__ void __launch_bounds__(MM_THREADS, 2)
         const int rows = max(0, min(share, g.M - m0)), sent = (rows + vw - 1) / vw * vw;
         if (sent > 0) {
             if (threadIdx.x == 0) mbar_expect_tx(&sh.joined, S * sent * MM_BN * 4);
-            // (longer than any sender's own waits, which end in its stores)
-            if (mm_wait(&sh.joined, 0, abort, 3 * MM_WAIT_CYCLES))
+            if (mm_wait_joined(&sh.joined, abort))
                 for (int i = threadIdx.x; i < rows * MM_BN; i += MM_THREADS) {
                     const int j = i / MM_BN, row = i % MM_BN, n = rb * MM_BN + row;
                     float v = 0.0f;

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "head.h"
+#include "matmul_wait.h"
 
 namespace xp {
 
@@ -48,26 +49,6 @@ __device__ __forceinline__ void st_async4(uint32_t addr, uint32_t bar, const flo
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
                  "r"(bar), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3])
                  : "memory");
-}
-
-// Bounded wait for a phase of `bar`.  It polls (a wait with a sleep hint wakes
-// up later: an earlier form at 2048 x 38912 x 4096 took 739 us against 683) and bounds itself by
-// the SM's cycle counter, read once in 64 polls: the global timer's latency
-// would sit in every hand-off of a K block.
-constexpr long long MM_WAIT_CYCLES = 4000000000ll;       // about 2 s
-__device__ __forceinline__ bool mm_wait(uint64_t *bar, uint32_t parity, volatile int *abort,
-                                        long long cycles = MM_WAIT_CYCLES)
-{
-    long long t0 = 0;
-    for (uint32_t it = 1;; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 63u) == 0) {
-            if (*abort) return false;
-            const long long t = clock64();
-            if (t0 == 0) t0 = t;
-            else if (t - t0 > cycles) { *abort = 1; return false; }
-        }
-    }
 }
 
 // Instruction descriptor, kind::f8f6f4: fp32 sums, e4m3 A and B, both K-major.

@@ -75,6 +75,7 @@ struct WideBars {
     uint64_t sfull[2], sempty[2];
     uint64_t drain[2];
     uint64_t joined[WD_EPI];
+    long long since;
     uint32_t tmem_base;
     int abort;
 };
@@ -165,6 +166,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
         for (int i = 0; i < 2; ++i) mbar_init(&sh.drain[i], 1);
         for (int i = 0; i < WD_EPI; ++i) mbar_init(&sh.joined[i], 1);
         sh.abort = 0;
+        sh.since = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tmap_w);
         tma_prefetch_desc(&tmap_a);
@@ -299,6 +301,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
         uint32_t par = 0, tphase = 0, sphase = 0;
         bool ok = true;
         int m0 = g.M, n0 = g.N;
+        volatile long long *since = S > 1 ? &sh.since : nullptr;    // one limit before the sums go to other CTAs
         float acc[WD_COLS];
         for (int64_t t = first; t < tiles; t += step) {
             int row, col;
@@ -310,8 +313,8 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
 #pragma unroll 4
             for (int kb = 0; kb < kb1 - kb0; ++kb) {
                 const int i = kb % WD_GROUP;
-                if (i == 0) ok = mm_wait(&sh.sfull[slot], sphase, abort);
-                ok = __all_sync(0xffffffffu, ok && mm_wait(&sh.tfull[par * 2 + half], tphase, abort));
+                if (i == 0) ok = mm_wait(&sh.sfull[slot], sphase, abort, MM_WAIT_CYCLES, since);
+                ok = __all_sync(0xffffffffu, ok && mm_wait(&sh.tfull[par * 2 + half], tphase, abort, MM_WAIT_CYCLES, since));
                 if (!ok) break;
                 tc_fence_after();
                 const float f = scales[slot * (WD_SCALES / 4) + (2 * i + half) * 128 + q * 32 + lane];
@@ -390,8 +393,7 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
                         }
                     }
             __syncwarp();
-            // (longer than any sender's own waits, which end in its stores)
-            if (S > 1) ok = __all_sync(0xffffffffu, mm_wait(joined, 0, abort, 3 * MM_WAIT_CYCLES)) && ok;
+            if (S > 1) ok = __all_sync(0xffffffffu, mm_wait_joined(joined, abort)) && ok;
             const int c = lane % LPR * 2, n = n0 + rank * share + c;
             const float *from = sums + c / 4 * WD_GROUP4 + (et - lane) * 4 + c % 4;
 #pragma unroll 2
