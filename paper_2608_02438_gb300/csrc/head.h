@@ -3,6 +3,8 @@
 // and stores, and the host helpers of their entry points.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 #include "xpress.h"
 
@@ -200,6 +202,33 @@ cudaError_t launch_head(void (*kernel)(KArgs...), dim3 grid, unsigned block, siz
 
 // SMs of the current device (0 on an error).
 int current_sms();
+
+constexpr int MAX_DEVICES = 64;          // that what is known of a device is kept for
+
+// What holds for the current device only, a kernel's attributes above all, set by
+// the first call on each device.  A failure is not kept: the next call tries again.
+class OncePerDevice {
+    std::atomic<bool> done_[MAX_DEVICES] = {};
+
+public:
+    template <typename Set> cudaError_t operator()(Set set)
+    {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess) {
+            if (dev < MAX_DEVICES && done_[dev].load(std::memory_order_acquire)) return cudaSuccess;
+            e = set();
+        }
+        if (e != cudaSuccess) (void)cudaGetLastError();
+        else if (dev < MAX_DEVICES) done_[dev].store(true, std::memory_order_release);
+        return e;
+    }
+};
+// The kernel's limit of dynamic shared memory on the current device.
+template <typename K> cudaError_t allow_smem(OncePerDevice &once, K kernel, size_t bytes)
+{
+    return once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); });
+}
 
 // 2-D byte tensor [rows][inner] with a row pitch of `pitch` bytes, 128-byte
 // swizzle, zero fill out of bounds (base 16-byte aligned, pitch a multiple of 16).

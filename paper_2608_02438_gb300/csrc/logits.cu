@@ -556,9 +556,9 @@ template <typename T, bool VEC, int U, bool MULTI, int NT>
 cudaError_t launch_logits_u(LogitsArgs a, int n_seq, cudaStream_t st)
 {
     constexpr int C = LT * 8 * U;
-    static const cudaError_t attr =
-        cudaFuncSetAttribute(k_logits<T, VEC, U, MULTI, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C * 10);
-    if (attr != cudaSuccess) { (void)cudaGetLastError(); return attr; }
+    static OncePerDevice once;
+    const cudaError_t attr = allow_smem(once, k_logits<T, VEC, U, MULTI, NT>, C * 10);
+    if (attr != cudaSuccess) return attr;
     const size_t smem = a.patch ? (size_t)C * (a.bias_ids ? 10 : 6) : 0;
     const unsigned G = (a.V + C - 1) / C;
     a.magic = (uint32_t)(((1ull << 32) + G - 1) / G);

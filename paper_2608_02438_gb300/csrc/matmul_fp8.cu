@@ -26,8 +26,6 @@
 // Bound by the weights' stream for large w (16 x 151936 x 4096: 96 us, 6.5 TB/s
 // of w alone), by the chain first copy - MMAs - join - store for small ones
 // (1 x 4096 x 4096: 5.9 us).
-#include <mutex>
-
 #include "matmul_fp8.h"
 
 namespace xp {
@@ -321,32 +319,30 @@ struct MmPlan {
     float us;
 };
 
-// Clusters of 2, 4 or 8 CTAs with an SM each that the GPU runs at a time.
+// Clusters of 2, 4 or 8 CTAs with an SM each that the current device runs at a time
+// (0, so no split, where it cannot tell).
 int resident_clusters(int S)
 {
-    static std::once_flag once;
-    static int n[3];
-    std::call_once(once, [] {
-        for (int i = 0; i < 3; ++i) {
-            cudaLaunchAttribute a[1];
-            a[0].id = cudaLaunchAttributeClusterDimension;
-            a[0].val.clusterDim.x = 2u << i;
-            a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
-            cudaLaunchConfig_t cfg{};
-            cfg.gridDim = dim3(2u << i);
-            cfg.blockDim = dim3(MM_THREADS);
-            cfg.dynamicSmemBytes = MM_SMEM_LIMIT - 1024;
-            cfg.attrs = a;
-            cfg.numAttrs = 1;
-            if (cudaFuncSetAttribute(k_matmul_fp8<16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)MM_SMEM_LIMIT - 1024) != cudaSuccess ||
-                cudaOccupancyMaxActiveClusters(&n[i], k_matmul_fp8<16>, &cfg) != cudaSuccess) {
-                (void)cudaGetLastError();
-                n[i] = 0;
-            }
-        }
-    });
-    return n[S == 2 ? 0 : S == 4 ? 1 : 2];
+    static std::atomic<int> known[MAX_DEVICES][3];       // plus 1
+    static OncePerDevice once;
+    const int i = S == 2 ? 0 : S == 4 ? 1 : 2;
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    if (dev < MAX_DEVICES && (n = known[dev][i].load(std::memory_order_relaxed)) > 0) return n - 1;
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeClusterDimension;
+    a[0].val.clusterDim.x = S;
+    a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(S);
+    cfg.blockDim = dim3(MM_THREADS);
+    cfg.dynamicSmemBytes = MM_SMEM_LIMIT - 1024;
+    cfg.attrs = a;
+    cfg.numAttrs = 1;
+    if (allow_smem(once, k_matmul_fp8<16>, MM_SMEM_LIMIT - 1024) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveClusters(&n, k_matmul_fp8<16>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    if (dev < MAX_DEVICES) known[dev][i].store(n + 1, std::memory_order_relaxed);
+    return n;
 }
 
 MmPlan plan_few(int M, int N, int KB, int NT, int sms)
@@ -417,12 +413,8 @@ int launch_mm(MmArgs g, int S, const void *a, int64_t lda, const void *w, int64_
     if (S > 1 && g.stages > want) g.stages = want;
     g.table_bytes = (uint32_t)table;
     const size_t smem = fixed - 1024 + (size_t)g.stages * Sh::STAGE;
-    static std::once_flag once;
-    static cudaError_t attr;
-    std::call_once(once, [] {
-        attr = cudaFuncSetAttribute(k_matmul_fp8<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MM_SMEM_LIMIT - 1024);
-    });
-    if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
+    static OncePerDevice once;
+    XH_CUDA(allow_smem(once, k_matmul_fp8<NT>, MM_SMEM_LIMIT - 1024));
     // by K blocks only where they are whole: past the last one the rows'
     // padding would be read
     CUtensorMap tw{}, ta{};

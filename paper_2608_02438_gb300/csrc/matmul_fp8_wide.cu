@@ -38,8 +38,6 @@
 // 321, a pair of CTAs on a 256 x 256 tile with two TMEM buffers 568 (each K block
 // waited for the other CTA's epilogue); sharing copies in clusters of 2 or 4 CTAs
 // by multicast gained nothing.
-#include <mutex>
-
 #include "matmul_fp8.h"
 
 namespace xp {
@@ -432,12 +430,8 @@ __global__ void __launch_bounds__(WD_THREADS, 1)
 template <int S>
 int launch_wide(const MmArgs &g, const CUtensorMap &ta, const CUtensorMap &tw, int64_t grid, cudaStream_t st)
 {
-    static std::once_flag once;
-    static cudaError_t attr;
-    std::call_once(once, [] {
-        attr = cudaFuncSetAttribute(k_matmul_fp8_wide<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WD_SMEM);
-    });
-    if (attr != cudaSuccess) { (void)cudaGetLastError(); return XPRESS_ERR_CUDA; }
+    static OncePerDevice once;
+    XH_CUDA(allow_smem(once, k_matmul_fp8_wide<S>, WD_SMEM));
     const int vec = mm_out_vec(g) ? 32 : aligned(g.out, 16) && g.ldo * (g.bf16 ? 2 : 4) % 16 == 0 ? 16 : 0;
     const int pairs = aligned(g.out, g.bf16 ? 4 : 8) && g.ldo % 2 == 0;
     XH_CUDA(launch_head(k_matmul_fp8_wide<S>, dim3((unsigned)grid), WD_THREADS, WD_SMEM, st, S ? S : 1u, g, ta, tw, vec,

@@ -1051,7 +1051,6 @@ bool tmap_bytes_kblocks(CUtensorMap *m, const void *base, uint64_t kblocks, uint
 
 int current_sms()
 {
-    constexpr int MAX_DEVICES = 64;
     static std::atomic<int> sms[MAX_DEVICES];
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
