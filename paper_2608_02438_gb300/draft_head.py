@@ -36,7 +36,13 @@ MASKED = -8192.0
 class Rules:
     """The sampling rules of b requests (tensors as binding.process_logits takes
     them; None: the rule is off).  mask holds the grammar states' bit rows;
-    base_mask_row [b * B] and target_mask_row [b * (B + 1)] name a row's state."""
+    base_mask_row [b * B] and target_mask_row [b * (B + 1)] name a row's state,
+    -1 for a row that is not masked.  A mask needs the table of the rows that it is
+    to be used on (ValueError without: nothing else tells a row's state).
+
+    What is emitted is allowed by its target row's state, unless that state allows
+    nothing: such a row is MASKED throughout and some forbidden token comes out of it
+    (id 0 at temperature 0).  End the request instead of asking for that row."""
     repetition: torch.Tensor | None = None
     frequency: torch.Tensor | None = None
     presence: torch.Tensor | None = None
@@ -52,6 +58,13 @@ class Rules:
 
     def common(self) -> dict:
         return {k: v for k, v in vars(self).items() if not k.endswith("mask_row")}
+
+    def rows(self, table: str) -> torch.Tensor | None:
+        """The state table `table` of a grammar; None without a grammar."""
+        rows = getattr(self, table)
+        if (self.mask is None) != (rows is None):
+            raise ValueError(f"Rules: mask and {table} go together (-1 in {table} leaves a row unmasked)")
+        return rows
 
 
 class DraftHead:
@@ -70,7 +83,8 @@ class DraftHead:
         """x [b, B, H] (the drafter's last layer, before its final norm) -> h
         [b, B, H], s [b, B, V] under the rules, their first maxima draft [b, B]
         (0 where a mask allows nothing), and the residual stream sum."""
-        R = self.refiner
+        R, rules = self.refiner, rules or Rules()
+        mask_row = rules.rows("base_mask_row")
         b = x.shape[0]
         n, dev = b * R.B, x.device
         h = torch.empty((n, R.H), dtype=torch.bfloat16, device=dev)
@@ -83,27 +97,28 @@ class DraftHead:
                   residual=None if residual is None else residual.reshape(n, R.H), sum_out=total, y_out=h, q_out=q,
                   scale_out=scale)
         X.matmul_fp8(q, scale, self.w, self.w_scale, s)
-        rules = rules or Rules()
-        X.process_logits(s, s, draft, rows=R.B, mask_row=rules.base_mask_row, mask_value=MASKED, **rules.common())
+        X.process_logits(s, s, draft, rows=R.B, mask_row=mask_row, mask_value=MASKED, **rules.common())
         return dict(h=h.view(b, R.B, R.H), s=s.view(b, R.B, R.V), draft=draft.clamp_(min=0).view(b, R.B),
                     sum=None if total is None else total.view(b, R.B, R.H))
 
     def target_logits(self, target, tokens, rules: Rules | None = None):
         """The rules on the target's rows [b, B + 1, V] of the blocks `tokens`
         [b, B]: row j counts the block's tokens before it as answered."""
-        R = self.refiner
-        rules = rules or Rules()
+        R, rules = self.refiner, rules or Rules()
+        mask_row = rules.rows("target_mask_row")
         out = torch.empty_like(target)
         n = target.shape[0] * (R.B + 1)
         X.process_logits(target.view(n, R.V), out.view(n, R.V), rows=R.B + 1, draft=tokens,
-                         mask_row=rules.target_mask_row, mask_value=MASKED, **rules.common())
+                         mask_row=mask_row, mask_value=MASKED, **rules.common())
         return out
 
     def round(self, x, residual, target, anchor, temperature, seed, offset: int, K_max: int,
               rules: Rules | None = None) -> dict:
         """One round on torch's current stream, which has to be the refiner's:
         base logits, refinement and acceptance against target [b, B + 1, V]."""
-        R = self.refiner
+        R, rules = self.refiner, rules or Rules()
+        for table in ("base_mask_row", "target_mask_row"):         # before anything is launched
+            rules.rows(table)
         if torch.cuda.current_stream(x.device).cuda_stream != R.stream.cuda_stream:
             raise ValueError("call round() on the refiner's stream")
         base = self.base_logits(x, residual, rules)
