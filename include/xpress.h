@@ -373,7 +373,8 @@ int xpress_debug_gemm(const void *A, int a_mn, const void *B, int b_mn, int M, i
  *   q     = e4m3(y / scale)                        (nearest even)
  * in fp32, every output rounded once from it (the norm is of the unrounded
  * sum).  sum, y and (q, scale) are optional; at least one is given.  sum and y
- * may be the same memory as x or residual (same pitch).  A row with a NaN or
+ * may be the same memory as x or residual (same pitch).  Rows of any finite t
+ * follow the formula, also where t^2 leaves fp32's range.  A row with a NaN or
  * an infinity gives NaNs, as the formula does; a NaN in a group shows in its
  * scale.  rows = 0 does nothing.
  * Errors: INVALID_ARG (NULL x / weight, no output, q without scale, a pitch

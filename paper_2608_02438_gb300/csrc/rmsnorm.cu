@@ -5,7 +5,8 @@
 //   scale_g = max(max_{i in g} |y_i| / 448, 2^-126),  q_i = e4m3(y_i / scale_g)
 // for groups g of 128 consecutive elements.  The norm is of the 32-bit sum,
 // not of its stored rounding, and q is of the 32-bit y: each output is rounded
-// once.
+// once.  Rows whose squares leave the range of 32 bits are scaled by a power of two
+// first, so that any finite row has the norm of the formula.
 //
 // One CTA per row.  A thread keeps its share of the row in registers (V slots
 // of 8 elements), so x is read once; the only exchange is the sum of squares.
@@ -33,6 +34,7 @@ struct NormArgs {
 };
 
 constexpr int SEG = 256;                        // elements a warp takes at a time
+constexpr float MIN_MEAN = 7.52316385e-37f;     // 2^-120: what the squares' underflow adds to a mean, 2^-150, is below 2^-29 of it
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
@@ -213,14 +215,57 @@ __global__ void __launch_bounds__(THREADS, FEW ? 1 : 2048 / THREADS) k_rmsnorm(c
             ss += s8;
         }
     }
+    auto over_block = [&](float v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (lane == 0) part[warp] = ss;
-    __syncthreads();
-    ss = lane < WARPS ? part[lane] : 0.0f;
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) part[warp] = v;
+        __syncthreads();
+        v = lane < WARPS ? part[lane] : 0.0f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float inv = 1.0f / sqrtf(ss / (float)H + a.eps);
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    };
+    float mean = over_block(ss) / (float)H + a.eps, up = 1.0f;
+    if (mean == INFINITY || mean < MIN_MEAN) {
+        // out of the squares' range (magnitudes above 1.8e19, or so small that eps
+        // does not cover what underflows): the row once more, times the power of two
+        // `up` that brings its largest magnitude, or the root of eps, to 2^40 (2^30
+        // squares still add up, and what underflows there does so in y as well)
+        auto all = [&](auto f) {                   // f(t of a segment)
+            if (V) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if ((i * WARPS + warp) * SEG < H) f(t[i]);
+            } else {
+                for (int e0 = warp * SEG; e0 < H; e0 += WARPS * SEG) {
+                    load_t(e0, t[0]);
+                    f(t[0]);
+                }
+            }
+        };
+        uint32_t m = __float_as_uint(sqrtf(a.eps));
+        all([&](float (&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+        });
+        m = __reduce_max_sync(0xffffffffu, m);
+        __syncthreads();                           // all have read part
+        if (lane == 0) part[warp] = __uint_as_float(m);
+        __syncthreads();
+        m = __reduce_max_sync(0xffffffffu, lane < WARPS ? __float_as_uint(part[lane]) : 0u);
+        up = __uint_as_float((uint32_t)min(294 - (int)(m >> 23), 253) << 23);
+        ss = 0.0f;
+        all([&](float (&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] *= up;
+                ss = fmaf(v[j], v[j], ss);
+            }
+        });
+        __syncthreads();
+        mean = over_block(ss) / (float)H + a.eps * up * up;
+    }
+    const float inv = 1.0f / sqrtf(mean);
     if (V) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -236,6 +281,8 @@ __global__ void __launch_bounds__(THREADS, FEW ? 1 : 2048 / THREADS) k_rmsnorm(c
             load_t(e0, t[0]);
             if (sum) store_seg<T, VEC>(sum, e0, H, lane, t[0]);
             load_seg<T, VEC>(w, e0, H, lane, wv[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[0][j] *= up;
             finish(e0, t[0], wv[0], inv);
         }
     }
