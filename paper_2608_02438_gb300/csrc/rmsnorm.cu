@@ -17,6 +17,8 @@
 // warp; a group is 4 of a lane's elements).  11853 x 5202 bf16 with rows on 4
 // bytes: 159 us by elements, 110 by pairs.  Rows longer than the registers hold
 // (V = 0) are read twice, the second time from L2.
+#include <type_traits>
+
 #include "head.h"
 
 namespace xp {
@@ -288,27 +290,27 @@ __global__ void __launch_bounds__(THREADS, FEW ? 1 : 2048 / THREADS) k_rmsnorm(c
     }
 }
 
-template <typename T, int VEC, int V, int THREADS>
-cudaError_t launch_norm(const NormArgs &a, int rows, bool few, cudaStream_t st)
+template <typename T, int VEC, int V, int THREADS, bool FEW>
+cudaError_t launch_norm(const NormArgs &a, int rows, cudaStream_t st)
 {
-    auto *k = few ? k_rmsnorm<T, VEC, V, THREADS, true> : k_rmsnorm<T, VEC, V, THREADS, false>;
     // as many warps as have a segment (12779 x 2301 bf16, 9 segments: 64 us with
     // 8 warps of two slots, 51 with 5)
     const int segs = (a.H + SEG - 1) / SEG;
-    return launch_head(k, dim3(rows), V ? 32 * ((segs + V - 1) / V) : THREADS, 0, st, 1, a);
+    return launch_head(k_rmsnorm<T, VEC, V, THREADS, FEW>, dim3(rows), V ? 32 * ((segs + V - 1) / V) : THREADS, 0, st, 1, a);
 }
 
-template <typename T, int VEC>
-cudaError_t launch_norm_h(const NormArgs &a, int rows, bool few, cudaStream_t st)
+// (few rows hold twice the warps at 4096 elements; rows past the registers have one form)
+template <typename T, int VEC, bool FEW>
+cudaError_t launch_norm_h(const NormArgs &a, int rows, cudaStream_t st)
 {
+    constexpr int V16 = FEW ? 1 : 2;
     const int segs = (a.H + SEG - 1) / SEG;
-    if (segs <= 4) return launch_norm<T, VEC, 1, 128>(a, rows, few, st);
-    if (segs <= 8) return launch_norm<T, VEC, 1, 256>(a, rows, few, st);
-    if (segs <= 16 && !few) return launch_norm<T, VEC, 2, 256>(a, rows, few, st);
-    if (segs <= 16) return launch_norm<T, VEC, 1, 512>(a, rows, few, st);
-    if (segs <= 32) return launch_norm<T, VEC, 2, 512>(a, rows, few, st);
-    if (segs <= 64) return launch_norm<T, VEC, 2, 1024>(a, rows, few, st);
-    return launch_norm<T, VEC, 0, 1024>(a, rows, true, st);
+    if (segs <= 4) return launch_norm<T, VEC, 1, 128, FEW>(a, rows, st);
+    if (segs <= 8) return launch_norm<T, VEC, 1, 256, FEW>(a, rows, st);
+    if (segs <= 16) return launch_norm<T, VEC, V16, 512 / V16, FEW>(a, rows, st);
+    if (segs <= 32) return launch_norm<T, VEC, 2, 512, FEW>(a, rows, st);
+    if (segs <= 64) return launch_norm<T, VEC, 2, 1024, FEW>(a, rows, st);
+    return launch_norm<T, VEC, 0, 1024, true>(a, rows, st);
 }
 
 template <typename T>
@@ -322,9 +324,13 @@ cudaError_t launch_norm_t(const NormArgs &a, int rows, cudaStream_t st)
                rows_on(a.y, a.ldy) && (!a.q || (aligned(a.q, q_bytes) && a.ldq % q_bytes == 0));
     };
     const bool few = rows <= current_sms();      // a CTA per SM at most: latency counts
-    return on(16, 8) ? launch_norm_h<T, 8>(a, rows, few, st)
-         : on(2 * es, 2) ? launch_norm_h<T, 2>(a, rows, few, st)
-                         : launch_norm_h<T, 1>(a, rows, few, st);
+    auto launch = [&](auto vec) {
+        constexpr int VEC = decltype(vec)::value;
+        return few ? launch_norm_h<T, VEC, true>(a, rows, st) : launch_norm_h<T, VEC, false>(a, rows, st);
+    };
+    return on(16, 8)       ? launch(std::integral_constant<int, 8>())
+         : on(2 * es, 2) ? launch(std::integral_constant<int, 2>())
+                         : launch(std::integral_constant<int, 1>());
 }
 
 }  // namespace
