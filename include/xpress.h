@@ -466,7 +466,8 @@ int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws
  * xpress_process_logits_workspace_size bytes, 256-byte aligned, needed for
  * argmax only (else it may be NULL).
  * Errors: INVALID_ARG, UNSUPPORTED (dtype, n_seq above 65535, V above
- * 2^24, 2^31 rows or more, more than 2^30 history tokens or bias entries), WORKSPACE, CUDA. */
+ * 2^24, 2^31 rows or more, 2^30 history tokens or more, more than 2^30 bias
+ * entries), WORKSPACE, CUDA. */
 typedef struct {
     int n_seq, rows, V;
     int dtype;                       /* xpress_dtype of logits and out */

@@ -68,7 +68,7 @@ struct LogitsArgs {
 };
 
 constexpr int LT = 256;            // threads: 8 warps
-constexpr int64_t MAX_ENTRIES = 1 << 30;     // of history and bias
+constexpr int64_t MAX_ENTRIES = 1 << 30;     // of history (its counts stay below it) and bias
 constexpr int MAX_V = 1 << 24;     // so that Share's division by multiplication is exact ((V / 256) (V / 2048) < 2^32)
 constexpr int LWARPS = LT / 32;
 constexpr uint32_t IN_PROMPT = 1u << 31, IN_BLOCK = 1u << 30, TIMES = IN_BLOCK - 1;   // of a count
@@ -598,7 +598,7 @@ extern "C" int xpress_process_logits(const xpress_logits_args *in, void *ws, siz
         in->ld < in->V || (in->out && in->ldo < in->V))
         return XPRESS_ERR_INVALID_ARG;
     if ((in->dtype != XPRESS_F32 && in->dtype != XPRESS_BF16) || in->n_seq > 65535 || in->V > MAX_V ||
-        (int64_t)in->n_seq * in->rows > 0x7fffffff || in->n_history > MAX_ENTRIES || in->n_bias > MAX_ENTRIES)
+        (int64_t)in->n_seq * in->rows > 0x7fffffff || in->n_history >= MAX_ENTRIES || in->n_bias > MAX_ENTRIES)
         return XPRESS_ERR_UNSUPPORTED;
     if ((in->history && (!in->history_offsets || in->n_history < 0)) ||
         (in->bias_ids && (!in->bias_values || !in->bias_offsets || in->n_bias < 0)) ||
