@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(NT, NT > LT ? 1 : ctas_per_sm(sizeof(T) == 4, 
     __shared__ int listed;
     __shared__ uint4 masks[sizeof(T) == 2 ? 256 : 1];
     __shared__ Raw8<T> turn[VEC ? 1 : LT];
-    extern __shared__ uint32_t cnt[];              // [C]: IN_PROMPT | IN_BLOCK | times answered
+    extern __shared__ __align__(16) uint32_t cnt[];            // [C]: IN_PROMPT | IN_BLOCK | times answered
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int q = blockIdx.y, V = a.V, R = a.rows;
     const int jb = blockIdx.z * a.rows_each, je = min(jb + a.rows_each, R);     // this CTA's rows
