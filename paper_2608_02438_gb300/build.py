@@ -3,7 +3,8 @@
 Each CUDA translation unit is compiled in parallel, then linked into
 ``paper_2608_02438_gb300/_build/libxpress.so``; beside it ``xpress_torch.so``,
 the argument checks of the binding's torch calls (``csrc/torch_ext.cpp``, host
-code against torch's headers).  No GPU is needed to build.
+code against torch's headers; left out where torch is not installed).  No GPU is
+needed to build.
 """
 from __future__ import annotations
 
@@ -45,10 +46,15 @@ def _cxx() -> str:
 
 
 def _ext_flags():
-    """Compile and link flags of xpress_torch.so."""
+    """Compile and link flags of xpress_torch.so; None without torch."""
     import sysconfig
 
-    import torch
+    try:
+        import torch
+    except ModuleNotFoundError as e:
+        if e.name != "torch":
+            raise
+        return None
     t = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(nvcc()))
     inc = [os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
@@ -80,7 +86,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
             jobs.append([nvcc()] + _flags() + ["-c", s, "-o", o])
     ext_src, ext_obj = os.path.join(CSRC, "torch_ext.cpp"), os.path.join(BUILD, "torch_ext.o")
     if force or _stale([ext_obj], [ext_src, os.path.join(ROOT, "include", "xpress.h")]):
-        jobs.append([_cxx()] + _ext_flags()[0] + ["-c", ext_src, "-o", ext_obj])
+        flags = _ext_flags()
+        if flags:
+            jobs.append([_cxx()] + flags[0] + ["-c", ext_src, "-o", ext_obj])
     if jobs:
         def run(cmd):
             r = subprocess.run(cmd, capture_output=True, text=True)
@@ -97,9 +105,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if r.returncode != 0:
             raise RuntimeError("link failed:\n" + r.stdout + r.stderr)
         os.replace(tmp, LIB)
-    if force or _stale([EXT], [ext_obj, LIB]):
+    flags = _ext_flags() if force or _stale([EXT], [ext_obj, LIB]) else None
+    if flags:
         tmp = EXT + f".tmp{os.getpid()}"
-        r = subprocess.run([_cxx(), "-shared", "-o", tmp, ext_obj] + _ext_flags()[1], capture_output=True, text=True)
+        r = subprocess.run([_cxx(), "-shared", "-o", tmp, ext_obj] + flags[1], capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("link failed:\n" + r.stdout + r.stderr)
         os.replace(tmp, EXT)
