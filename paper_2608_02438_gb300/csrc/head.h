@@ -134,15 +134,31 @@ __device__ __forceinline__ uint32_t amax8(const Raw8<float> &r)
     return m;
 }
 
-// Division by a group's scale.  x / s as x times 1 / s with the remainder put
-// back, q + (x - q s) / s, which rounds as the division does (ties between
-// e4m3 values are common: inputs of few bits over a scale made of one of them)
-// at a fraction of its instructions.  An infinite scale takes no remainder:
-// finite elements become 0 and infinite ones NaN, as x / s.
+// Division by a group's scale, rounded as x / s is (ties between e4m3 values are
+// common: inputs of few bits over a scale made of one of them) at a fraction of a
+// division's instructions.  The method is Markstein's (Computation of elementary
+// functions on the IBM RISC System/6000 processor, IBM J. Res. Dev. 34, 1990): with
+// the correctly rounded inv = 1 / s and q = x inv, the remainder x - q s is exact in
+// one FMA and q + (x - q s) inv rounds as the quotient.  An infinite scale takes no
+// remainder: finite elements become 0 and infinite ones NaN, as x / s.  Where s is so
+// small that the remainder would underflow, x has to come times `up` (raise(); as a
+// factor in operator() it costs 5 % of the weights' quantisation).
 struct ScaleDiv {
     float inv, s;
-    __device__ __forceinline__ explicit ScaleDiv(float scale)
-        : inv(1.0f / scale), s(scale == INFINITY ? 0.0f : scale) {}
+    bool small;
+    static constexpr float UP = 1.84467441e19f;                     // 2^64
+    __device__ __forceinline__ explicit ScaleDiv(float scale) : small(scale < 7.88860905e-31f)   // 2^-100
+    {
+        s = small ? scale * UP : scale;
+        inv = 1.0f / s;
+        if (s == INFINITY) s = 0.0f;
+    }
+    template <int N> __device__ __forceinline__ void raise(float *x) const
+    {
+        if (__builtin_expect(small, 0))
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] *= UP;
+    }
     __device__ __forceinline__ float operator()(float x) const
     {
         const float q = x * inv;

@@ -55,6 +55,14 @@ __global__ void __launch_bounds__(QT, sizeof(T) == 2 ? 4 : 2)
     const float s = group_scale(m);
     const ScaleDiv div(s);
     if (threadIdx.x == 0) scale[blockIdx.x] = s;
+    if (div.small)
+#pragma unroll
+        for (int i = 0; i < QS; ++i) {
+            float v[8];
+            unpack(raw[i], v);
+            div.raise<8>(v);
+            pack(v, raw[i]);                       // exact
+        }
 #pragma unroll
     for (int i = 0; i < QS; ++i) {
         float v[8];

@@ -106,9 +106,9 @@ __device__ __forceinline__ void store_seg(T *row, int e0, int H, int lane, const
     }
 }
 
-// q and the scales of a segment (two groups) of y.
+// q and the scales of a segment (two groups) of y, which it may scale.
 template <int VEC>
-__device__ __forceinline__ void quant_seg(uint8_t *qrow, float *srow, int e0, int H, int lane, const float (&y)[8])
+__device__ __forceinline__ void quant_seg(uint8_t *qrow, float *srow, int e0, int H, int lane, float (&y)[8])
 {
     if (VEC == 8) {
         uint32_t m = 0;
@@ -118,6 +118,7 @@ __device__ __forceinline__ void quant_seg(uint8_t *qrow, float *srow, int e0, in
         for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
         const float s = group_scale(m);
         const ScaleDiv div(s);
+        div.raise<8>(y);
         const int e = e0 + lane * 8;
         if ((lane & 15) == 0 && e < H) srow[e / QBLOCK] = s;
         if (e + 8 <= H) store8_e4m3(qrow + e, y, div);
@@ -134,6 +135,7 @@ __device__ __forceinline__ void quant_seg(uint8_t *qrow, float *srow, int e0, in
             m = __reduce_max_sync(0xffffffffu, m);
             const float s = group_scale(m);
             const ScaleDiv div(s);
+            div.raise<4>(y + 4 * g);
             if (lane == 0 && e0 + g * QBLOCK < H) srow[e0 / QBLOCK + g] = s;
             if (VEC == 2 && e0 + SEG <= H) {
 #pragma unroll
