@@ -69,7 +69,9 @@ class Rules:
 
 class DraftHead:
     """A bf16 refiner's drafter head: the final norm's weight [H] and the LM head
-    W_lm [V, H], quantised here once (W_lm is not kept)."""
+    W_lm [V, H], quantised here once (W_lm is not kept).  The weights are quantised on
+    the refiner's stream, after what torch's current stream has done so far, and both
+    streams' next calls find them ready."""
 
     def __init__(self, refiner: X.Refiner, norm_weight: torch.Tensor, W_lm: torch.Tensor, eps: float = 1e-6):
         if refiner.dtype != X.XPRESS_BF16:
@@ -77,7 +79,10 @@ class DraftHead:
         if tuple(W_lm.shape) != (refiner.V, refiner.H):
             raise ValueError(f"W_lm: expected [{refiner.V}, {refiner.H}], got {list(W_lm.shape)}")
         self.refiner, self.norm_weight, self.eps = refiner, norm_weight, eps
-        self.w, self.w_scale = X.quantize_weight(W_lm)
+        here = torch.cuda.current_stream(W_lm.device)
+        refiner.stream.wait_stream(here)
+        self.w, self.w_scale = X.quantize_weight(W_lm, stream=refiner.stream)
+        here.wait_stream(refiner.stream)
 
     def base_logits(self, x, residual=None, rules: Rules | None = None) -> dict:
         """x [b, B, H] (the drafter's last layer, before its final norm) -> h
