@@ -31,10 +31,13 @@
 // warp % 4, 64 columns of a half tile) with the 64 sums of a thread in
 // registers: the first warpgroup hands registers to the others.
 //
-// Measured at 2048 x 38912 x 4096: 279 us, 2.3 PFLOP/s; the MMAs and their
+// Measured at 2048 x 38912 x 4096: 271 to 279 us, 2.4 PFLOP/s; the MMAs and their
 // hand-offs alone take 191 us, with the operands' copies 224, with the TMEM loads
-// 210.  What binds is the epilogue: 64 FMAs (32 packed) and 4 TMEM loads per
-// thread and K block on 16 warps.  One issuer warp took 379 us, unpacked FMAs
+// 210.  No unit is saturated (2048 x 19456 x 4096): the tensor cores work 49 % of
+// the cycles, their operands' reads take shared memory's port in as many, the
+// other accesses in 25 %, and the warps issue in 54 %; the rest is what copies,
+// MMAs and the epilogue (32 packed FMAs and 4 TMEM loads per thread and K block on
+// 16 warps) wait for one another.  One issuer warp took 379 us, unpacked FMAs
 // 321, a pair of CTAs on a 256 x 256 tile with two TMEM buffers 568 (each K block
 // waited for the other CTA's epilogue); sharing copies in clusters of 2 or 4 CTAs
 // by multicast gained nothing.

@@ -15,7 +15,7 @@
 // on 16 bytes, the pairs at 2 l, 2 l + 64, ..., or where it starts on no pair
 // either the elements l, l + 32, ... (loads of consecutive elements across the
 // warp; a group is 4 of a lane's elements).  11853 x 5202 bf16 with rows on 4
-// bytes: 159 us by elements, 110 by pairs.  Rows longer than the registers hold
+// bytes: 159 us by elements, 112 by pairs.  Rows longer than the registers hold
 // (V = 0) are read twice, the second time from L2.
 #include <type_traits>
 
