@@ -30,7 +30,7 @@
 // for one row of one request, 118 against 113 for the batch below.)
 //
 // 32 x 17 rows of 151936 bf16 (histories of 3000 to 6000, half of the rows
-// masked): 112 us, 3.0 TB/s; without rules 72 us, 4.6 TB/s.  No unit is saturated (53 %
+// masked): 112 us, 3.0 TB/s; without rules 62 us, 5.3 TB/s.  No unit is saturated (53 %
 // of the issue slots, 33 % of HBM): with two CTAs of eight warps on an SM the
 // latencies of dependent instructions show, 2.1 of the 7.2 cycles from one of a
 // warp's instructions to its next, loads 0.9 and shared memory 0.8.  The patch is about a
