@@ -40,7 +40,12 @@ extern "C" {
 typedef enum { XPRESS_F32 = 0, XPRESS_BF16 = 1 } xpress_dtype;
 
 /* sigma in Trans (Sec. 4.1 calls it "a pointwise nonlinearity"). */
-typedef enum { XPRESS_ACT_SILU = 0, XPRESS_ACT_GELU = 1, XPRESS_ACT_RELU = 2 } xpress_act;
+typedef enum {
+    XPRESS_ACT_NONE = -1,          /* xpress_linear only */
+    XPRESS_ACT_SILU = 0,
+    XPRESS_ACT_GELU = 1,
+    XPRESS_ACT_RELU = 2
+} xpress_act;
 
 typedef enum {
     XPRESS_OK = 0,
@@ -436,6 +441,37 @@ typedef struct {
 } xpress_matmul_args;
 size_t xpress_matmul_fp8_workspace_size(void);
 int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws_bytes, void *stream);
+
+/* Matrix product with bias, activation and residual (e.g. the feed-forward block
+ * in front of the drafter's head, x + W_2 act(W_1 norm(x) + b_1) + b_2):
+ *   out[m][n] = residual[m][n] + act(sum_k x[m][k] w[n][k] + bias[n])
+ * x [M, K], w [N, K] and bias [N] bf16, out and residual bf16 or fp32; fp32 sums,
+ * every step in fp32, one rounding to out's type.  act is an xpress_act
+ * (XPRESS_ACT_NONE: the identity; GELU is t Phi(t)).  bias and residual are
+ * optional (NULL).  Any M >= 0, N, K >= 1; x and w 16-byte aligned with pitches
+ * that are multiples of 8 (the padding is never used).  out may be residual's
+ * memory (same pitch).  workspace: xpress_linear_workspace_size() bytes,
+ * 256-byte aligned, zeroed once by the caller; it only holds the status word
+ * (xpress_get_device_status reads and clears it) and may be shared by calls, with
+ * xpress_matmul_fp8 too.  Reproducible: the order of every sum is fixed.
+ * Errors: INVALID_ARG, UNSUPPORTED (out_dtype, act, K above 2^24, M or N above
+ * 2^30), WORKSPACE, CUDA. */
+typedef struct {
+    int M, N, K;
+    int out_dtype;          /* xpress_dtype of out and residual */
+    int act;                /* xpress_act */
+    const void *x;          /* [M, K] bf16, pitch ldx */
+    int64_t ldx;
+    const void *w;          /* [N, K] bf16, pitch ldw */
+    int64_t ldw;
+    const void *bias;       /* [N] bf16 or NULL */
+    const void *residual;   /* [M, N], pitch ldr, or NULL */
+    int64_t ldr;
+    void *out;              /* [M, N], pitch ldo */
+    int64_t ldo;
+} xpress_linear_args;
+size_t xpress_linear_workspace_size(void);
+int xpress_linear(const xpress_linear_args *args, void *workspace, size_t ws_bytes, void *stream);
 
 /* The request's rules on logits, and the first maximum of the row that
  * results.  logits holds n_seq * rows rows of V; row j of sequence q is row

@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(HERE, "_build", "libxpress.so")
 HEADER = os.path.join(ROOT, "include", "xpress.h")
 
 XPRESS_F32, XPRESS_BF16 = 0, 1
-XPRESS_ACT_SILU, XPRESS_ACT_GELU, XPRESS_ACT_RELU = 0, 1, 2
+XPRESS_ACT_NONE, XPRESS_ACT_SILU, XPRESS_ACT_GELU, XPRESS_ACT_RELU = -1, 0, 1, 2
 XPRESS_MODE_JACOBI, XPRESS_MODE_SEQUENTIAL = 0, 1
 XPRESS_OK = 0
 XPRESS_ERR_INVALID_ARG, XPRESS_ERR_UNSUPPORTED, XPRESS_ERR_CUDA = -1, -2, -3
@@ -72,6 +72,12 @@ class XpressMatmulArgs(C.Structure):
                 ("lda", C.c_int64), ("a_scale", C.c_void_p), ("ld_a_scale", C.c_int64), ("w", C.c_void_p),
                 ("ldw", C.c_int64), ("w_scale", C.c_void_p), ("ld_w_scale", C.c_int64), ("out", C.c_void_p),
                 ("ldo", C.c_int64)]
+
+
+class XpressLinearArgs(C.Structure):
+    _fields_ = [("M", C.c_int), ("N", C.c_int), ("K", C.c_int), ("out_dtype", C.c_int), ("act", C.c_int),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ldr", C.c_int64), ("out", C.c_void_p), ("ldo", C.c_int64)]
 
 
 class XpressLogitsArgs(C.Structure):
@@ -150,6 +156,10 @@ def load(path: str = LIB_PATH):
     lib.xpress_matmul_fp8_workspace_size.restype = S
     lib.xpress_matmul_fp8.argtypes = [C.POINTER(XpressMatmulArgs), P, S, P]
     lib.xpress_matmul_fp8.restype = I
+    lib.xpress_linear_workspace_size.argtypes = []
+    lib.xpress_linear_workspace_size.restype = S
+    lib.xpress_linear.argtypes = [C.POINTER(XpressLinearArgs), P, S, P]
+    lib.xpress_linear.restype = I
     lib.xpress_process_logits_workspace_size.argtypes = [I, I, I]
     lib.xpress_process_logits_workspace_size.restype = S
     lib.xpress_process_logits.argtypes = [C.POINTER(XpressLogitsArgs), P, S, P]
@@ -382,10 +392,25 @@ def matmul_fp8(a, a_scale, w, w_scale, out, stream=None) -> int:
 
 def matmul_fp8_status(stream=None) -> int:
     """Synchronises `stream` (default: torch's current stream), then reads and
-    clears the device status of the matmul_fp8 calls so far on this device."""
+    clears the device status of the matmul_fp8 and linear calls so far on this
+    device (they share the word)."""
     import torch
     st = stream if stream is not None else torch.cuda.current_stream()
     return xpress_get_device_status((_ext or _load_ext()).matmul_fp8_workspace(), st.cuda_stream)
+
+
+def linear(x, w, out, bias=None, act: int = XPRESS_ACT_NONE, residual=None, stream=None) -> int:
+    """out [M, N] (bf16 or fp32) = residual + act(x w^T + bias) for bf16 x [M, K],
+    w [N, K], bias [N] and residual [M, N] of out's type, which may be out (see
+    xpress_linear).  x's and w's rows start on 16 bytes.  Asynchronous; returns
+    XPRESS_OK; matmul_fp8_status() reads the device status of the calls so far.
+    The first call on a device makes the status word: not inside a graph
+    capture."""
+    call, args = (_ext or _load_ext()).linear, (x, w, out, bias, act, residual)
+    code = call(*args) if stream is None else _on_stream(stream, call, args)
+    if code:
+        _check("xpress_linear", code)
+    return XPRESS_OK
 
 
 def process_logits(logits, out=None, argmax_out=None, rows: int = 1, repetition=None, frequency=None, presence=None,

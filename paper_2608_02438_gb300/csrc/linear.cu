@@ -1,0 +1,383 @@
+// linear.cu -- the bf16 matrix product with its epilogue
+//   out[m, n] = residual[m, n] + act(sum_k x[m, k] w[n, k] + bias[n])
+// for x [M, K], w [N, K] bf16, fp32 sums, one rounding to the output type.
+//
+// This kernel, for few rows of x: D = w x^T on tcgen05 (kind::f16), 128 weight rows
+// the MMA's M (TMEM lanes), NT rows of x its N, so that hardly a lane is idle and w
+// is read once.  The sums of a tile stay in TMEM over all of K; two tiles' worth of
+// columns let the next tile's products run under the epilogue of the last.
+//
+// Roles (192 threads): warp 0 TMA producer (two K blocks of 128 rows of w and of
+// NT rows of x per copy), warp 1 TMEM allocator and MMA issuer, warps 2-5 epilogue
+// (one TMEM lane quarter each, so that a warp stores 32 consecutive outputs of a
+// row).
+//
+// Where tiles are few, the CTAs of a cluster of S split K; each sends every CTA its
+// sums of that CTA's share of the rows (asynchronous stores that the receiver's
+// mbarrier counts), which adds them in rank order: the result does not depend on
+// timing.
+#include "linear.h"
+
+namespace xp {
+
+namespace {
+
+constexpr int LF_BN = 128;                             // weight rows per tile
+constexpr int LF_EPI = 4;                              // epilogue warps
+constexpr int LF_THREADS = 32 * (2 + LF_EPI);
+constexpr uint32_t LF_W = LF_BN * 128;                 // 16 KB: a K block of w
+constexpr int LF_SKB = 2;                              // K blocks of a stage
+constexpr int LF_MAX_STAGES = 6;
+
+template <int NT>
+struct FewShape {
+    static constexpr uint32_t X = NT * 128;            // a K block of x
+    static constexpr uint32_t STAGE = LF_SKB * (LF_W + X);       // w's K blocks, then x's
+    static constexpr uint32_t TMEM_COLS = 2 * NT < 32 ? 32 : 2 * NT;
+    static constexpr uint32_t IDESC = idesc_bf16(LF_BN, NT);
+    static constexpr size_t PART = (size_t)NT * LF_BN * 4;       // sums of a K split
+};
+
+struct FewBars {
+    uint64_t full[LF_MAX_STAGES], empty[LF_MAX_STAGES];
+    uint64_t tfull[2], tempty[2];
+    uint64_t drain, joined;
+    long long since;
+    uint32_t tmem_base;
+    int abort;
+};
+
+// grid: clusters of S CTAs; LF_THREADS threads; stages of STAGE bytes, then the sums
+// of a split [S][groups of vw rows of x][128][vw].
+template <int NT>
+__global__ void __launch_bounds__(LF_THREADS, NT <= 32 ? 2 : 1)
+    k_linear_few(const __grid_constant__ LinArgs g, const __grid_constant__ CUtensorMap tmap_w,
+                 const __grid_constant__ CUtensorMap tmap_x)
+{
+    using Sh = FewShape<NT>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int stages = g.stages;
+    float *part = reinterpret_cast<float *>(base + stages * Sh::STAGE);
+    __shared__ FewBars sh;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int S = g.S, rank = S > 1 ? (int)cluster_rank() : 0;
+    const int KB = (g.K + LK - 1) / LK;
+    const int KP = (KB + LF_SKB - 1) / LF_SKB;             // stages of K, split over the cluster
+    const int kb0 = (int)((int64_t)KP * rank / S) * LF_SKB, kb1 = min(KB, (int)((int64_t)KP * (rank + 1) / S) * LF_SKB);
+    const bool whole = g.K % LK == 0;                      // the maps: (64 columns, rows, K blocks), else (K, rows)
+    const int NRB = (g.N + LF_BN - 1) / LF_BN, NC = (g.M + NT - 1) / NT;
+    const int64_t items = (int64_t)NRB * NC;               // item i: weight rows 128 (i / NC), rows of x NT (i % NC)
+    const int64_t first = blockIdx.x / S, step = gridDim.x / S;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], LF_EPI); }
+        mbar_init(&sh.drain, 1);
+        mbar_init(&sh.joined, 1);
+        sh.abort = 0;
+        sh.since = 0;
+        fence_barrier_init();
+        tma_prefetch_desc(&tmap_w);
+        tma_prefetch_desc(&tmap_x);
+    }
+    if (warp == 1) { tmem_alloc(&sh.tmem_base, Sh::TMEM_COLS); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem_base;
+    volatile int *abort = &sh.abort;
+    if (S > 1) cluster_arrive();                            // waited for before the first access to another CTA
+    pdl_wait();
+
+    if (warp == 0) {
+        // ------------------------------------------------------- producer
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, pending = 0, pend_par = 0;
+            bool ok = true;
+            for (int64_t it = first; it < items && ok; it += step) {
+                const int rb = (int)(it / NC), mc = (int)(it % NC);
+                for (int kb = kb0; kb < kb1; kb += LF_SKB) {
+                    if (!mm_wait(&sh.empty[stage], phase ^ 1, abort)) { ok = false; break; }
+                    uint8_t *dw = base + stage * Sh::STAGE, *dx = dw + LF_SKB * LF_W;
+                    if (whole) {
+                        // one copy per operand; a K block past the end reads as zero
+                        mbar_expect_tx(&sh.full[stage], Sh::STAGE);
+                        tma_load_3d(dw, &tmap_w, &sh.full[stage], 0, rb * LF_BN, kb);
+                        tma_load_3d(dx, &tmap_x, &sh.full[stage], 0, mc * NT, kb);
+                    } else {
+                        const int n = min(LF_SKB, kb1 - kb);
+                        mbar_expect_tx(&sh.full[stage], n * (LF_W + Sh::X));
+                        for (int i = 0; i < n; ++i) {
+                            tma_load_2d(dw + i * LF_W, &tmap_w, &sh.full[stage], (kb + i) * 128, rb * LF_BN);
+                            tma_load_2d(dx + i * Sh::X, &tmap_x, &sh.full[stage], (kb + i) * 128, mc * NT);
+                        }
+                    }
+                    pending |= 1u << stage;
+                    pend_par = (pend_par & ~(1u << stage)) | (phase << stage);
+                    if (++stage == stages) { stage = 0; phase ^= 1; }
+                }
+            }
+            // no copy may still be landing when the CTA leaves
+            int dummy = 0;
+            for (int st = 0; st < stages; ++st)
+                if (pending & (1u << st)) mm_wait(&sh.full[st], (pend_par >> st) & 1, &dummy, MM_WAIT_CYCLES / 20);
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------- MMA issuer
+        // the whole warp runs the loop, so that the descriptors stay in uniform
+        // registers, and one elected lane issues
+        const uint32_t base_u = __shfl_sync(0xffffffffu, smem_u32(base), 0);
+        const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t lo0 = (uint32_t)smem_desc_sw128(base_u), hi = (uint32_t)(smem_desc_sw128(base_u) >> 32);
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, tphase = 0;
+        bool ok = true;
+        for (int64_t it = first; it < items && ok; it += step) {
+            ok = __all_sync(0xffffffffu, mm_wait(&sh.tempty[buf], tphase ^ 1, abort));
+            for (int kb = kb0; kb < kb1 && ok; kb += LF_SKB) {
+                ok = __all_sync(0xffffffffu, mm_wait(&sh.full[stage], phase, abort));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t w_lo = lo0 + stage * (Sh::STAGE >> 4), x_lo = w_lo + (LF_SKB * LF_W >> 4);
+                if (elect_one()) {
+                    for (int i = 0; i < LF_SKB && kb + i < kb1; ++i)
+                        tc_mma_bf16_kblock<1>(tmem_u + buf * NT, w_lo + i * (LF_W >> 4), x_lo + i * (Sh::X >> 4), hi, Sh::IDESC,
+                                              kb + i > kb0);
+                    tc_commit(&sh.empty[stage]);
+                    if (kb + LF_SKB >= kb1) tc_commit(&sh.tfull[buf]);
+                }
+                __syncwarp();
+                if (++stage == stages) { stage = 0; phase ^= 1; }
+            }
+            buf ^= 1;
+            if (buf == 0) tphase ^= 1;
+        }
+        if (elect_one()) tc_commit(&sh.drain);
+        __syncwarp();
+        int dummy = 0;
+        mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------ epilogue
+        const int q = warp & 3;
+        const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        int buf = 0;
+        uint32_t tphase = 0;
+        bool ok = true;
+        for (int64_t it = first; it < items; it += step) {
+            const int rb = (int)(it / NC), mc = (int)(it % NC), row = q * 32 + lane, n = rb * LF_BN + row;
+            const int rows = min(NT, g.M - mc * NT);
+            const float bias = S == 1 ? lin_bias(g, n) : 0.0f;
+            // the residual of the next 16 rows is asked for before the sums are waited for
+            float next[16];
+            auto fetch = [&](int j0) {
+                if (S == 1 && g.res && n < g.N)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j0 + j < rows) next[j] = lin_res(g, mc * NT + j0 + j, n);
+            };
+            fetch(0);
+            if (ok) ok = mm_wait(&sh.tfull[buf], tphase, abort, MM_WAIT_CYCLES, S > 1 ? &sh.since : nullptr);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            if (S > 1) { __syncwarp(); cluster_wait(); }            // one item per cluster (the host's grid)
+#pragma unroll 1
+            for (int j0 = 0; j0 < NT && j0 < rows; j0 += 16) {
+                float d[16], r[16];
+                if (ok) tmem_ld16(tmem + lane_base + buf * NT + j0, d);
+                else
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) d[j] = 0.0f;
+                if (S == 1) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) r[j] = next[j];
+                    fetch(j0 + 16);
+                    if (ok && n < g.N)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (j0 + j < rows) {
+                                float v = lin_act(g.act, g.bf16, d[j] + bias);
+                                if (g.res) v += r[j];
+                                lin_store(g, mc * NT + j0 + j, n, v);
+                            }
+                } else {
+                    // rows of x travel in groups of 4 (2 where a share has no more)
+                    const int share = NT / S;
+                    if (share >= 4) {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            const int jj = j0 + j;
+                            if (jj < rows)
+                                st_async4(cluster_addr(part + ((rank * share + jj % share) * LF_BN + row * 4), jj / share),
+                                          cluster_addr(&sh.joined, jj / share), d + j);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const int jj = j0 + j;
+                            if (jj < rows)
+                                st_async2(cluster_addr(part + (rank * share * LF_BN + row * 2), jj / share),
+                                          cluster_addr(&sh.joined, jj / share), d + j);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.tempty[buf]);
+            buf ^= 1;
+            if (buf == 0) tphase ^= 1;
+        }
+    }
+    if (S > 1) {
+        __syncwarp();
+        if (warp < 2) cluster_wait();
+        const int rb = (int)(first / NC), mc = (int)(first % NC), share = NT / S, vw = share >= 4 ? 4 : 2;
+        const int m0 = mc * NT + rank * share;                 // this CTA's rows of x: m0 .. m0 + rows - 1
+        const int rows = max(0, min(share, g.M - m0)), sent = (rows + vw - 1) / vw * vw;
+        if (sent > 0) {
+            if (threadIdx.x == 0) mbar_expect_tx(&sh.joined, S * sent * LF_BN * 4);
+            if (mm_wait_joined(&sh.joined, abort))
+                for (int i = threadIdx.x; i < rows * LF_BN; i += LF_THREADS) {
+                    const int j = i / LF_BN, row = i % LF_BN, n = rb * LF_BN + row;
+                    if (n >= g.N) continue;
+                    const float r = g.res ? lin_res(g, m0 + j, n) : 0.0f;
+                    float v = 0.0f;
+                    for (int s = 0; s < S; ++s) v += part[(s * share + j / vw * vw) * LF_BN + row * vw + j % vw];
+                    v = lin_act(g.act, g.bf16, v + lin_bias(g, n));
+                    lin_store(g, m0 + j, n, g.res ? v + r : v);
+                }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, Sh::TMEM_COLS);
+    }
+    if (threadIdx.x == 0 && sh.abort) set_status(g.status, ST_TIMEOUT);
+}
+
+struct LinPlan {
+    int NT, S;             // NT = 0: the kernel for many rows, S pairs of CTAs to a tile's K
+};
+
+// Clusters of S CTAs with an SM each that the current device runs at a time (0, so
+// no split, where it cannot tell).
+int resident(int S)
+{
+    static std::atomic<int> known[MAX_DEVICES][3];       // plus 1
+    static OncePerDevice once;
+    const int i = S == 2 ? 0 : S == 4 ? 1 : 2;
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    if (dev < MAX_DEVICES && (n = known[dev][i].load(std::memory_order_relaxed)) > 0) return n - 1;
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeClusterDimension;
+    a[0].val.clusterDim.x = S;
+    a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(S);
+    cfg.blockDim = dim3(LF_THREADS);
+    cfg.dynamicSmemBytes = MM_SMEM_LIMIT - 1024;
+    cfg.attrs = a;
+    cfg.numAttrs = 1;
+    if (allow_smem(once, k_linear_few<16>, MM_SMEM_LIMIT - 1024) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveClusters(&n, k_linear_few<16>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    if (dev < MAX_DEVICES) known[dev][i].store(n + 1, std::memory_order_relaxed);
+    return n;
+}
+
+LinPlan plan_linear(int M, int N, int KB, int sms)
+{
+    if (M > 128) {
+        const int64_t tiles = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
+        int S = 1;
+        for (int s = 2; s <= 4; s *= 2)
+            if (tiles <= resident(2 * s) && KB >= 16 * s) S = s;
+        return {0, S};
+    }
+    const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int64_t items = (int64_t)((N + LF_BN - 1) / LF_BN) * ((M + NT - 1) / NT);
+    int S = 1;
+    const int KP = (KB + LF_SKB - 1) / LF_SKB;
+    for (int s = 2; s <= 8 && items * s <= sms && KP >= 2 * s; s *= 2)
+        if (items <= resident(s)) S = s;
+    return {NT, S};
+}
+
+template <int NT>
+int launch_few(LinArgs g, int S, const void *x, int64_t ldx, const void *w, int64_t ldw, int sms, cudaStream_t st)
+{
+    using Sh = FewShape<NT>;
+    const int KB = (g.K + LK - 1) / LK, KP = (KB + LF_SKB - 1) / LF_SKB, want = (KP + S - 1) / S;
+    const int64_t items = (int64_t)((g.N + LF_BN - 1) / LF_BN) * ((g.M + NT - 1) / NT);
+    g.S = S;
+    // two CTAs per SM where there are many items, so that one streams while the other
+    // starts, drains or stores
+    const int per_sm = NT <= 32 && items >= 2 * sms ? 2 : 1;
+    const size_t fixed = 1024 + (S > 1 ? Sh::PART : 0) + 1024;
+    g.stages = (int)((MM_SMEM_LIMIT / per_sm - fixed) / Sh::STAGE);
+    if (g.stages > LF_MAX_STAGES) g.stages = LF_MAX_STAGES;
+    if (S > 1 && g.stages > want) g.stages = want;          // a cluster has one item
+    const size_t smem = fixed - 1024 + (size_t)g.stages * Sh::STAGE;
+    static OncePerDevice once;
+    XH_CUDA(allow_smem(once, k_linear_few<NT>, MM_SMEM_LIMIT - 1024));
+    // by K blocks only where they are whole: past the last one the rows' padding
+    // would be read
+    CUtensorMap tw{}, tx{};
+    const bool ok = g.K % LK == 0
+                        ? tmap_bytes_kblocks(&tw, w, (uint64_t)KB, (uint64_t)g.N, (uint64_t)ldw * 2, LF_BN, LF_SKB) &&
+                              tmap_bytes_kblocks(&tx, x, (uint64_t)KB, (uint64_t)g.M, (uint64_t)ldx * 2, NT, LF_SKB)
+                        : tmap_bytes(&tw, w, (uint64_t)g.K * 2, (uint64_t)g.N, (uint64_t)ldw * 2, 128, LF_BN) &&
+                              tmap_bytes(&tx, x, (uint64_t)g.K * 2, (uint64_t)g.M, (uint64_t)ldx * 2, 128, NT);
+    if (!ok) return XPRESS_ERR_CUDA;
+    const int64_t grid = S > 1 ? items * S : items < per_sm * sms ? items : per_sm * sms;
+    XH_CUDA(launch_head(k_linear_few<NT>, dim3((unsigned)grid), LF_THREADS, smem, st, (unsigned)S, g, tw, tx));
+    return XPRESS_OK;
+}
+
+}  // namespace
+}  // namespace xp
+
+using namespace xp;
+
+extern "C" size_t xpress_linear_workspace_size(void) { return 256; }
+
+extern "C" int xpress_linear(const xpress_linear_args *in, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!in || in->M < 0 || in->N < 1 || in->K < 1 || !in->x || !in->w || !in->out) return XPRESS_ERR_INVALID_ARG;
+    if ((in->out_dtype != XPRESS_F32 && in->out_dtype != XPRESS_BF16) || in->act < XPRESS_ACT_NONE || in->act > XPRESS_ACT_RELU)
+        return XPRESS_ERR_UNSUPPORTED;
+    const bool bf16 = in->out_dtype == XPRESS_BF16;
+    const uintptr_t es = bf16 ? 2 : 4;
+    if (in->ldx < in->K || in->ldw < in->K || in->ldx % 8 || in->ldw % 8 || !aligned(in->x, 16) || !aligned(in->w, 16) ||
+        in->ldo < in->N || !aligned(in->out, es) || !aligned(in->bias, 2) ||
+        (in->residual && (in->ldr < in->N || !aligned(in->residual, es))))
+        return XPRESS_ERR_INVALID_ARG;
+    if (in->K > MAX_DIM / 64 || in->M > MAX_DIM || in->N > MAX_DIM) return XPRESS_ERR_UNSUPPORTED;
+    if (!ws || !aligned(ws, 256) || ws_bytes < xpress_linear_workspace_size()) return XPRESS_ERR_WORKSPACE;
+    if (in->M == 0) return XPRESS_OK;
+    const int sms = current_sms();
+    if (sms < 1) return XPRESS_ERR_CUDA;
+    LinArgs g{};
+    g.M = in->M; g.N = in->N; g.K = in->K;
+    g.bias = static_cast<const uint16_t *>(in->bias);
+    g.res = in->residual; g.ldr = in->ldr;
+    g.out = in->out; g.ldo = in->ldo;
+    g.act = in->act;
+    g.bf16 = bf16;
+    g.vec = aligned(g.out, 16) && g.ldo * es % 16 == 0 && (!g.res || (aligned(g.res, 16) && g.ldr * es % 16 == 0));
+    g.pairs = aligned(g.out, 4 * es) && g.ldo % 4 == 0 && (!g.res || (aligned(g.res, 4 * es) && g.ldr % 4 == 0));
+    g.status = static_cast<int32_t *>(ws);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const LinPlan p = plan_linear(in->M, in->N, (in->K + LK - 1) / LK, sms);
+    if (p.NT == 16) return launch_few<16>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
+    if (p.NT == 32) return launch_few<32>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
+    if (p.NT == 64) return launch_few<64>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
+    if (p.NT == 128) return launch_few<128>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
+    g.S = p.S;
+    return launch_lin_wide(g, in->x, in->ldx, in->w, in->ldw, sms, st);
+}

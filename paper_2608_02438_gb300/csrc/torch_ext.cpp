@@ -158,7 +158,7 @@ PyObject *quantize_weight(PyObject *, PyObject *const *v, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// The zeroed workspace of matmul_fp8 on a device (its status word), made once.
+// The zeroed workspace of matmul_fp8 and linear on a device (its status word), made once.
 void *matmul_workspace(int dev)
 {
     constexpr int MAX_DEVICES = 64;
@@ -194,6 +194,33 @@ PyObject *matmul_fp8(PyObject *, PyObject *const *v, Py_ssize_t n)
     void *st = current_stream(dev);
     if (M == 0) return PyLong_FromLong(XPRESS_OK);
     return PyLong_FromLong(xpress_matmul_fp8(&g, matmul_workspace(dev), xpress_matmul_fp8_workspace_size(), st));
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, w, out, bias, act, residual)
+PyObject *linear(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count("linear", n, 6);
+    const at::Tensor &x = rank2("x", v[0]), &w = rank2("w", v[1]), &out = rank2("out", v[2]);
+    const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+    const int dev = x.get_device();
+    xpress_linear_args g{};
+    g.M = narrow("M", M);
+    g.N = narrow("N", N);
+    g.K = narrow("K", K);
+    g.out_dtype = dtype_code(out);
+    const long act = PyLong_AsLong(v[4]);
+    if (PyErr_Occurred()) return nullptr;
+    g.act = narrow("act", act);
+    g.x = matrix("x", v[0], M, K, BF16, dev, g.ldx);
+    g.w = matrix("w", v[1], N, K, BF16, dev, g.ldw);
+    g.out = matrix("out", v[2], M, N, out.scalar_type(), dev, g.ldo);
+    if (given(v[3])) g.bias = vector("bias", v[3], N, BF16, dev);
+    if (given(v[5])) g.residual = matrix("residual", v[5], M, N, out.scalar_type(), dev, g.ldr);
+    void *st = current_stream(dev);
+    if (M == 0) return PyLong_FromLong(XPRESS_OK);                    // empty tensors have no address
+    return PyLong_FromLong(xpress_linear(&g, matmul_workspace(dev), xpress_linear_workspace_size(), st));
     END_HANDLE_TH_ERRORS
 }
 
@@ -296,7 +323,7 @@ PyObject *process_logits(PyObject *, PyObject *const *v, Py_ssize_t n)
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(rmsnorm), FAST(quantize_weight), FAST(matmul_fp8), FAST(matmul_fp8_workspace),
-                         FAST(process_logits), {nullptr, nullptr, 0, nullptr}};
+                         FAST(linear), FAST(process_logits), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "xpress_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
