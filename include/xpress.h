@@ -534,6 +534,47 @@ typedef struct {
 size_t xpress_process_logits_workspace_size(int n_seq, int rows, int V);
 int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_t ws_bytes, void *stream);
 
+/* Tokens drawn from logits rows with the request's filters, from given random
+ * numbers, and the rows truncated by these filters.  logits holds n_seq * rows
+ * rows of V; row j of sequence q is row q * rows + j and takes q's parameters.  At
+ * T > 0, with m the row's maximum:
+ *   w_v   = exp((l_v - m) / T)
+ *   order = by falling l, equal ones by rising id
+ *   kept by min_p and top_k: w_v >= min_p, and among the first top_k of the order
+ *   kept by top_p: what stands before v in the order has less mass than top_p
+ *           times the mass of what min_p and top_k keep
+ *   token = the first id v at which the kept w_0 + .. + w_v exceeds u times their sum
+ * The first of the order is always kept.  A filter is off where its array is NULL
+ * or its value is top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN.  T <= 0 (or NaN)
+ * keeps the first of the order alone.  NaN and -inf logits are never kept; of a row
+ * that has +inf only these are.  A row without anything to keep gives token -1.
+ *   u       [n_seq * rows] in [0, 1) (cut to it; NaN: 0), with tokens
+ *   tokens  [n_seq * rows] int32 or NULL
+ *   out     [n_seq * rows, V], pitch ldo, or NULL: the kept logits, mask_value in all
+ *           other places; may be logits (same pitch).  For rows that go on to
+ *           xpress_accept see mask_value of xpress_process_logits.
+ * Masses are compared to about 2^-31 of the row's, in sums that do not depend on
+ * any order: calls repeat bit for bit.  No workspace; one kernel launch.
+ * Errors: INVALID_ARG (NULL logits / temperature, neither tokens nor out, tokens
+ * without u, a pitch below V, misaligned pointers), UNSUPPORTED (dtype, V above
+ * 2^24, 2^28 rows or more), CUDA. */
+typedef struct {
+    int n_seq, rows, V;
+    int dtype;                       /* xpress_dtype of logits and out */
+    const void *logits;              /* [n_seq * rows, V], pitch ld */
+    int64_t ld;
+    const float *temperature;        /* [n_seq] */
+    const int32_t *top_k;            /* [n_seq] or NULL */
+    const float *top_p;              /* [n_seq] or NULL */
+    const float *min_p;              /* [n_seq] or NULL */
+    const float *u;
+    int32_t *tokens;
+    void *out;
+    int64_t ldo;
+    float mask_value;
+} xpress_sample_args;
+int xpress_sample(const xpress_sample_args *args, void *stream);
+
 const char *xpress_status_string(int status);
 int xpress_version(void);
 

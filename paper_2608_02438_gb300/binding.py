@@ -91,6 +91,13 @@ class XpressLogitsArgs(C.Structure):
                 ("mask_value", C.c_float)]
 
 
+class XpressSampleArgs(C.Structure):
+    _fields_ = [("n_seq", C.c_int), ("rows", C.c_int), ("V", C.c_int), ("dtype", C.c_int), ("logits", C.c_void_p),
+                ("ld", C.c_int64), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p), ("u", C.c_void_p), ("tokens", C.c_void_p), ("out", C.c_void_p),
+                ("ldo", C.c_int64), ("mask_value", C.c_float)]
+
+
 _lib = None
 
 
@@ -164,6 +171,8 @@ def load(path: str = LIB_PATH):
     lib.xpress_process_logits_workspace_size.restype = S
     lib.xpress_process_logits.argtypes = [C.POINTER(XpressLogitsArgs), P, S, P]
     lib.xpress_process_logits.restype = I
+    lib.xpress_sample.argtypes = [C.POINTER(XpressSampleArgs), P]
+    lib.xpress_sample.restype = I
     _lib = lib
     return lib
 
@@ -430,6 +439,22 @@ def process_logits(logits, out=None, argmax_out=None, rows: int = 1, repetition=
     code = call(*args) if stream is None else _on_stream(stream, call, args)
     if code:
         _check("xpress_process_logits", code)
+    return XPRESS_OK
+
+
+def sample(logits, temperature, u=None, tokens_out=None, out=None, rows: int = 1, top_k=None, top_p=None, min_p=None,
+           mask_value: float = float("-inf"), stream=None) -> int:
+    """Tokens drawn from logits [n_seq * rows, V] (bf16 or fp32) into tokens_out
+    int32 [n_seq * rows] with the random numbers u fp32 [n_seq * rows] in [0, 1),
+    and / or the truncated rows into out (the same type; may be logits), under
+    each sequence's temperature fp32, top_k int32, top_p fp32 and min_p fp32
+    [n_seq] (see xpress_sample for the filters).  Asynchronous; returns
+    XPRESS_OK."""
+    call = (_ext or _load_ext()).sample
+    args = (logits, temperature, u, tokens_out, out, rows, top_k, top_p, min_p, mask_value)
+    code = call(*args) if stream is None else _on_stream(stream, call, args)
+    if code:
+        _check("xpress_sample", code)
     return XPRESS_OK
 
 

@@ -21,7 +21,7 @@ LIB = os.path.join(BUILD, "libxpress.so")
 SOURCES = ["refine_kernels.cu", "read_tc.cu", "read_tcv.cu", "refine_small.cu", "pre_tc.cu", "accept_kernels.cu", "xpress_host.cu",
            "accept_noalloc.cu", "lm_head.cu", "trans_tc.cu", "train_read.cu", "train_gemm.cu",
            "train_kernels.cu", "train_host.cu", "rmsnorm.cu", "quant_fp8.cu", "matmul_fp8.cu",
-           "matmul_fp8_wide.cu", "logits.cu", "linear.cu", "linear_wide.cu"]
+           "matmul_fp8_wide.cu", "logits.cu", "linear.cu", "linear_wide.cu", "sample.cu"]
 EXT = os.path.join(BUILD, "xpress_torch.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -1,6 +1,7 @@
-// torch_ext.cpp -- the torch side of the 8-bit drafter head's entry points: the
+// torch_ext.cpp -- the torch side of the drafter head's entry points: the
 // checks of the tensors and the argument blocks of xpress_rmsnorm,
-// xpress_quantize_weight, xpress_matmul_fp8 and xpress_process_logits.
+// xpress_quantize_weight, xpress_matmul_fp8, xpress_linear, xpress_process_logits
+// and xpress_sample.
 //
 // The calls take a few microseconds on the GPU at a decode step's sizes, and as
 // many Python operations as a dozen tensors need (shape, strides, type, device,
@@ -321,9 +322,45 @@ PyObject *process_logits(PyObject *, PyObject *const *v, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// (logits, temperature, u, tokens_out, out, rows, top_k, top_p, min_p, mask_value)
+PyObject *sample(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count("sample", n, 10);
+    const at::Tensor &x = rank2("logits", v[0]);
+    const int64_t rows = PyLong_AsLongLong(v[5]);
+    if (PyErr_Occurred()) return nullptr;
+    const int64_t total = x.size(0), V = x.size(1);
+    if (rows < 1 || total % rows) bad_value("logits: expected [n_seq * rows, V] with rows = ", rows);
+    const int64_t n_seq = total / rows;
+    const auto dt = x.scalar_type();
+    const int dev = x.get_device();
+    xpress_sample_args g{};
+    g.n_seq = narrow("n_seq", n_seq);
+    g.rows = narrow("rows", rows);
+    g.V = narrow("V", V);
+    g.dtype = dtype_code(x);
+    g.logits = matrix("logits", v[0], total, V, dt, dev, g.ld);
+    g.temperature = static_cast<float *>(vector("temperature", v[1], n_seq, F32, dev));
+    if (given(v[3])) {
+        if (!given(v[2])) bad_value("tokens_out needs u");
+        g.u = static_cast<float *>(vector("u", v[2], total, F32, dev));
+        g.tokens = static_cast<int32_t *>(vector("tokens_out", v[3], total, I32, dev));
+    }
+    if (given(v[4])) g.out = matrix("out", v[4], total, V, dt, dev, g.ldo);
+    if (given(v[6])) g.top_k = static_cast<int32_t *>(vector("top_k", v[6], n_seq, I32, dev));
+    if (given(v[7])) g.top_p = static_cast<float *>(vector("top_p", v[7], n_seq, F32, dev));
+    if (given(v[8])) g.min_p = static_cast<float *>(vector("min_p", v[8], n_seq, F32, dev));
+    g.mask_value = (float)PyFloat_AsDouble(v[9]);
+    if (PyErr_Occurred()) return nullptr;
+    void *st = current_stream(dev);
+    return PyLong_FromLong(total == 0 ? XPRESS_OK : xpress_sample(&g, st));   // empty tensors have no address
+    END_HANDLE_TH_ERRORS
+}
+
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(rmsnorm), FAST(quantize_weight), FAST(matmul_fp8), FAST(matmul_fp8_workspace),
-                         FAST(linear), FAST(process_logits), {nullptr, nullptr, 0, nullptr}};
+                         FAST(linear), FAST(process_logits), FAST(sample), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "xpress_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
