@@ -56,17 +56,18 @@ struct SampleArgs {
     const int32_t *top_k;
     int32_t *tokens;
     float mask_value;
-    int per;                       // pieces of a thread (odd)
+    int slice;                     // 16-byte pieces of a CTA
+    int per;                       // ... of a thread (odd)
     int scale;                     // a weight of 1 is 2^scale
     float slack;                   // what a sum of fast weights may be off, relative
     ExpTable table;
 };
 
-constexpr int ST = 512, SWARPS = ST / 32;
-constexpr int BINS = 2048;
+constexpr int ST = 256, SWARPS = ST / 32;
+constexpr int BINS = 4 * ST;                     // of a histogram: four to a thread
 constexpr int MAX_CLUSTER = 8;
 constexpr int ALL = 0x7fffffff;
-constexpr size_t HIST_BYTES = BINS * 12;         // counts, then masses (64 bits)
+constexpr size_t HIST_BYTES = BINS * 16;         // counts, masses, largest and smallest key
 constexpr size_t SAMPLE_SMEM = 219 * 1024, SAMPLE_HALF = 107 * 1024;      // pieces and histogram of one, of two CTAs on an SM
 
 template <typename T> struct Piece;
@@ -160,21 +161,20 @@ struct Scale {
 // series of 2^g - 1, whose fifth term is below 2^-42.
 __device__ __forceinline__ unsigned long long weight_exact(float l, const Scale &s, const unsigned long long *table)
 {
-    if (l == s.m) return 1ull << s.bits;
     const float dh = __fsub_rn(l, s.m), bb = __fsub_rn(dh, l);
     const float dl = __fadd_rn(__fsub_rn(l, __fsub_rn(dh, bb)), __fsub_rn(-s.m, bb));
-    const float ph = __fmul_rn(dh, s.kh);
-    if (!(ph > -63.0f)) return 0;
+    const float ph = fmaxf(__fmul_rn(dh, s.kh), -70.0f);            // 2^-70 is below half a unit
     const float pl = fmaf(dh, s.kh, -ph) + fmaf(dh, s.kl, dl * s.kh);
     const float steps = rintf(ph * 64.0f);
     const float g = fmaf(steps, -0.015625f, ph) + pl;
     const float e = g * fmaf(g, fmaf(g, fmaf(g, 9.61812910e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f);
-    const int i = (int)steps, down = -(i >> 6);
+    const int i = (int)steps;
     const unsigned long long t = table[i & 63];
     const unsigned long long w = t + (unsigned long long)(((long long)t * __float2int_rn(e * 4294967296.0f)) >> 32);
-    // w has 32 bits behind the point
-    const int up = s.bits - 32 - down;
-    return up >= 0 ? w << up : up > -34 ? (w + (1ull << (-up - 1))) >> -up : 0;
+    // w has 32 bits behind the point, and 2^(i >> 6) to come
+    const int up = s.bits - 32 + (i >> 6), down = min(max(-up, 1), 63);
+    const unsigned long long r = up >= 0 ? w << max(up, 0) : (w + (1ull << (down - 1))) >> down;
+    return l == s.m ? 1ull << s.bits : r;                            // (both may be infinite)
 }
 // The same with the hardware's exponential: 2^-22 off, and 2^-24 of the exponent
 // from each of three roundings (the difference, K, the product).
@@ -207,20 +207,21 @@ __device__ __forceinline__ uint4 ld_cluster4(uint32_t addr)
     asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ void ld_cluster2(uint32_t addr, unsigned long long &a, unsigned long long &b)
-{
-    asm volatile("ld.shared::cluster.v2.u64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr) : "memory");
-}
 __device__ __forceinline__ void cluster_sync() { cluster_arrive(); cluster_wait(); }
 
 struct SampleShared {
     unsigned long long table[64];                                    // 2^(j / 64)
-    unsigned long long slot[2][2][MAX_CLUSTER * SWARPS];             // what the cluster's warps exchange: [turn][value][warp]
+    unsigned long long slot[2][3][MAX_CLUSTER * SWARPS];             // what the cluster's warps exchange: [turn][value][warp]
     unsigned long long scan[2][SWARPS];
     unsigned long long note[4];                                      // written by one thread of the cluster: the id cut, a draw to repeat
-    double k, shift;                                                 // log2(e) / T and T ln(min_p)
+    double shift;                                                    // T ln(min_p)
     unsigned long long before, mass;                                 // of the bin that was looked for
-    uint32_t bin, count, above;
+    uint32_t bin, count, largest, smallest;
+};
+
+// Four bins of each thread, summed over the cluster.
+struct Bins {
+    uint32_t count[4], mass[4], largest[4], smallest[4];
 };
 
 // What a kernel's passes share.
@@ -230,15 +231,17 @@ struct Sampler {
     static constexpr int E = P::E;
     const SampleArgs &a;
     SampleShared &sh;
-    uint4 *pieces;                 // [per * ST] of this CTA (RES)
-    uint32_t *cnt;                 // [BINS]
-    unsigned long long *mass;      // [BINS]
+    uint4 *pieces;                 // [slice] of this CTA (RES)
+    uint32_t *hist;                // [4][BINS]: counts, masses, largest and smallest key
     const T *row;                  // the row's first element
     int shift;                     // elements from a 16-byte boundary to it
     int C, rank, turn;
     Scale s;
 
-    __device__ __forceinline__ int64_t position(int p) const { return ((int64_t)rank * a.per * ST + p) * E; }
+    __device__ __forceinline__ int64_t position(int p) const { return ((int64_t)rank * a.slice + p) * E; }
+    // This thread's pieces, in the order of the ids.
+    __device__ __forceinline__ int first() const { return threadIdx.x * a.per; }
+    __device__ __forceinline__ int count(int from) const { return max(0, min(a.per, a.slice - from)); }
     __device__ uint4 fetch(int p) const                              // piece p of this CTA from the row, NaNs and what is outside as -inf
     {
         const int64_t at = position(p) - shift;
@@ -253,56 +256,78 @@ struct Sampler {
         if (RES) return pieces[p];
         return fetch(p);
     }
-    // Every warp's two values to all CTAs of the cluster.
-    __device__ void exchange(unsigned long long v0, unsigned long long v1)
+    // Every warp's values to all CTAs of the cluster.
+    __device__ void exchange(unsigned long long v0, unsigned long long v1, unsigned long long v2 = 0)
     {
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
         turn ^= 1;
         if (lane < C) {
             const uint32_t to = cluster_addr(&sh.slot[turn][0][rank * SWARPS + warp], lane);
             st_cluster(to, v0);
-            st_cluster(to + sizeof(sh.slot[0][0]), v1);
+            st_cluster(to + (uint32_t)sizeof(sh.slot[0][0]), v1);
+            st_cluster(to + 2 * (uint32_t)sizeof(sh.slot[0][0]), v2);
         }
         cluster_sync();
     }
-    __device__ unsigned long long slot_of(int which, int i) const { return i < C * SWARPS ? sh.slot[turn][which][i] : 0; }
-    // The sum of what the warps exchanged.
-    __device__ unsigned long long exchanged_sum(int which) const
+    // What the warp 2 lane + i exchanged (0 past the last one).
+    __device__ __forceinline__ unsigned long long slot_of(int which, int i) const
     {
-        unsigned long long v = 0;
-#pragma unroll
-        for (int i = 0; i < MAX_CLUSTER * SWARPS / 32; ++i) v += slot_of(which, threadIdx.x % 32 + 32 * i);
-        return warp_sum(v);
+        const int w = 2 * (threadIdx.x % 32) + i;
+        return w < C * SWARPS ? sh.slot[turn][which][w] : 0;
     }
-    // Exclusive sum over the CTA's threads; total of all.
-    __device__ unsigned long long block_scan(unsigned long long v, int which, unsigned long long &total)
+    // The sum of what the warps exchanged.
+    __device__ unsigned long long exchanged_sum(int which) const { return warp_sum(slot_of(which, 0) + slot_of(which, 1)); }
+    // The smallest key above `key` (or the largest below it) of any element; ~0 (0) if there is none.
+    __device__ uint32_t next_key(uint32_t key, bool above)
+    {
+        uint32_t best = above ? ~0u : 0u;
+        for (int i = 0; i < count(first()); ++i) {
+            float v[E];
+            P::unpack(piece(first() + i), v);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const uint32_t k = order_of(v[j]) >> P::KEY_SHIFT;
+                if (above && k > key) best = min(best, k);
+                if (!above && k < key) best = max(best, k);
+            }
+        }
+        best = above ? __reduce_min_sync(0xffffffffu, best) : __reduce_max_sync(0xffffffffu, best);
+        exchange(above ? (uint32_t)~best : best, 0);
+        best = __reduce_max_sync(0xffffffffu, max((uint32_t)slot_of(0, 0), (uint32_t)slot_of(0, 1)));
+        return above ? ~best : best;
+    }
+    // Exclusive sum over the CTA's threads.
+    __device__ unsigned long long block_scan(unsigned long long v, int which)
     {
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
         const unsigned long long in = warp_scan(v);
         if (lane == 31) sh.scan[which][warp] = in;
         __syncthreads();
-        const unsigned long long w = warp_scan(lane < SWARPS ? sh.scan[which][lane] : 0ull);
-        total = __shfl_sync(0xffffffffu, w, SWARPS - 1);
-        const unsigned long long base = __shfl_sync(0xffffffffu, w, (warp + 31) % 32);
-        return (warp ? base : 0) + in - v;
+        unsigned long long base = 0;
+#pragma unroll
+        for (int i = 0; i < SWARPS; ++i) base += i < warp ? sh.scan[which][i] : 0ull;
+        return base + in - v;
     }
 
-    // Sum of the weights of l > t and number of l == t in `count` pieces from p of this CTA.
-    template <bool EXACT>
-    __device__ void sums(int p, int count, float t, unsigned long long &sum, uint32_t &ties) const
+    // Sum of the weights of l > t and number of l == t in n pieces from p of this CTA
+    // (ROW: of every element, none of which is limited by t).
+    template <bool EXACT, bool ROW>
+    __device__ void sums(int p, int n, float t, unsigned long long &sum, uint32_t &ties) const
     {
         unsigned long long fixed = 0;
         float hi = 0.0f, lo = 0.0f;
         ties = 0;
-        for (int i = 0; i < count; ++i) {
+#pragma unroll 2
+        for (int i = 0; i < n; ++i) {
             const uint4 r = piece(p + i);
-            if (EXACT && P::max_of(r) < t) continue;
+            if (!ROW && P::max_of(r) < t) continue;
             float v[E];
             P::unpack(r, v);
             if (EXACT) {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    if (v[j] > t) fixed += weight_exact(v[j], s, sh.table);
+                    const unsigned long long w = weight_exact(v[j], s, sh.table);
+                    fixed += v[j] > t ? w : 0ull;
                     ties += v[j] == t;
                 }
             } else {
@@ -310,38 +335,71 @@ struct Sampler {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     w[j] = weight_fast(v[j], s);
-                    if (!(v[j] > t)) w[j] = 0.0f;
-                    ties += v[j] == t;
+                    if (!ROW) {
+                        if (!(v[j] > t)) w[j] = 0.0f;
+                        ties += v[j] == t;
+                    }
                 }
 #pragma unroll
                 for (int o = E / 2; o > 0; o >>= 1)
 #pragma unroll
                     for (int j = 0; j < o; ++j) w[j] += w[j + o];
                 // hi + lo keeps what the addition rounds away
-                const float n = __fadd_rn(hi, w[0]), b = __fsub_rn(n, hi);
-                lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(n, b)), __fsub_rn(w[0], b));
-                hi = n;
+                const float x = __fadd_rn(hi, w[0]), b = __fsub_rn(x, hi);
+                lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(x, b)), __fsub_rn(w[0], b));
+                hi = x;
             }
         }
         const float one = __uint_as_float((uint32_t)(127 + s.bits) << 23);
         sum = EXACT ? fixed : __float2ull_rn(hi * one) + (unsigned long long)__float2ll_rn(lo * one);
     }
-
-    // Counts (and masses) of the elements from lo up whose keys are at most khi, by
-    // bins of 2^bits keys from the largest down; each thread gets four of the bins,
-    // summed over the cluster.
-    template <bool MASS>
-    __device__ void histogram(float lo, uint32_t khi, int bits, uint32_t (&c)[4], unsigned long long (&w)[4])
+    __device__ void sums(bool exact, int p, int n, float t, unsigned long long &sum, uint32_t &ties) const
     {
-        const int tid = threadIdx.x;
-        reinterpret_cast<uint4 *>(cnt)[tid] = make_uint4(0, 0, 0, 0);
-        if (MASS) {
-            reinterpret_cast<uint4 *>(mass)[tid] = make_uint4(0, 0, 0, 0);
-            reinterpret_cast<uint4 *>(mass)[tid + ST] = make_uint4(0, 0, 0, 0);
+        if (exact) sums<true, false>(p, n, t, sum, ties);
+        else if (t == -INFINITY) sums<false, true>(p, n, t, sum, ties);
+        else sums<false, false>(p, n, t, sum, ties);
+    }
+    // sums() of this thread's pieces with exact weights for t, and for a lower t0 beside it.
+    __device__ void sums_two(float t, float t0, unsigned long long &sum, uint32_t &ties, unsigned long long &sum0, uint32_t &ties0) const
+    {
+        sum = sum0 = 0;
+        ties = ties0 = 0;
+        const int n = count(first());
+        for (int i = 0; i < n; ++i) {
+            const uint4 r = piece(first() + i);
+            if (P::max_of(r) < t0) continue;
+            float v[E];
+            P::unpack(r, v);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const unsigned long long w = weight_exact(v[j], s, sh.table);
+                sum += v[j] > t ? w : 0ull;
+                sum0 += v[j] > t0 ? w : 0ull;
+                ties += v[j] == t;
+                ties0 += v[j] == t0;
+            }
+        }
+    }
+
+    // Histogram of the elements from lo up whose keys are at most khi, from the largest
+    // down, by bins of equal width 1 / inv (inv > 0) or of 2^bits keys: their number, and
+    // where a bin may have several keys (bits > 0) the largest and the smallest, and
+    // (MASS) their mass times `unit`, rounded.
+    template <bool MASS>
+    __device__ void histogram(float lo, uint32_t khi, int bits, float inv, float unit, Bins &b)
+    {
+        const int tid = threadIdx.x, n = count(first());
+        const bool keys = bits > 0;
+        reinterpret_cast<uint4 *>(hist)[tid] = make_uint4(0, 0, 0, 0);
+        if (keys) {
+            if (MASS) reinterpret_cast<uint4 *>(hist + BINS)[tid] = make_uint4(0, 0, 0, 0);
+            reinterpret_cast<uint4 *>(hist + 2 * BINS)[tid] = make_uint4(0, 0, 0, 0);
+            reinterpret_cast<uint4 *>(hist + 3 * BINS)[tid] = make_uint4(~0u, ~0u, ~0u, ~0u);
         }
         __syncthreads();
-        for (int i = 0; i < a.per; ++i) {
-            const uint4 r = piece(tid * a.per + i);
+#pragma unroll 2
+        for (int i = 0; i < n; ++i) {
+            const uint4 r = piece(first() + i);
             if (!(P::max_of(r) >= lo)) continue;
             float v[E];
             P::unpack(r, v);
@@ -350,51 +408,70 @@ struct Sampler {
                 if (v[j] >= lo) {
                     const uint32_t key = order_of(v[j]) >> P::KEY_SHIFT;
                     if (key > khi) continue;
-                    const uint32_t b = (khi - key) >> bits;            // below BINS: key is at least lo's
-                    atomicAdd(cnt + b, 1u);
-                    if (MASS) atomicAdd(mass + b, weight_exact(v[j], s, sh.table));
+                    // (below BINS also by keys: key is at least lo's)
+                    const uint32_t at = inv > 0.0f ? min((uint32_t)((s.m - v[j]) * inv), (uint32_t)BINS - 1) : (khi - key) >> bits;
+                    atomicAdd(hist + at, 1u);
+                    if (keys) {
+                        if (MASS) atomicAdd(hist + BINS + at, __float2uint_rn(weight_fast(v[j], s) * unit));
+                        atomicMax(hist + 2 * BINS + at, key);
+                        atomicMin(hist + 3 * BINS + at, key);
+                    }
                 }
         }
         cluster_sync();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { c[k] = 0; w[k] = 0; }
+        for (int k = 0; k < 4; ++k) { b.count[k] = b.mass[k] = b.largest[k] = 0; b.smallest[k] = ~0u; }
 #pragma unroll
         for (int r = 0; r < MAX_CLUSTER; ++r)
             if (r < C) {
-                const uint4 x = ld_cluster4(cluster_addr(cnt + 4 * tid, r));
-                c[0] += x.x; c[1] += x.y; c[2] += x.z; c[3] += x.w;
+                const uint4 x = ld_cluster4(cluster_addr(hist + 4 * tid, r));
+                b.count[0] += x.x; b.count[1] += x.y; b.count[2] += x.z; b.count[3] += x.w;
             }
-        if (MASS)
-#pragma unroll
-            for (int r = 0; r < MAX_CLUSTER; ++r)
-                if (r < C) {
-                    unsigned long long x[4];
-                    ld_cluster2(cluster_addr(mass + 4 * tid, r), x[0], x[1]);
-                    ld_cluster2(cluster_addr(mass + 4 * tid + 2, r), x[2], x[3]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] += x[k];
+        if (keys)
+#pragma unroll 2
+            for (int r = 0; r < C; ++r) {
+                if (MASS) {
+                    const uint4 x = ld_cluster4(cluster_addr(hist + BINS + 4 * tid, r));
+                    b.mass[0] += x.x; b.mass[1] += x.y; b.mass[2] += x.z; b.mass[3] += x.w;
                 }
+                const uint4 y = ld_cluster4(cluster_addr(hist + 2 * BINS + 4 * tid, r));
+                b.largest[0] = max(b.largest[0], y.x); b.largest[1] = max(b.largest[1], y.y);
+                b.largest[2] = max(b.largest[2], y.z); b.largest[3] = max(b.largest[3], y.w);
+                const uint4 z = ld_cluster4(cluster_addr(hist + 3 * BINS + 4 * tid, r));
+                b.smallest[0] = min(b.smallest[0], z.x); b.smallest[1] = min(b.smallest[1], z.y);
+                b.smallest[2] = min(b.smallest[2], z.z); b.smallest[3] = min(b.smallest[3], z.w);
+            }
         cluster_arrive();                          // others may read on; waited for before the bins are used again
+    }
+    // Bins of equal width from m down to lo, for the first level (0 where the width has no use).
+    __device__ __forceinline__ float bins_per(float lo) const
+    {
+        const float d = s.m - lo;
+        return d > 1e-30f && d < 1e30f ? (BINS - 0.5f) / d : 0.0f;
     }
     static __device__ __forceinline__ int level_bits(uint32_t klo, uint32_t khi)
     {
+        constexpr int LOG = 10;
+        static_assert(1 << LOG == BINS, "bins by bits of the keys");
         const int n = 32 - __clz(khi - klo);       // bits of the largest difference
-        return n > 11 ? n - 11 : 0;
+        return n > LOG ? n - LOG : 0;
     }
-    // The first of the CTA's bins (four of each thread) at which the sum of x reaches
-    // `target`; before and count as there.  False: none does.
-    __device__ bool find_bin(const unsigned long long (&x)[4], const uint32_t (&c)[4], unsigned long long target, int which)
+    // The first of the CTA's bins at which the sum of x reaches `target`; what is known
+    // of it.  False: none does.
+    __device__ bool find_bin(const unsigned long long (&x)[4], const Bins &b, unsigned long long target, int which)
     {
         const int tid = threadIdx.x;
         if (tid == 0) sh.bin = BINS;
-        unsigned long long total, at = block_scan(x[0] + x[1] + x[2] + x[3], which, total);    // its barrier comes before the writing
+        unsigned long long at = block_scan(x[0] + x[1] + x[2] + x[3], which);    // its barrier comes before the writing
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (at < target && target <= at + x[k]) {
                 sh.bin = 4 * tid + k;
                 sh.before = at;
                 sh.mass = x[k];
-                sh.count = c[k];
+                sh.count = b.count[k];
+                sh.largest = b.largest[k];
+                sh.smallest = b.smallest[k];
             }
             at += x[k];
         }
@@ -403,12 +480,19 @@ struct Sampler {
     }
 };
 
+// What a row keeps: l > t, and the first q with l == t.
+struct Kept {
+    float t;
+    int q;
+};
+
 // grid: a cluster of C CTAs for each row; ST threads; pieces, then the histogram.
 template <typename T, bool RES>
-__global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ SampleArgs a)
+__global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ SampleArgs a)
 {
     using S = Sampler<T, RES>;
     using P = Piece<T>;
+    using F = Piece<float>;
     constexpr int E = P::E, KS = P::KEY_SHIFT;
     extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ SampleShared sh;
@@ -417,11 +501,9 @@ __global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ Sample
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
     const int64_t n = blockIdx.x / C;
     const int q_seq = (int)(n / a.rows);
-    uint8_t *after = dyn + (RES ? (size_t)a.per * ST * 16 : 0);
     const T *row = static_cast<const T *>(a.in) + n * a.ld;
-    S x{a, sh, reinterpret_cast<uint4 *>(dyn), reinterpret_cast<uint32_t *>(after + BINS * 8),
-        reinterpret_cast<unsigned long long *>(after), row, (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)), (int)C,
-        (int)cluster_rank(), 0, Scale{}};
+    S x{a, sh, reinterpret_cast<uint4 *>(dyn), reinterpret_cast<uint32_t *>(dyn + (RES ? (size_t)a.slice * 16 : 0)), row,
+        (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)), (int)C, (int)cluster_rank(), 0, Scale{}};
     if (tid < 64) sh.table[tid] = a.table.v[tid];
     if (tid < 4) sh.note[tid] = ~0ull;
     cluster_arrive();                              // waited for before the first access to another CTA
@@ -430,176 +512,213 @@ __global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ Sample
     const int top_k = a.top_k ? a.top_k[q_seq] : 0;
     const float top_p = a.top_p ? a.top_p[q_seq] : 1.0f, min_p = a.min_p ? a.min_p[q_seq] : 0.0f;
     const float u = a.tokens ? fminf(fmaxf(a.u[n], 0.0f), 1.0f) : 0.0f;
-    const bool greedy = !(temp > 0.0f);
-    if (tid == 0) {
-        sh.k = 1.4426950408889634 / (double)temp;
-        sh.shift = min_p > 0.0f ? (double)temp * log(fmin((double)min_p, 1.0)) : 0.0;
-    }
 
     // ---------------------------------------------------- the row, and its maximum
     float mx = -INFINITY;
-    {
-        constexpr int UN = 4;
-        for (int j0 = 0; j0 < a.per; j0 += UN) {
-            uint4 r[UN];
-#pragma unroll
-            for (int j = 0; j < UN; ++j)
-                if (j0 + j < a.per) r[j] = x.fetch((j0 + j) * ST + tid);
-#pragma unroll
-            for (int j = 0; j < UN; ++j)
-                if (j0 + j < a.per) {
-                    mx = fmaxf(mx, P::max_of(r[j]));
-                    if (RES) x.pieces[(j0 + j) * ST + tid] = r[j];
-                }
+    const int64_t ids0 = (int64_t)x.rank * a.slice * E - x.shift;              // the id of this CTA's position 0
+    if (RES) {
+        // what lies inside the row comes by asynchronous copies, all under way at once
+        const int p0 = ids0 < 0 ? 1 : 0, p1 = (int)min((int64_t)a.slice, max((a.V - ids0) / E, (int64_t)0));
+        const uint64_t policy = policy_evict_first();
+        const int half = (a.slice / 2 + ST - 1) / ST * ST;
+        for (int p = tid; p < a.slice; p += ST) {
+            if (p >= p0 && p < p1) cp_async16(x.pieces + p, row + ids0 + (int64_t)p * E, 16, policy);
+            if (p < half && p + ST >= half) cp_async_commit();                  // (each thread has one such p, or none)
         }
+        cp_async_commit();
+        if (tid == 0) sh.shift = min_p > 0.0f ? (double)temp * log(fmin((double)min_p, 1.0)) : 0.0;
+        auto take = [&](int from, int to) {
+#pragma unroll 4
+            for (int p = from; p < to; p += ST) {
+                const bool inside = p >= p0 && p < p1;
+                const uint4 got = inside ? x.pieces[p] : make_uint4(0, 0, 0, 0), r = inside ? P::no_nan(got) : x.fetch(p);
+                if (!inside || r.x != got.x || r.y != got.y || r.z != got.z || r.w != got.w) x.pieces[p] = r;
+                mx = fmaxf(mx, P::max_of(r));
+            }
+        };
+        if (tid < half) {
+            cp_async_wait<1>();
+            take(tid, min(half, a.slice));
+        }
+        cp_async_wait<0>();
+        take(half + tid, a.slice);
+    } else {
+        if (tid == 0) sh.shift = min_p > 0.0f ? (double)temp * log(fmin((double)min_p, 1.0)) : 0.0;
+#pragma unroll 4
+        for (int p = tid; p < a.slice; p += ST) mx = fmaxf(mx, P::max_of(x.fetch(p)));
     }
     // the maxima of groups of 2^g lanes, at least top_k of them: the smallest bounds
     // the top_k-th largest element from below
-    uint32_t key = order_of(mx), group = 0;
+    uint32_t key = order_of(mx), group = ~0u, groups = 0;
     {
         int g = -1;
-        if (top_k > 0 && top_k <= (int)C * ST) g = min(5, 31 - __clz((int)C * ST / top_k));
+        if (top_k > 0) {
+            const int64_t pieces = ((int64_t)a.V + x.shift + E - 1) / E, full = pieces / a.slice;
+            const int64_t threads = full * min(ST, a.slice) + min((int64_t)ST, pieces - full * a.slice);    // that have elements
+            if (threads >= top_k) g = min(5, 31 - __clz((int)threads / top_k));
+        }
 #pragma unroll
         for (int i = 0; i <= 5; ++i) {
-            if (i == g) group = __reduce_min_sync(0xffffffffu, key);
+            if (i == g) {
+                groups = __popc(__ballot_sync(0xffffffffu, key >= LOWEST)) >> g;
+                group = __reduce_min_sync(0xffffffffu, key >= LOWEST ? key : ~0u);
+            }
             if (i < 5) key = max(key, __shfl_xor_sync(0xffffffffu, key, 1 << i));
         }
     }
     cluster_wait();
-    x.exchange(key, group);
-    uint32_t kmax = 0, kgroup = 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < MAX_CLUSTER * SWARPS / 32; ++i) {
-        const int at = lane + 32 * i;
-        if (at < (int)C * SWARPS) {
-            kmax = max(kmax, (uint32_t)sh.slot[x.turn][0][at]);
-            kgroup = min(kgroup, (uint32_t)sh.slot[x.turn][1][at]);
-        }
-    }
-    kmax = __reduce_max_sync(0xffffffffu, kmax);
-    kgroup = __reduce_min_sync(0xffffffffu, kgroup);
+    x.exchange(key, (unsigned long long)groups << 32 | (uint32_t)~group);
+    const uint32_t kmax = __reduce_max_sync(0xffffffffu, max((uint32_t)x.slot_of(0, 0), (uint32_t)x.slot_of(0, 1)));
+    uint32_t kgroup = ~__reduce_max_sync(0xffffffffu, max((uint32_t)x.slot_of(1, 0), (uint32_t)x.slot_of(1, 1)));
+    if ((int)__reduce_add_sync(0xffffffffu, (uint32_t)(x.slot_of(1, 0) >> 32) + (uint32_t)(x.slot_of(1, 1) >> 32)) < top_k) kgroup = 0;
 
-    float t = -INFINITY;                           // kept: l > t, and the first q with l == t
-    int q = 0, kept_at_most = ALL;
+    Kept kept{-INFINITY, 0};
     const bool empty = kmax < LOWEST;
+    bool k_on = false, p_on = false, check_p = false;
+    int few = ALL;                                 // at most so many are kept
+    unsigned long long z1 = 0;                     // mass of what min-p and top-k keep
+    bool z1_exact = false;
+    Kept first{-INFINITY, 0};                      // ... as a threshold
     if (!empty) {
-        const float m = Piece<float>::value(kmax);
-        const double k = fmin(fmax(sh.k, 1e-38), 3e38);
-        x.s = Scale{m, (float)k, 0.0f, a.scale};
-        x.s.kl = (float)(k - (double)x.s.kh);
+        const float m = F::value(kmax);
+        {
+            // log2(e) / T to 48 bits: the quotient's rounding comes back through the remainder
+            const float tc = fminf(fmaxf(temp, 1e-37f), 1e37f), kh = 1.44269502f / tc;
+            x.s = Scale{m, kh, (fmaf(-kh, tc, 1.44269502f) + 1.92596303e-8f) / tc, a.scale};
+        }
         const uint32_t top = kmax >> KS;
         float low = -3.402823466e38f;              // the lowest value that may be kept
         if (m == INFINITY) low = INFINITY;         // the limit: the infinities share all the mass
         else if (min_p > 0.0f) low = fmaxf(__double2float_ru((double)m + sh.shift), low);
-        if (low > -3.402823466e38f) { t = low; q = ALL; }
-        if (greedy || top_k == 1 || (top_p <= 0.0f)) {
-            t = m;
-            q = kept_at_most = 1;
+        if (low > -3.402823466e38f) kept = {low, ALL};
+        if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {
+            kept = {m, 1};
+            few = 1;
         } else {
-            bool k_on = top_k > 0 && top_k < a.V && m < INFINITY, p_on = top_p < 1.0f && m < INFINITY;
-            uint32_t c[4];
-            unsigned long long w[4], wide[4];
-            // -------------------------------------------------------- top-k
-            if (k_on) {
-                float lo = fmaxf(low, kgroup >= LOWEST ? Piece<float>::value(kgroup) : low);
-                uint32_t klo = order_of(lo) >> KS, khi = top, left = top_k;
-                for (int level = 0;; ++level) {
-                    const int bits = S::level_bits(klo, khi);
-                    x.template histogram<false>(lo, khi, bits, c, w);
+            k_on = top_k > 0 && top_k < a.V && m < INFINITY;
+            p_on = top_p < 1.0f && m < INFINITY;
+        }
+        Bins b;
+        unsigned long long wide[4];
+        // ------------------------------------------------------------ top-k
+        if (k_on) {
+            float lo = kgroup >= LOWEST ? fmaxf(low, F::value(kgroup)) : low;
+            uint32_t klo = order_of(lo) >> KS, khi = top, left = top_k;
+            for (int level = 0;; ++level) {
+                const int bits = S::level_bits(klo, khi);
+                x.template histogram<false>(lo, khi, bits, level == 0 && bits ? x.bins_per(lo) : 0.0f, 0.0f, b);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) wide[i] = c[i];
-                    const bool found = x.find_bin(wide, c, left, level & 1);
-                    cluster_wait();
-                    if (!found) { k_on = false; break; }              // fewer than k
-                    left -= (uint32_t)sh.before;
-                    khi -= sh.bin << bits;
-                    if (bits == 0) {
-                        t = P::value(khi);
-                        q = (int)left;
-                        kept_at_most = top_k;
-                        if (p_on && level == 0) {
-                            // the bins are single values: top-p from the same counts
-                            const uint32_t last = sh.bin;
+                for (int i = 0; i < 4; ++i) wide[i] = b.count[i];
+                const bool found = x.find_bin(wide, b, left, level & 1);
+                cluster_wait();
+                if (!found) break;                                    // fewer than k
+                few = top_k;
+                left -= (uint32_t)sh.before;
+                if (bits == 0) {
+                    kept = {P::value(khi - sh.bin), (int)left};
+                    if (p_on && level == 0) {
+                        // the bins are single values: top-p from the same counts
+                        const uint32_t last = sh.bin;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t b = 4 * tid + i;
-                                if (b > last) c[i] = 0;
-                                if (b == last) c[i] = left;
-                                w[i] = c[i] ? c[i] * weight_exact(P::value(top - b), x.s, sh.table) : 0;
-                            }
-                            unsigned long long z;
-                            x.block_scan(w[0] + w[1] + w[2] + w[3], 1, z);
-                            const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z), 1.0);
-                            if (x.find_bin(w, c, target, 0)) {
-                                t = P::value(top - sh.bin);
-                                q = (int)((target - sh.before + sh.mass / sh.count - 1) / (sh.mass / sh.count));
-                            }
-                            p_on = false;
-                            __syncthreads();                          // before what was found is written again
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t at = 4 * tid + i;
+                            if (at > last) b.count[i] = 0;
+                            if (at == last) b.count[i] = left;
+                            wide[i] = b.count[i] ? b.count[i] * weight_exact(P::value(top - at), x.s, sh.table) : 0;
                         }
-                        break;
+                        const unsigned long long mine = wide[0] + wide[1] + wide[2] + wide[3];
+                        const unsigned long long z = warp_sum(mine);
+                        __syncthreads();                              // what was found has been read
+                        if (lane == 0) sh.scan[1][warp] = z;
+                        __syncthreads();
+                        for (int i = 0; i < SWARPS; ++i) z1 += sh.scan[1][i];
+                        const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z1), 1.0);
+                        if (x.find_bin(wide, b, target, 0)) {
+                            const unsigned long long each = sh.mass / sh.count;
+                            kept = {P::value(top - sh.bin), (int)((target - sh.before + each - 1) / each)};
+                        }
+                        p_on = false;
                     }
-                    klo = max(klo, khi - ((1u << bits) - 1));
-                    lo = fmaxf(lo, P::value(klo));
-                    __syncthreads();
+                    break;
                 }
-            }
-            // -------------------------------------------------------- top-p
-            const float t0 = t;
-            const int q0 = q;
-            for (int attempt = kept_at_most <= 4096 * (int)C ? 1 : 0; p_on; ++attempt) {
-                unsigned long long sum;
-                uint32_t ties;
-                if (attempt) x.template sums<true>(tid * a.per, a.per, t, sum, ties);
-                else x.template sums<false>(tid * a.per, a.per, t, sum, ties);
-                x.exchange(warp_sum(sum), warp_sum(ties));
-                unsigned long long z = x.exchanged_sum(0);
-                const unsigned long long nt = min(x.exchanged_sum(1), (unsigned long long)q);
-                if (nt) z += nt * weight_exact(t, x.s, sh.table);
-                const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z), 1.0);
-                const unsigned long long slack = attempt ? 0 : (unsigned long long)((double)z * a.slack) + 64;
-                // what may be left out has at most 1 - top_p of the mass
-                float lo = fmaxf(low, t);
-                {
-                    const float share = (1.0f - top_p) * ((float)z * __uint_as_float((uint32_t)(127 - a.scale) << 23)) / (float)a.V;
-                    const float d = (logf(share) - 0.01f) * temp;
-                    lo = fmaxf(lo, m + d * (d < 0.0f ? 1.001f : 0.999f) - 1e-5f * fabsf(m));
-                    lo = fminf(lo, m);
-                }
-                uint32_t klo = order_of(lo) >> KS, khi = top;
-                unsigned long long left = target;
-                bool sure = true, found;
-                for (int level = 0;; ++level) {
-                    const int bits = S::level_bits(klo, khi);
-                    if (bits == 0) {                                  // single values: their masses from the counts
-                        x.template histogram<false>(lo, khi, bits, c, w);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            w[i] = c[i] ? c[i] * weight_exact(P::value(khi - (4 * tid + i)), x.s, sh.table) : 0;
-                    } else {
-                        x.template histogram<true>(lo, khi, bits, c, w);
-                    }
-                    found = x.find_bin(w, c, left, level & 1);
-                    cluster_wait();
-                    if (!found) { sure = false; break; }
-                    left -= sh.before;
-                    khi -= sh.bin << bits;
-                    if (bits == 0) {
-                        const unsigned long long each = sh.mass / sh.count, need = (left + each - 1) / each;
-                        sure = left > (need - 1) * each + slack && need * each >= left + slack;
-                        t = P::value(khi);
-                        q = (int)need;
-                        kept_at_most = ALL;
-                        break;
-                    }
-                    klo = max(klo, khi - ((1u << bits) - 1));
-                    lo = fmaxf(lo, P::value(klo));
-                    __syncthreads();
-                }
+                if (left == 1) { kept = {P::value(sh.largest), 1}; break; }
+                if (left == sh.count) { kept = {P::value(sh.smallest), ALL}; break; }
+                klo = sh.smallest;
+                khi = sh.largest;
+                lo = P::value(klo);
                 __syncthreads();
-                if (sure || attempt) break;
-                t = t0;                            // once more, with the exact mass
-                q = q0;
+            }
+        }
+        // ------------------------------------------------------------ top-p
+        first = kept;
+        if (p_on) {
+            unsigned long long sum;
+            uint32_t ties;
+            z1_exact = few <= 4096 * (int)C;
+            x.sums(z1_exact, x.first(), x.count(x.first()), kept.t, sum, ties);
+            x.exchange(warp_sum(sum), warp_sum(ties));
+            z1 = x.exchanged_sum(0);
+            const unsigned long long nt = min(x.exchanged_sum(1), (unsigned long long)kept.q);
+            if (nt) z1 += nt * weight_exact(kept.t, x.s, sh.table);
+            const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z1), 1.0);
+            const unsigned long long slack = z1_exact ? 0 : (unsigned long long)((double)z1 * a.slack) + 64;
+            const int down = max(0, 33 - __clzll(z1));                // z1 >> down has 31 bits
+            const float unit = __uint_as_float((uint32_t)(127 + a.scale - down) << 23);
+            // what may be left out has at most 1 - top_p of the mass
+            float lo = fmaxf(low, kept.t);
+            {
+                const float share = (1.0f - top_p) * ((float)z1 * __uint_as_float((uint32_t)(127 - a.scale) << 23)) / (float)a.V;
+                const float d = (logf(share) - 0.01f) * temp;
+                lo = fminf(fmaxf(lo, m + d * (d < 0.0f ? 1.001f : 0.999f) - 1e-5f * fabsf(m)), m);
+            }
+            uint32_t klo = order_of(lo) >> KS, khi = top;
+            unsigned long long left = 0;
+            bool sure = true;                                         // no bin was taken by rounded masses
+            for (int level = 0;; ++level) {
+                const int bits = S::level_bits(klo, khi);
+                x.template histogram<true>(lo, khi, bits, level == 0 && bits ? x.bins_per(lo) : 0.0f, unit, b);
+                if (level == 0) left = bits ? target >> down : target;
+                bool found;
+                if (bits == 0) {
+                    // single values: their masses from the counts
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        wide[i] = b.count[i] ? b.count[i] * weight_exact(P::value(khi - (4 * tid + i)), x.s, sh.table) : 0;
+                    found = x.find_bin(wide, b, sure ? left : max(left, 1ull) << down, level & 1);
+                } else {
+                    sure = false;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wide[i] = b.mass[i];
+                    found = x.find_bin(wide, b, max(left, 1ull), level & 1);
+                }
+                cluster_wait();
+                if (!found) {
+                    // by rounding: the smallest that was counted, or what the bound left out
+                    check_p = true;
+                    kept.t = P::value(klo);
+                    break;
+                }
+                left -= min(left, sh.before);
+                if (bits == 0) {
+                    kept.t = P::value(khi - sh.bin);
+                    if (sure) {
+                        const unsigned long long each = sh.mass / sh.count, need = (left + each - 1) / each;
+                        kept.q = (int)need;
+                        check_p = !(left > (need - 1) * each + slack && need * each >= left + slack);
+                    } else {
+                        check_p = true;
+                    }
+                    break;
+                }
+                check_p = true;
+                // one of two, or the largest of several, by its mass
+                const uint32_t big = sh.largest, small = sh.smallest;
+                const bool take = left <= (weight_exact(P::value(big), x.s, sh.table) >> down);
+                if (take || sh.count <= 2) { kept.t = P::value(take ? big : small); break; }
+                klo = small;
+                khi = big;
+                lo = P::value(klo);
+                __syncthreads();
             }
         }
     }
@@ -608,60 +727,88 @@ __global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ Sample
     int cut = ALL;                                 // the last id with l == t that is kept
     if (empty) {
         if (tid == 0 && x.rank == 0 && a.tokens) a.tokens[n] = -1;
-        t = INFINITY;
-        q = 0;
-    } else if (a.tokens || (a.out && q < ALL)) {
-        const unsigned long long wt = q ? weight_exact(t, x.s, sh.table) : 0;
-        for (int attempt = kept_at_most <= 4096 * (int)C ? 1 : 0;; ++attempt) {
+        kept = {INFINITY, 0};
+    } else if (a.tokens || check_p || (a.out && kept.q < ALL && kept.q > 0)) {
+        // a check that the fast weights could hardly decide starts with exact ones
+        bool exact = few <= 4096 * (int)C || (check_p && (double)weight_exact(kept.t, x.s, sh.table) < 20.0 * a.slack * (double)z1);
+        // while t is not sure: what is known of its key, from below and above
+        uint32_t known_lo = max(order_of(first.t), LOWEST) >> KS, known_hi = kmax >> KS;
+        int moves = 0;
+        for (;;) {
+            const float t = kept.t;
             unsigned long long sum;
             uint32_t ties;
-            if (attempt) x.template sums<true>(tid * a.per, a.per, t, sum, ties);
-            else x.template sums<false>(tid * a.per, a.per, t, sum, ties);
-            x.exchange(warp_sum(sum), warp_sum(ties));
-            // each lane takes four consecutive warps: their ties, then their kept mass
-            unsigned long long wm[4];
-            uint32_t wn[4], n4 = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) n4 += wn[i] = (uint32_t)x.slot_of(1, 4 * lane + i);
-            const uint32_t n_in = warp_scan(n4), n_ex = n_in - n4;
-            uint32_t at_n = n_ex;
-            unsigned long long m4 = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t b = min(at_n, (uint32_t)q), e = min(at_n + wn[i], (uint32_t)q);
-                m4 += wm[i] = x.slot_of(0, 4 * lane + i) + (e - b) * wt;
-                at_n += wn[i];
+            if (check_p && exact && !z1_exact) {
+                unsigned long long sum0;
+                uint32_t ties0;
+                x.sums_two(t, first.t, sum, ties, sum0, ties0);
+                x.exchange(warp_sum(sum), warp_sum((unsigned long long)ties0 << 32 | ties), warp_sum(sum0));
+                z1 = x.exchanged_sum(2);
+                const unsigned long long nt = min(x.exchanged_sum(1) >> 32, (unsigned long long)first.q);
+                if (nt) z1 += nt * weight_exact(first.t, x.s, sh.table);
+                z1_exact = true;
+            } else {
+                x.sums(exact, x.first(), x.count(x.first()), t, sum, ties);
+                x.exchange(warp_sum(sum), warp_sum(ties));
             }
-            const unsigned long long m_in = warp_scan(m4);
-            const unsigned long long z = __shfl_sync(0xffffffffu, m_in, 31);
+            // each lane takes two consecutive warps: their ties, then their kept mass
+            const uint32_t wn0 = (uint32_t)x.slot_of(1, 0), wn1 = (uint32_t)x.slot_of(1, 1);
+            const unsigned long long ws0 = x.slot_of(0, 0), ws1 = x.slot_of(0, 1);
+            const uint32_t n_in = warp_scan(wn0 + wn1), n0 = n_in - wn0 - wn1, n1 = n_in - wn1;
             const uint32_t all_ties = __shfl_sync(0xffffffffu, n_in, 31);
-            const bool cuts = q && (uint32_t)q < all_ties;
-            if (cuts && a.out && attempt <= 1) {
-                // the q-th of the ties
-                int who = 4 * MAX_CLUSTER * SWARPS;
-                uint32_t base = n_ex, there = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (base < (uint32_t)q && (uint32_t)q <= base + wn[i]) { who = 4 * lane + i; there = base; }
-                    base += wn[i];
+            const unsigned long long wt = all_ties ? weight_exact(t, x.s, sh.table) : 0;
+            if (check_p) {
+                // is t where the mass before reaches the target?  How many of its ties?
+                const unsigned long long above = warp_sum(ws0 + ws1);
+                const uint32_t may = t == first.t ? min(all_ties, (uint32_t)first.q) : all_ties;
+                const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z1), 1.0);
+                const unsigned long long slack = (exact ? 0 : (unsigned long long)((double)above * a.slack) + 64) +
+                                                 (z1_exact ? 0 : (unsigned long long)((double)z1 * a.slack) + 64);
+                const bool small = above >= target + slack, large = above + may * wt + slack < target && t > first.t;
+                if ((small || large) && moves < 40) {                 // 33 halve any range of keys to one
+                    // the next value first (rounded masses put t off by one), then the middle
+                    const uint32_t at = order_of(t) >> KS;
+                    if (small) known_lo = max(known_lo, at + 1);
+                    else known_hi = min(known_hi, at - 1);
+                    uint32_t to = known_lo + (known_hi - known_lo) / 2;
+                    if (moves++ == 0) to = min(max(x.next_key(at, small), known_lo), known_hi);
+                    kept.t = P::value(to);
+                    continue;
                 }
-                const unsigned found = __ballot_sync(0xffffffffu, who < MAX_CLUSTER * SWARPS);
-                const int src = __ffs(found) - 1;
-                who = __shfl_sync(0xffffffffu, who, src);
-                there = __shfl_sync(0xffffffffu, there, src);
-                if (who == x.rank * SWARPS + warp) {
+                const unsigned long long over = target > above ? target - above : 1;
+                const unsigned long long need = wt ? min((over + wt - 1) / wt, (unsigned long long)max(may, 1u)) : 1;
+                const bool sure = target > above + (need - 1) * wt + slack && (above + need * wt >= target + slack);
+                if (!sure && !(exact && z1_exact)) {
+                    exact = true;                                     // once more, with exact masses
+                    continue;
+                }
+                kept.q = (int)need;
+                check_p = false;
+            }
+            const uint32_t q = (uint32_t)kept.q;
+            const unsigned long long wm0 = ws0 + (min(n0 + wn0, q) - min(n0, q)) * wt, wm1 = ws1 + (min(n1 + wn1, q) - min(n1, q)) * wt;
+            const unsigned long long m_in = warp_scan(wm0 + wm1);
+            const unsigned long long z = __shfl_sync(0xffffffffu, m_in, 31);
+            const bool cuts = a.out && q && q < all_ties;
+            const int me = x.rank * SWARPS + warp;
+            if (cuts) {
+                // the q-th of the ties
+                const unsigned f0 = __ballot_sync(0xffffffffu, n0 < q && q <= n0 + wn0), f1 = __ballot_sync(0xffffffffu, n1 < q && q <= n1 + wn1);
+                const int who = f0 ? 2 * (__ffs(f0) - 1) : 2 * (__ffs(f1) - 1) + 1;
+                if (who == me) {
+                    const uint32_t there = __shfl_sync(0xffffffffu, f0 ? n0 : n1, who / 2);
                     const uint32_t in = warp_scan(ties);
                     uint32_t seen = there + in - ties;
-                    if (seen < (uint32_t)q && (uint32_t)q <= seen + ties) {
-                        for (int i = 0; i < a.per; ++i) {
+                    if (seen < q && q <= seen + ties) {
+                        for (int i = 0; i < x.count(x.first()); ++i) {
                             float v[E];
-                            P::unpack(x.piece(tid * a.per + i), v);
+                            P::unpack(x.piece(x.first() + i), v);
 #pragma unroll
                             for (int j = 0; j < E; ++j)
-                                if (v[j] == t && ++seen == (uint32_t)q)
+                                if (v[j] == t && ++seen == q)
                                     for (int r = 0; r < (int)C; ++r)
                                         st_cluster(cluster_addr(&sh.note[0], r),
-                                                   (unsigned long long)(x.position(tid * a.per + i) + j - x.shift));
+                                                   (unsigned long long)(x.position(x.first() + i) + j - x.shift));
                         }
                     }
                 }
@@ -669,87 +816,71 @@ __global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ Sample
             if (a.tokens) {
                 unsigned long long goal = (unsigned long long)((double)u * (double)z);
                 if (goal >= z) goal = z - 1;
-                const unsigned long long slack = attempt ? 0 : (unsigned long long)((double)z * a.slack) + 64;
-                int who = MAX_CLUSTER * SWARPS;
-                unsigned long long base = m_in - m4, there = 0;
-                uint32_t base_n = n_ex, there_n = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (base <= goal && goal < base + wm[i]) { who = 4 * lane + i; there = base; there_n = base_n; }
-                    base += wm[i];
-                    base_n += wn[i];
-                }
-                const unsigned found = __ballot_sync(0xffffffffu, who < MAX_CLUSTER * SWARPS);
-                const int src = __ffs(found) - 1;
-                who = __shfl_sync(0xffffffffu, who, src);
-                there = __shfl_sync(0xffffffffu, there, src);
-                there_n = __shfl_sync(0xffffffffu, there_n, src);
-                if (who == x.rank * SWARPS + warp) {
+                const unsigned long long slack = exact ? 0 : (unsigned long long)((double)z * a.slack) + 64;
+                const unsigned long long m0 = m_in - wm0 - wm1, m1 = m_in - wm1;
+                const unsigned f0 = __ballot_sync(0xffffffffu, m0 <= goal && goal < m0 + wm0), f1 = __ballot_sync(0xffffffffu, m1 <= goal && goal < m1 + wm1);
+                const int who = f0 ? 2 * (__ffs(f0) - 1) : 2 * (__ffs(f1) - 1) + 1;
+                if (who == me) {
                     // the lane, then the piece, then the element
-                    int token = -1;
-                    bool sure = true;
-                    unsigned long long mine = sum;
-                    uint32_t my_ties = ties;
-                    int p = tid * a.per, count = a.per;
+                    unsigned long long there = __shfl_sync(0xffffffffu, f0 ? m0 : m1, who / 2), mine = sum;
+                    uint32_t there_n = __shfl_sync(0xffffffffu, f0 ? n0 : n1, who / 2), my_ties = ties;
+                    int p = 0;
                     bool ok = true;
-                    for (int step = 0; step < 2 && ok; ++step) {
+                    for (int step = 0; step < 3 && ok; ++step) {
                         for (int p0 = 0;; p0 += 32) {
-                            // step 0: the lanes' own ranges; step 1: 32 pieces of the range found
+                            // step 0: the lanes' own ranges; 1: 32 pieces of the range found; 2: the elements of the piece found
                             if (step == 1) {
                                 mine = 0;
                                 my_ties = 0;
-                                if (p0 + lane < count) {
-                                    if (attempt) x.template sums<true>(p + p0 + lane, 1, t, mine, my_ties);
-                                    else x.template sums<false>(p + p0 + lane, 1, t, mine, my_ties);
+                                if (p0 + lane < x.count(p)) x.sums(exact, p + p0 + lane, 1, t, mine, my_ties);
+                            }
+                            if (step == 2) {
+                                mine = 0;
+                                my_ties = 0;
+                                if (lane < E) {
+                                    float v[E];
+                                    P::unpack(x.piece(p), v);
+                                    float l = v[0];
+#pragma unroll
+                                    for (int j = 1; j < E; ++j) l = lane == j ? v[j] : l;
+                                    if (l > t) mine = weight_exact(l, x.s, sh.table);
+                                    my_ties = l == t;
                                 }
                             }
                             const uint32_t in_n = warp_scan(my_ties), ex_n = there_n + in_n - my_ties;
-                            const uint32_t b = min(ex_n, (uint32_t)q), e = min(ex_n + my_ties, (uint32_t)q);
-                            const unsigned long long kept = mine + (e - b) * wt;
-                            const unsigned long long in_m = warp_scan(kept), ex_m = there + in_m - kept;
-                            const unsigned hit = __ballot_sync(0xffffffffu, ex_m <= goal && goal < ex_m + kept);
+                            const unsigned long long own = mine + (min(ex_n + my_ties, q) - min(ex_n, q)) * wt;
+                            const unsigned long long in_m = warp_scan(own), ex_m = there + in_m - own;
+                            const unsigned hit = __ballot_sync(0xffffffffu, ex_m <= goal && goal < ex_m + own);
                             if (hit) {
                                 const int l = __ffs(hit) - 1;
-                                there = __shfl_sync(0xffffffffu, ex_m, l);
-                                there_n = __shfl_sync(0xffffffffu, ex_n, l);
-                                p = step == 0 ? __shfl_sync(0xffffffffu, p, l) : p + p0 + l;
+                                if (step == 2) {
+                                    const bool sure = ex_m + slack <= goal && goal + slack < ex_m + own;
+                                    if (lane == l) {
+                                        a.tokens[n] = (int)(x.position(p) + l - x.shift);
+                                        if (!exact && !sure)
+                                            for (int r = 0; r < (int)C; ++r) st_cluster(cluster_addr(&sh.note[1], r), 1ull);
+                                    }
+                                    p = -1;
+                                } else {
+                                    there = __shfl_sync(0xffffffffu, ex_m, l);
+                                    there_n = __shfl_sync(0xffffffffu, ex_n, l);
+                                    p = step == 0 ? (warp * 32 + l) * a.per : p + p0 + l;
+                                }
                                 break;
                             }
                             there += __shfl_sync(0xffffffffu, in_m, 31);
                             there_n += __shfl_sync(0xffffffffu, in_n, 31);
-                            if (step == 0 || p0 + 32 >= count) { ok = false; break; }
+                            if (step != 1 || p0 + 32 >= x.count(p)) { ok = false; break; }
                         }
                     }
-                    if (ok) {
-                        float v[E];
-                        P::unpack(x.piece(p), v);
-                        unsigned long long at = there;
-                        uint32_t at_tie = there_n;
-                        sure = false;
-#pragma unroll
-                        for (int j = 0; j < E; ++j) {
-                            unsigned long long w = 0;
-                            if (v[j] > t) w = weight_exact(v[j], x.s, sh.table);
-                            else if (v[j] == t) { if (at_tie < (uint32_t)q) w = wt; ++at_tie; }
-                            if (token < 0 && goal < at + w) {
-                                token = (int)(x.position(p) + j - x.shift);
-                                sure = attempt || (goal >= at + slack && goal + slack < at + w);
-                            }
-                            at += w;
-                        }
-                    }
-                    if (token < 0) sure = false;
-                    if (lane == 0) {
-                        if (token >= 0) a.tokens[n] = token;
-                        if (!sure && !attempt)
-                            for (int r = 0; r < (int)C; ++r) st_cluster(cluster_addr(&sh.note[1], r), 1ull);
-                    }
+                    if (!exact && p >= 0 && lane < (int)C) st_cluster(cluster_addr(&sh.note[1], lane), 1ull);   // lost in rounding
                 }
             }
-            if (attempt && !(cuts && a.out)) break;
+            if (exact && !cuts) break;
             cluster_sync();
-            if (cuts && a.out) cut = (int)sh.note[0];
-            if (attempt || sh.note[1] != 1ull) break;
+            if (cuts) cut = (int)sh.note[0];
+            if (exact || sh.note[1] != 1ull) break;
+            exact = true;
         }
     }
 
@@ -759,18 +890,20 @@ __global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ Sample
         T *out = static_cast<T *>(a.out) + n * a.ldo;
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
         const T dropped = P::raw(a.mask_value);
-        for (int i = 0; i < a.per; ++i) {
-            const int p = i * ST + tid;
+#pragma unroll 2
+        for (int p = tid; p < a.slice; p += ST) {
             const int64_t at = x.position(p) - x.shift;
-            if (at <= -E || at >= a.V) continue;
+            if (at >= a.V) break;
             const uint4 r = x.piece(p);
-            float v[E];
-            P::unpack(r, v);
             T e[E];
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const bool keep = v[j] > t || (v[j] == t && q && at + j <= cut);
-                e[j] = keep ? P::raw(v[j]) : dropped;
+            for (int j = 0; j < E; ++j) e[j] = dropped;
+            if (P::max_of(r) >= kept.t) {
+                float v[E];
+                P::unpack(r, v);
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (v[j] > kept.t || (v[j] == kept.t && kept.q && at + j <= cut)) e[j] = P::raw(v[j]);
             }
             if (same && at >= 0 && at + E <= a.V) {
                 *reinterpret_cast<uint4 *>(out + at) = P::pack_raw(e);
@@ -784,23 +917,21 @@ __global__ void __launch_bounds__(ST, 2) k_sample(const __grid_constant__ Sample
 }
 
 struct SamplePlan {
-    int C, per;
+    int C, slice, per;
     bool resident;
 };
 
-// CTAs of a row's cluster and pieces of a thread: the fewest CTAs that leave two on
-// an SM, more while SMs would be idle.
+// CTAs of a row's cluster: the fewest that leave two on an SM, more while SMs would be
+// idle; the pieces of a CTA and of a thread.
 SamplePlan sample_plan(int64_t n, int V, int E, int sms)
 {
-    auto per_of = [&](int C) {
-        const int64_t pieces = ((int64_t)V + E - 1 + E - 1) / E;
-        const int64_t per = (pieces + (int64_t)C * ST - 1) / ((int64_t)C * ST);
-        return (int)(per | 1);
-    };
-    auto bytes = [&](int C) { return (size_t)per_of(C) * ST * 16 + HIST_BYTES; };
+    const int64_t pieces = ((int64_t)V + E - 1 + E - 1) / E;          // wherever the row starts
+    auto slice_of = [&](int C) { return (pieces + C - 1) / C; };
+    auto bytes = [&](int C) { return (size_t)slice_of(C) * 16 + HIST_BYTES; };
     int C = 1;
-    while (C < MAX_CLUSTER && (bytes(C) > SAMPLE_HALF || (n * C * 2 <= sms && per_of(C) > 1))) C *= 2;
-    return {C, per_of(C), bytes(C) <= SAMPLE_SMEM};
+    while (C < MAX_CLUSTER && (bytes(C) > SAMPLE_HALF || (n * C < 2 * sms && slice_of(C) > 2 * ST))) C *= 2;
+    const int slice = (int)slice_of(C);
+    return {C, slice, ((slice + ST - 1) / ST) | 1, bytes(C) <= SAMPLE_SMEM};
 }
 
 template <typename T, bool RES>
@@ -808,7 +939,7 @@ int launch_sample(const SampleArgs &a, int64_t n, int C, cudaStream_t st)
 {
     static OncePerDevice once;
     XH_CUDA(allow_smem(once, k_sample<T, RES>, SAMPLE_SMEM));
-    const size_t smem = (RES ? (size_t)a.per * ST * 16 : 0) + HIST_BYTES;
+    const size_t smem = (RES ? (size_t)a.slice * 16 : 0) + HIST_BYTES;
     XH_CUDA(launch_head(k_sample<T, RES>, dim3((unsigned)(n * C)), ST, smem, st, (unsigned)C, a));
     return XPRESS_OK;
 }
@@ -851,6 +982,7 @@ extern "C" int xpress_sample(const xpress_sample_args *in, void *stream)
     // below log2 V + 5: an element at -x has at most 2^-x of it), the sums
     a.slack = 1.1f * (1.0f / (1 << 21) + 3.0f * 0.6932f * (log2v + 5) / (1 << 24));
     const SamplePlan p = sample_plan(n, in->V, (int)(16 / es), sms);
+    a.slice = p.slice;
     a.per = p.per;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (in->dtype == XPRESS_BF16)
