@@ -59,16 +59,15 @@ struct SampleArgs {
     int slice;                     // 16-byte pieces of a CTA
     int per;                       // ... of a thread (odd)
     int scale;                     // a weight of 1 is 2^scale
-    float slack;                   // what a sum of fast weights may be off, relative
     ExpTable table;
 };
 
-constexpr int ST = 256, SWARPS = ST / 32;
-constexpr int BINS = 4 * ST;                     // of a histogram: four to a thread
+constexpr int BINS = 1024;                       // of a histogram
+constexpr int FEW = BINS;                        // elements that are sorted: as many to a thread as bins
 constexpr int MAX_CLUSTER = 8;
 constexpr int ALL = 0x7fffffff;
-constexpr size_t HIST_BYTES = BINS * 16;         // counts, masses, largest and smallest key
-constexpr size_t SAMPLE_SMEM = 219 * 1024, SAMPLE_HALF = 107 * 1024;      // pieces and histogram of one, of two CTAs on an SM
+constexpr size_t HIST_BYTES = BINS * 16 + FEW * 8;        // counts, masses, largest and smallest key; a CTA's part of the few
+constexpr size_t SAMPLE_SMEM = 219 * 1024, SAMPLE_HALF = 105 * 1024;      // pieces and histogram of one, of two CTAs on an SM
 
 template <typename T> struct Piece;
 template <> struct Piece<uint16_t> {
@@ -153,7 +152,23 @@ constexpr uint32_t LOWEST = 0x00800000u;         // of the lowest finite value
 struct Scale {
     float m, kh, kl;
     int bits;                                    // a weight of 1 is 2^bits
+    float floor;                                 // below it weights are under 2^-120
+    float rest;                                  // K m's fraction
+    uint32_t back;                               // K m's integer, negative, at a float's exponent
+    bool near;                                   // K m is small enough for weight_fast's exponents
 };
+constexpr float MAGIC = 12582912.0f;             // 1.5 2^23: added and taken away, it rounds to an integer
+
+__device__ __forceinline__ Scale make_scale(float m, float T, int bits)
+{
+    // log2(e) / T to 48 bits: the quotient's rounding comes back through the remainder
+    const float t = fminf(fmaxf(T, 1e-37f), 1e37f), kh = 1.44269502f / t;
+    const float kl = (fmaf(-kh, t, 1.44269502f) + 1.92596303e-8f) / t;
+    const float ph = __fmul_rn(m, kh), pl = fmaf(m, kl, fmaf(m, kh, -ph)), i = __fadd_rn(ph, MAGIC);
+    const float reach = 120.0f / kh;
+    return Scale{m, kh, kl, bits, m - reach, __fsub_rn(ph, __fsub_rn(i, MAGIC)) + pl, 0u - (__float_as_uint(i) << 23),
+                 fabsf(ph) < 5e5f && reach < 1e30f};
+}
 
 // w = 2^(K (l - m)) as a 64-bit fixed-point number, to 2^-31 of its value (and half a
 // unit).  The difference and its product with K are kept in two parts; of the
@@ -176,9 +191,23 @@ __device__ __forceinline__ unsigned long long weight_exact(float l, const Scale 
     const unsigned long long r = up >= 0 ? w << max(up, 0) : (w + (1ull << (down - 1))) >> down;
     return l == s.m ? 1ull << s.bits : r;                            // (both may be infinite)
 }
-// The same with the hardware's exponential: 2^-22 off, and 2^-24 of the exponent
-// from each of three roundings (the difference, K, the product).
-__device__ __forceinline__ float weight_fast(float l, const Scale &s) { return ex2_approx(fminf(l - s.m, 0.0f) * s.kh); }
+// The same with the hardware's exponential of the exponent's fraction: 2^-22 off, and
+// 2^-24 from the fraction's roundings (K l is split into an integer, its fraction and
+// the product's remainder).
+__device__ __forceinline__ float weight_fast(float l, const Scale &s)
+{
+    if (!s.near) return ex2_approx(fminf(l - s.m, 0.0f) * s.kh);     // (a guess: such rows are summed exactly)
+    l = fmaxf(l, s.floor);
+    const float ph = __fmul_rn(l, s.kh), i = __fadd_rn(ph, MAGIC);
+    const float f = __fsub_rn(ph, __fsub_rn(i, MAGIC)) + (fmaf(l, s.kh, -ph) + fmaf(l, s.kl, -s.rest));
+    return __uint_as_float(__float_as_uint(ex2_approx(f)) + (__float_as_uint(i) << 23) + s.back);
+}
+// What fast weights may be off, and a sum of them by its own roundings (three levels
+// of 2^-24 each), in 2^-26 of their size, a tenth added; and by fixed-point roundings.
+constexpr float SLACK_W = 24.0f, SLACK_SUM = 14.0f, SLACK = SLACK_W + SLACK_SUM;
+constexpr unsigned long long SLACK_UNITS = 8192;
+// 2^-26 of z, as a float.
+__device__ __forceinline__ float part_of(unsigned long long z) { return (float)(uint32_t)(z >> 32) * 64.0f; }
 
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v)
 {
@@ -201,41 +230,72 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, unsigned long long v)
 {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
-__device__ __forceinline__ uint4 ld_cluster4(uint32_t addr)
+__device__ __forceinline__ void ld_cluster(uint32_t addr, uint32_t (&v)[4])
 {
-    uint4 v;
-    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ld_cluster(uint32_t addr, uint32_t (&v)[2])
+{
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t ld_cluster1(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ void cluster_sync() { cluster_arrive(); cluster_wait(); }
 
-struct SampleShared {
+template <int SWARPS> struct SampleShared {
     unsigned long long table[64];                                    // 2^(j / 64)
     unsigned long long slot[2][3][MAX_CLUSTER * SWARPS];             // what the cluster's warps exchange: [turn][value][warp]
     unsigned long long scan[2][SWARPS];
     unsigned long long note[4];                                      // written by one thread of the cluster: the id cut, a draw to repeat
-    double shift;                                                    // T ln(min_p)
+    float shift_hi, shift_lo;                                        // T ln(min_p)
     unsigned long long before, mass;                                 // of the bin that was looked for
     uint32_t bin, count, largest, smallest;
+    int base[MAX_CLUSTER + 1];                                       // where the CTAs' parts of the few begin
 };
 
-// Four bins of each thread, summed over the cluster.
-struct Bins {
-    uint32_t count[4], mass[4], largest[4], smallest[4];
-};
+// z f, rounded down, and whether anything was lost; 0 <= f < 1.
+__device__ __forceinline__ unsigned long long scaled(unsigned long long z, float f, bool &more)
+{
+    const uint32_t bits = __float_as_uint(f), e = bits >> 23;
+    const unsigned long long mant = e ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
+    const int s = 150 - (int)max(e, 1u);                             // f = mant 2^-s, s >= 24
+    const unsigned long long hi = __umul64hi(z, mant), lo = z * mant;
+    if (s < 64) {
+        more = lo << (64 - s) != 0;
+        return hi << (64 - s) | lo >> s;
+    }
+    const int t = min(s - 64, 63);
+    more = lo != 0 || (hi & ((1ull << t) - 1)) != 0;
+    return hi >> t;
+}
+// The mass that top-p's kept tokens have to reach: at least one unit, so that one is kept.
+__device__ __forceinline__ unsigned long long goal_of(unsigned long long z, float p)
+{
+    bool more;
+    const unsigned long long g = scaled(z, p, more);
+    return max(g + more, 1ull);
+}
 
 // What a kernel's passes share.
-template <typename T, bool RES>
+template <typename T, bool RES, int ST>
 struct Sampler {
     using P = Piece<T>;
-    static constexpr int E = P::E;
+    using F = Piece<float>;
+    static constexpr int E = P::E, SWARPS = ST / 32;
+    static constexpr int NB = BINS / ST;         // bins of a thread
+    static constexpr int NS = MAX_CLUSTER * SWARPS / 32;             // warps whose exchanged values a lane looks at
     const SampleArgs &a;
-    SampleShared &sh;
+    SampleShared<SWARPS> &sh;
     uint4 *pieces;                 // [slice] of this CTA (RES)
     uint32_t *hist;                // [4][BINS]: counts, masses, largest and smallest key
     const T *row;                  // the row's first element
     int shift;                     // elements from a 16-byte boundary to it
     int C, rank, turn;
+    bool open;                     // other CTAs may still read this one's histogram
     Scale s;
 
     __device__ __forceinline__ int64_t position(int p) const { return ((int64_t)rank * a.slice + p) * E; }
@@ -268,15 +328,29 @@ struct Sampler {
             st_cluster(to + 2 * (uint32_t)sizeof(sh.slot[0][0]), v2);
         }
         cluster_sync();
+        open = false;
     }
-    // What the warp 2 lane + i exchanged (0 past the last one).
+    // What the warp NS lane + i exchanged (0 past the last one).
     __device__ __forceinline__ unsigned long long slot_of(int which, int i) const
     {
-        const int w = 2 * (threadIdx.x % 32) + i;
+        const int w = NS * (threadIdx.x % 32) + i;
         return w < C * SWARPS ? sh.slot[turn][which][w] : 0;
     }
-    // The sum of what the warps exchanged.
-    __device__ unsigned long long exchanged_sum(int which) const { return warp_sum(slot_of(which, 0) + slot_of(which, 1)); }
+    // The sum, and the largest low word, of what the warps exchanged.
+    __device__ unsigned long long exchanged_sum(int which) const
+    {
+        unsigned long long v = 0;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) v += slot_of(which, i);
+        return warp_sum(v);
+    }
+    __device__ uint32_t exchanged_max(int which) const
+    {
+        uint32_t v = 0;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) v = max(v, (uint32_t)slot_of(which, i));
+        return __reduce_max_sync(0xffffffffu, v);
+    }
     // The smallest key above `key` (or the largest below it) of any element; ~0 (0) if there is none.
     __device__ uint32_t next_key(uint32_t key, bool above)
     {
@@ -293,7 +367,7 @@ struct Sampler {
         }
         best = above ? __reduce_min_sync(0xffffffffu, best) : __reduce_max_sync(0xffffffffu, best);
         exchange(above ? (uint32_t)~best : best, 0);
-        best = __reduce_max_sync(0xffffffffu, max((uint32_t)slot_of(0, 0), (uint32_t)slot_of(0, 1)));
+        best = exchanged_max(0);
         return above ? ~best : best;
     }
     // Exclusive sum over the CTA's threads.
@@ -303,10 +377,156 @@ struct Sampler {
         const unsigned long long in = warp_scan(v);
         if (lane == 31) sh.scan[which][warp] = in;
         __syncthreads();
-        unsigned long long base = 0;
+        return warp_sum(lane < warp ? sh.scan[which][lane] : 0ull) + in - v;
+    }
+
+    // Sum over the CTA's threads.
+    __device__ unsigned long long block_sum(unsigned long long v, int which)
+    {
+        v = warp_sum(v);
+        if (threadIdx.x % 32 == 0) sh.scan[which][threadIdx.x / 32] = v;
+        __syncthreads();
+        return warp_sum(threadIdx.x % 32 < SWARPS ? sh.scan[which][threadIdx.x % 32] : 0ull);
+    }
+
+    // The elements from t up, of the whole row and in the order of the ids, NB to each
+    // thread of every CTA: their order's word above the id, 0 past the last one.  Their
+    // number; above FEW nothing is done.
+    __device__ int gather(float t, unsigned long long (&e)[NB])
+    {
+        const int tid = threadIdx.x, lane = tid % 32, n = count(first());
+        uint2 *list = reinterpret_cast<uint2 *>(hist + 4 * BINS);
+        uint32_t c = 0, some = 0;                                    // elements, and the pieces that have them
+#pragma unroll 2
+        for (int i = 0; i < n; ++i) {
+            const uint4 r = piece(first() + i);
+            if (P::max_of(r) < t) continue;
+            some |= 1u << (i & 31);
+            float v[E];
+            P::unpack(r, v);
 #pragma unroll
-        for (int i = 0; i < SWARPS; ++i) base += i < warp ? sh.scan[which][i] : 0ull;
-        return base + in - v;
+            for (int j = 0; j < E; ++j) c += v[j] >= t;
+        }
+        uint32_t at = (uint32_t)block_scan(c, 0);
+        for (int i = 0; i < n; ++i) {
+            if (!(some >> (i & 31) & 1u)) continue;
+            float v[E];
+            P::unpack(piece(first() + i), v);
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (v[j] >= t) {
+                    if (at < FEW) list[at] = make_uint2(order_of(v[j]), (uint32_t)(position(first() + i) + j - shift));
+                    ++at;
+                }
+        }
+        exchange(warp_sum(c), 0);
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) mine += (uint32_t)slot_of(0, i);
+        const uint32_t to = warp_scan(mine);                         // (SWARPS / NS = 4 lanes to a CTA)
+        const int total = (int)__shfl_sync(0xffffffffu, to, 31);
+        if (total > FEW) return total;
+        if (tid < 32 && lane % 4 == 0) sh.base[lane / 4] = (int)(to - mine);
+        if (tid == 0) sh.base[MAX_CLUSTER] = total;
+        __syncthreads();
+        const int each = (total + ST - 1) / ST;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int k = each * tid + i;
+            e[i] = 0;
+            if (i < each && k < total) {
+                int r = 0;
+#pragma unroll
+                for (int c = 1; c < MAX_CLUSTER; ++c) r += k >= sh.base[c];
+                uint32_t x[2];
+                ld_cluster(cluster_addr(list + (k - sh.base[r]), r), x);
+                e[i] = (unsigned long long)x[0] << 32 | x[1];
+            }
+        }
+        open = true;
+        return total;
+    }
+    static __device__ __forceinline__ uint32_t word_of(unsigned long long e) { return (uint32_t)(e >> 32); }
+    static __device__ __forceinline__ float value_of(unsigned long long e) { return Piece<float>::value((uint32_t)(e >> 32)); }
+
+    // Of gathered elements with words from klo to khi, each worth x (0: out of it), from
+    // the largest down: the word at which their sum reaches `target`, and of the elements
+    // with it the one that does, counted from 1.  False: none does.  By levels of this
+    // CTA's histogram of worths (numbers, where they are 1; so too where a bin has one
+    // value, times its weight: 64-bit sums take the place of many), largest and smallest
+    // words.
+    template <bool MASS>
+    __device__ bool select(const unsigned long long (&e)[NB], const unsigned long long (&x)[NB], uint32_t klo, uint32_t khi,
+                           unsigned long long target, uint32_t &word, uint32_t &which)
+    {
+        const int tid = threadIdx.x;
+        constexpr bool COUNT = !MASS || P::KEY_SHIFT > 0;
+        unsigned long long *worth = reinterpret_cast<unsigned long long *>(hist);
+        for (;;) {
+            constexpr int LOG = 10;
+            const int n = 32 - __clz(khi - klo), bits = n > LOG ? n - LOG : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i * ST + tid < BINS) {
+                    if (COUNT) hist[i * ST + tid] = 0;
+                    else worth[i * ST + tid] = 0;
+                    hist[2 * BINS + i * ST + tid] = 0;
+                    hist[3 * BINS + i * ST + tid] = ~0u;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+                if (x[i] && word_of(e[i]) >= klo && word_of(e[i]) <= khi) {
+                    const uint32_t at = (khi - word_of(e[i])) >> bits;
+                    if (COUNT) atomicAdd(hist + at, 1u);
+                    else atomicAdd(worth + at, x[i]);
+                    atomicMax(hist + 2 * BINS + at, word_of(e[i]));
+                    atomicMin(hist + 3 * BINS + at, word_of(e[i]));
+                }
+            __syncthreads();
+            unsigned long long w[NB];
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const int at = NB * tid + i;
+                if (!COUNT) w[i] = worth[at];
+                else if (!MASS) w[i] = hist[at];
+                else if (bits <= P::KEY_SHIFT) w[i] = hist[at] ? hist[at] * weight_exact(F::value(hist[2 * BINS + at]), s, sh.table) : 0;
+                else w[i] = 0;
+            }
+            if (MASS && COUNT && bits > P::KEY_SHIFT) {
+                // (a range of more than ten octaves) the sums themselves
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i * ST + tid < BINS) worth[i * ST + tid] = 0;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+                    if (x[i] && word_of(e[i]) >= klo && word_of(e[i]) <= khi) atomicAdd(worth + ((khi - word_of(e[i])) >> bits), x[i]);
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NB; ++i) w[i] = worth[NB * tid + i];
+            }
+            if (!find_bin(w, target, 0, false)) return false;
+            const uint32_t bin = sh.bin, big = hist[2 * BINS + bin], small = hist[3 * BINS + bin];
+            target -= sh.before;
+            if (big == small) {
+                word = big;
+                // equal elements are worth the same
+                unsigned long long each = 0;
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+                    if (x[i] && word_of(e[i]) == big) each = x[i];
+                if (each) sh.mass = each;
+                __syncthreads();
+                each = sh.mass;
+                which = (uint32_t)((target + each - 1) / each);
+                return true;
+            }
+            klo = small;
+            khi = big;
+            __syncthreads();
+        }
     }
 
     // Sum of the weights of l > t and number of l == t in n pieces from p of this CTA
@@ -384,17 +604,21 @@ struct Sampler {
     // Histogram of the elements from lo up whose keys are at most khi, from the largest
     // down, by bins of equal width 1 / inv (inv > 0) or of 2^bits keys: their number, and
     // where a bin may have several keys (bits > 0) the largest and the smallest, and
-    // (MASS) their mass times `unit`, rounded.
+    // (MASS) their mass times `unit`, rounded.  Each thread gets NB of the masses, or of
+    // the numbers, summed over the cluster.
     template <bool MASS>
-    __device__ void histogram(float lo, uint32_t khi, int bits, float inv, float unit, Bins &b)
+    __device__ void histogram(float lo, uint32_t khi, int bits, float inv, float unit, uint32_t (&b)[NB])
     {
         const int tid = threadIdx.x, n = count(first());
         const bool keys = bits > 0;
-        reinterpret_cast<uint4 *>(hist)[tid] = make_uint4(0, 0, 0, 0);
-        if (keys) {
-            if (MASS) reinterpret_cast<uint4 *>(hist + BINS)[tid] = make_uint4(0, 0, 0, 0);
-            reinterpret_cast<uint4 *>(hist + 2 * BINS)[tid] = make_uint4(0, 0, 0, 0);
-            reinterpret_cast<uint4 *>(hist + 3 * BINS)[tid] = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (open) cluster_sync();
+        for (int i = tid; i < BINS / 4; i += ST) {
+            reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0, 0, 0, 0);
+            if (keys) {
+                if (MASS) reinterpret_cast<uint4 *>(hist + BINS)[i] = make_uint4(0, 0, 0, 0);
+                reinterpret_cast<uint4 *>(hist + 2 * BINS)[i] = make_uint4(0, 0, 0, 0);
+                reinterpret_cast<uint4 *>(hist + 3 * BINS)[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+            }
         }
         __syncthreads();
 #pragma unroll 2
@@ -419,29 +643,19 @@ struct Sampler {
                 }
         }
         cluster_sync();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { b.count[k] = b.mass[k] = b.largest[k] = 0; b.smallest[k] = ~0u; }
+        open = true;
+        uint32_t x[MAX_CLUSTER][NB];
+        const uint32_t *from = hist + (MASS && keys ? BINS : 0) + NB * tid;
 #pragma unroll
         for (int r = 0; r < MAX_CLUSTER; ++r)
-            if (r < C) {
-                const uint4 x = ld_cluster4(cluster_addr(hist + 4 * tid, r));
-                b.count[0] += x.x; b.count[1] += x.y; b.count[2] += x.z; b.count[3] += x.w;
-            }
-        if (keys)
-#pragma unroll 2
-            for (int r = 0; r < C; ++r) {
-                if (MASS) {
-                    const uint4 x = ld_cluster4(cluster_addr(hist + BINS + 4 * tid, r));
-                    b.mass[0] += x.x; b.mass[1] += x.y; b.mass[2] += x.z; b.mass[3] += x.w;
-                }
-                const uint4 y = ld_cluster4(cluster_addr(hist + 2 * BINS + 4 * tid, r));
-                b.largest[0] = max(b.largest[0], y.x); b.largest[1] = max(b.largest[1], y.y);
-                b.largest[2] = max(b.largest[2], y.z); b.largest[3] = max(b.largest[3], y.w);
-                const uint4 z = ld_cluster4(cluster_addr(hist + 3 * BINS + 4 * tid, r));
-                b.smallest[0] = min(b.smallest[0], z.x); b.smallest[1] = min(b.smallest[1], z.y);
-                b.smallest[2] = min(b.smallest[2], z.z); b.smallest[3] = min(b.smallest[3], z.w);
-            }
-        cluster_arrive();                          // others may read on; waited for before the bins are used again
+            if (r < C) ld_cluster(cluster_addr(from, r), x[r]);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+            b[k] = 0;
+#pragma unroll
+            for (int r = 0; r < MAX_CLUSTER; ++r)
+                if (r < C) b[k] += x[r][k];
+        }
     }
     // Bins of equal width from m down to lo, for the first level (0 where the width has no use).
     __device__ __forceinline__ float bins_per(float lo) const
@@ -456,27 +670,44 @@ struct Sampler {
         const int n = 32 - __clz(khi - klo);       // bits of the largest difference
         return n > LOG ? n - LOG : 0;
     }
-    // The first of the CTA's bins at which the sum of x reaches `target`; what is known
-    // of it.  False: none does.
-    __device__ bool find_bin(const unsigned long long (&x)[4], const Bins &b, unsigned long long target, int which)
+    // The first bin at which the sum of x reaches `target`, and what is known of it
+    // (keys: its number of elements, largest and smallest key).  False: none does.
+    __device__ bool find_bin(const unsigned long long (&x)[NB], unsigned long long target, int which, bool keys)
     {
         const int tid = threadIdx.x;
         if (tid == 0) sh.bin = BINS;
-        unsigned long long at = block_scan(x[0] + x[1] + x[2] + x[3], which);    // its barrier comes before the writing
+        unsigned long long mine = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < NB; ++k) mine += x[k];
+        unsigned long long at = block_scan(mine, which);             // its barrier comes before the writing
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
             if (at < target && target <= at + x[k]) {
-                sh.bin = 4 * tid + k;
+                sh.bin = NB * tid + k;
                 sh.before = at;
                 sh.mass = x[k];
-                sh.count = b.count[k];
-                sh.largest = b.largest[k];
-                sh.smallest = b.smallest[k];
             }
             at += x[k];
         }
         __syncthreads();
-        return sh.bin < BINS;
+        const uint32_t bin = sh.bin;
+        if (bin == BINS) return false;
+        if (keys) {
+            if (tid < 32) {
+                uint32_t c = 0, big = 0, small = ~0u;
+                if (tid < C) {
+                    c = ld_cluster1(cluster_addr(hist + bin, tid));
+                    big = ld_cluster1(cluster_addr(hist + 2 * BINS + bin, tid));
+                    small = ld_cluster1(cluster_addr(hist + 3 * BINS + bin, tid));
+                }
+                c = __reduce_add_sync(0xffffffffu, c);
+                big = __reduce_max_sync(0xffffffffu, big);
+                small = __reduce_min_sync(0xffffffffu, small);
+                if (tid == 0) { sh.count = c; sh.largest = big; sh.smallest = small; }
+            }
+            __syncthreads();
+        }
+        return true;
     }
 };
 
@@ -487,15 +718,15 @@ struct Kept {
 };
 
 // grid: a cluster of C CTAs for each row; ST threads; pieces, then the histogram.
-template <typename T, bool RES>
-__global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ SampleArgs a)
+template <typename T, bool RES, int ST>
+__global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant__ SampleArgs a)
 {
-    using S = Sampler<T, RES>;
+    using S = Sampler<T, RES, ST>;
     using P = Piece<T>;
     using F = Piece<float>;
-    constexpr int E = P::E, KS = P::KEY_SHIFT;
+    constexpr int E = P::E, KS = P::KEY_SHIFT, SWARPS = ST / 32, NB = S::NB, NS = S::NS;
     extern __shared__ __align__(16) uint8_t dyn[];
-    __shared__ SampleShared sh;
+    __shared__ SampleShared<SWARPS> sh;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     uint32_t C;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
@@ -503,7 +734,7 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
     const int q_seq = (int)(n / a.rows);
     const T *row = static_cast<const T *>(a.in) + n * a.ld;
     S x{a, sh, reinterpret_cast<uint4 *>(dyn), reinterpret_cast<uint32_t *>(dyn + (RES ? (size_t)a.slice * 16 : 0)), row,
-        (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)), (int)C, (int)cluster_rank(), 0, Scale{}};
+        (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)), (int)C, (int)cluster_rank(), 0, false, Scale{}};
     if (tid < 64) sh.table[tid] = a.table.v[tid];
     if (tid < 4) sh.note[tid] = ~0ull;
     cluster_arrive();                              // waited for before the first access to another CTA
@@ -526,7 +757,11 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
             if (p < half && p + ST >= half) cp_async_commit();                  // (each thread has one such p, or none)
         }
         cp_async_commit();
-        if (tid == 0) sh.shift = min_p > 0.0f ? (double)temp * log(fmin((double)min_p, 1.0)) : 0.0;
+        if (tid == 0 && min_p > 0.0f) {
+            const double d = (double)temp * log(fmin((double)min_p, 1.0));
+            sh.shift_hi = (float)d;
+            sh.shift_lo = (float)(d - (double)sh.shift_hi);
+        }
         auto take = [&](int from, int to) {
 #pragma unroll 4
             for (int p = from; p < to; p += ST) {
@@ -543,7 +778,11 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
         cp_async_wait<0>();
         take(half + tid, a.slice);
     } else {
-        if (tid == 0) sh.shift = min_p > 0.0f ? (double)temp * log(fmin((double)min_p, 1.0)) : 0.0;
+        if (tid == 0 && min_p > 0.0f) {
+            const double d = (double)temp * log(fmin((double)min_p, 1.0));
+            sh.shift_hi = (float)d;
+            sh.shift_lo = (float)(d - (double)sh.shift_hi);
+        }
 #pragma unroll 4
         for (int p = tid; p < a.slice; p += ST) mx = fmaxf(mx, P::max_of(x.fetch(p)));
     }
@@ -568,28 +807,63 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
     }
     cluster_wait();
     x.exchange(key, (unsigned long long)groups << 32 | (uint32_t)~group);
-    const uint32_t kmax = __reduce_max_sync(0xffffffffu, max((uint32_t)x.slot_of(0, 0), (uint32_t)x.slot_of(0, 1)));
-    uint32_t kgroup = ~__reduce_max_sync(0xffffffffu, max((uint32_t)x.slot_of(1, 0), (uint32_t)x.slot_of(1, 1)));
-    if ((int)__reduce_add_sync(0xffffffffu, (uint32_t)(x.slot_of(1, 0) >> 32) + (uint32_t)(x.slot_of(1, 1) >> 32)) < top_k) kgroup = 0;
+    const uint32_t kmax = x.exchanged_max(0);
+    uint32_t kgroup = ~x.exchanged_max(1), n_groups = 0;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) n_groups += (uint32_t)(x.slot_of(1, i) >> 32);
+    n_groups = __reduce_add_sync(0xffffffffu, n_groups);
+    if ((int)n_groups < top_k) kgroup = 0;
 
     Kept kept{-INFINITY, 0};
+    // The truncated row; cut: the last id with l == t that is kept.  (Pieces below the
+    // first bound written as soon as it is known: 226 us for 544 rows, 209 without.)
+    auto write_out = [&](int cut) {
+        T *out = static_cast<T *>(a.out) + n * a.ldo;
+        const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
+        const T dropped = P::raw(a.mask_value);
+#pragma unroll 4
+        for (int p = tid; p < a.slice; p += ST) {
+            const int64_t at = ids0 + (int64_t)p * E;
+            if (at >= a.V) break;
+            const uint4 r = x.piece(p);
+            T e[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) e[j] = dropped;
+            if (P::max_of(r) >= kept.t) {
+                float v[E];
+                P::unpack(r, v);
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (v[j] > kept.t || (v[j] == kept.t && kept.q && at + j <= cut)) e[j] = P::raw(v[j]);
+            }
+            if (same && at >= 0 && at + E <= a.V) {
+                *reinterpret_cast<uint4 *>(out + at) = P::pack_raw(e);
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (at + j >= 0 && at + j < a.V) out[at + j] = e[j];
+            }
+        }
+    };
     const bool empty = kmax < LOWEST;
-    bool k_on = false, p_on = false, check_p = false;
+    bool k_on = false, p_on = false, check_p = false, settled = false;
+    int cut = ALL;
     int few = ALL;                                 // at most so many are kept
     unsigned long long z1 = 0;                     // mass of what min-p and top-k keep
     bool z1_exact = false;
     Kept first{-INFINITY, 0};                      // ... as a threshold
     if (!empty) {
         const float m = F::value(kmax);
-        {
-            // log2(e) / T to 48 bits: the quotient's rounding comes back through the remainder
-            const float tc = fminf(fmaxf(temp, 1e-37f), 1e37f), kh = 1.44269502f / tc;
-            x.s = Scale{m, kh, (fmaf(-kh, tc, 1.44269502f) + 1.92596303e-8f) / tc, a.scale};
-        }
+        x.s = make_scale(m, temp, a.scale);
         const uint32_t top = kmax >> KS;
         float low = -3.402823466e38f;              // the lowest value that may be kept
         if (m == INFINITY) low = INFINITY;         // the limit: the infinities share all the mass
-        else if (min_p > 0.0f) low = fmaxf(__double2float_ru((double)m + sh.shift), low);
+        else if (min_p > 0.0f) {
+            // the smallest value that is not below m + T ln(min_p)
+            const float hi = sh.shift_hi, sum = __fadd_rn(m, hi), bb = __fsub_rn(sum, m);
+            const float rest = __fadd_rn(__fsub_rn(m, __fsub_rn(sum, bb)), __fsub_rn(hi, bb)) + sh.shift_lo;
+            low = fmaxf(rest > 0.0f ? nextafterf(sum, INFINITY) : sum, low);
+        }
         if (low > -3.402823466e38f) kept = {low, ALL};
         if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {
             kept = {m, 1};
@@ -598,47 +872,105 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
             k_on = top_k > 0 && top_k < a.V && m < INFINITY;
             p_on = top_p < 1.0f && m < INFINITY;
         }
-        Bins b;
-        unsigned long long wide[4];
+        uint32_t b[NB];
+        unsigned long long wide[NB];
+        // All of it where few elements, those from t up, can be kept.  False if there are
+        // too many.
+        auto settle = [&](float t, int k) {
+            unsigned long long e[NB];
+            const int total = x.gather(t, e);
+            if (total > FEW) return false;
+            uint32_t last = max(order_of(low), order_of(t)), q = ALL;  // kept: words above last, and the first q of those equal to it
+            if (total > k) {
+#pragma unroll
+                for (int i = 0; i < NB; ++i) wide[i] = S::word_of(e[i]) >= last;
+                x.template select<false>(e, wide, last, kmax, k, last, q);             // (false: fewer than k)
+            }
+            // the ties' places, as long as only some of them are kept
+            uint32_t tie = 0;
+            auto worth = [&]() {
+                uint32_t at = 0;
+                if (q < ALL) {
+                    uint32_t ties = 0;
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) ties += S::word_of(e[i]) == last;
+                    __syncthreads();
+                    at = tie = (uint32_t)x.block_scan(ties, 1);
+                }
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    const bool equal = S::word_of(e[i]) == last;
+                    const bool keep = S::word_of(e[i]) > last || (equal && at < q);
+                    at += equal;
+                    wide[i] = keep && e[i] ? weight_exact(S::value_of(e[i]), x.s, sh.table) : 0;
+                }
+            };
+            if (p_on) {
+                worth();
+                unsigned long long mine = 0;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) mine += wide[i];
+                __syncthreads();
+                z1 = x.block_sum(mine, 0);
+                __syncthreads();
+                uint32_t word, which;
+                if (x.template select<true>(e, wide, last, kmax, goal_of(z1, top_p), word, which)) { last = word; q = which; }
+            }
+            kept = {F::value(last), 1};
+            settled = true;
+            worth();
+            if (q < ALL) {
+                // the id of the last tie that is kept
+                if (tid == 0) sh.note[2] = (unsigned long long)ALL;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+                    if (S::word_of(e[i]) == last && ++tie == q) sh.note[2] = (uint32_t)e[i];
+                __syncthreads();
+                cut = (int)sh.note[2];
+            }
+            if (a.tokens && x.rank == 0) {
+                unsigned long long mine = 0;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) mine += wide[i];
+                const unsigned long long z = x.block_sum(mine, 0);
+                bool more;
+                const unsigned long long goal = u < 1.0f ? min(scaled(z, u, more), z - 1) : z - 1;
+                __syncthreads();
+                unsigned long long at = x.block_scan(mine, 1);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    if (at <= goal && goal < at + wide[i]) a.tokens[n] = (int)(uint32_t)e[i];
+                    at += wide[i];
+                }
+            }
+            return true;
+        };
+        if (few == 1) settle(m, 1);
         // ------------------------------------------------------------ top-k
         if (k_on) {
             float lo = kgroup >= LOWEST ? fmaxf(low, F::value(kgroup)) : low;
+            // above the smallest of g maxima there are about g ln g elements
+            if (kgroup >= LOWEST && n_groups <= 128 && settle(lo, top_k)) k_on = p_on = false;
             uint32_t klo = order_of(lo) >> KS, khi = top, left = top_k;
-            for (int level = 0;; ++level) {
+            for (int level = 0; k_on; ++level) {
                 const int bits = S::level_bits(klo, khi);
                 x.template histogram<false>(lo, khi, bits, level == 0 && bits ? x.bins_per(lo) : 0.0f, 0.0f, b);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) wide[i] = b.count[i];
-                const bool found = x.find_bin(wide, b, left, level & 1);
-                cluster_wait();
+                for (int i = 0; i < NB; ++i) wide[i] = b[i];
+                const bool found = x.find_bin(wide, left, level & 1, bits > 0);
                 if (!found) break;                                    // fewer than k
                 few = top_k;
+                if (level == 0 && (bits ? sh.count : sh.mass) + sh.before <= FEW) {
+                    const float t = bits ? P::value(sh.smallest) : P::value(khi - sh.bin);
+                    __syncthreads();
+                    settle(t, top_k);
+                    p_on = false;
+                    break;
+                }
                 left -= (uint32_t)sh.before;
                 if (bits == 0) {
                     kept = {P::value(khi - sh.bin), (int)left};
-                    if (p_on && level == 0) {
-                        // the bins are single values: top-p from the same counts
-                        const uint32_t last = sh.bin;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t at = 4 * tid + i;
-                            if (at > last) b.count[i] = 0;
-                            if (at == last) b.count[i] = left;
-                            wide[i] = b.count[i] ? b.count[i] * weight_exact(P::value(top - at), x.s, sh.table) : 0;
-                        }
-                        const unsigned long long mine = wide[0] + wide[1] + wide[2] + wide[3];
-                        const unsigned long long z = warp_sum(mine);
-                        __syncthreads();                              // what was found has been read
-                        if (lane == 0) sh.scan[1][warp] = z;
-                        __syncthreads();
-                        for (int i = 0; i < SWARPS; ++i) z1 += sh.scan[1][i];
-                        const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z1), 1.0);
-                        if (x.find_bin(wide, b, target, 0)) {
-                            const unsigned long long each = sh.mass / sh.count;
-                            kept = {P::value(top - sh.bin), (int)((target - sh.before + each - 1) / each)};
-                        }
-                        p_on = false;
-                    }
                     break;
                 }
                 if (left == 1) { kept = {P::value(sh.largest), 1}; break; }
@@ -654,14 +986,15 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
         if (p_on) {
             unsigned long long sum;
             uint32_t ties;
-            z1_exact = few <= 4096 * (int)C;
+            z1_exact = few <= 4096 * (int)C || !x.s.near;
             x.sums(z1_exact, x.first(), x.count(x.first()), kept.t, sum, ties);
             x.exchange(warp_sum(sum), warp_sum(ties));
             z1 = x.exchanged_sum(0);
             const unsigned long long nt = min(x.exchanged_sum(1), (unsigned long long)kept.q);
             if (nt) z1 += nt * weight_exact(kept.t, x.s, sh.table);
-            const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z1), 1.0);
-            const unsigned long long slack = z1_exact ? 0 : (unsigned long long)((double)z1 * a.slack) + 64;
+            const unsigned long long target = goal_of(z1, top_p);
+            // only the target is off: its masses are exact
+            const unsigned long long slack = z1_exact ? 0 : (unsigned long long)(part_of(z1) * (SLACK * top_p)) + SLACK_UNITS;
             const int down = max(0, 33 - __clzll(z1));                // z1 >> down has 31 bits
             const float unit = __uint_as_float((uint32_t)(127 + a.scale - down) << 23);
             // what may be left out has at most 1 - top_p of the mass
@@ -682,16 +1015,15 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                 if (bits == 0) {
                     // single values: their masses from the counts
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        wide[i] = b.count[i] ? b.count[i] * weight_exact(P::value(khi - (4 * tid + i)), x.s, sh.table) : 0;
-                    found = x.find_bin(wide, b, sure ? left : max(left, 1ull) << down, level & 1);
+                    for (int i = 0; i < NB; ++i)
+                        wide[i] = b[i] ? b[i] * weight_exact(P::value(khi - (NB * tid + i)), x.s, sh.table) : 0;
+                    found = x.find_bin(wide, sure ? left : max(left, 1ull) << down, level & 1, false);
                 } else {
                     sure = false;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) wide[i] = b.mass[i];
-                    found = x.find_bin(wide, b, max(left, 1ull), level & 1);
+                    for (int i = 0; i < NB; ++i) wide[i] = b[i];
+                    found = x.find_bin(wide, max(left, 1ull), level & 1, true);
                 }
-                cluster_wait();
                 if (!found) {
                     // by rounding: the smallest that was counted, or what the bound left out
                     check_p = true;
@@ -702,7 +1034,7 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                 if (bits == 0) {
                     kept.t = P::value(khi - sh.bin);
                     if (sure) {
-                        const unsigned long long each = sh.mass / sh.count, need = (left + each - 1) / each;
+                        const unsigned long long each = weight_exact(kept.t, x.s, sh.table), need = (left + each - 1) / each;
                         kept.q = (int)need;
                         check_p = !(left > (need - 1) * each + slack && need * each >= left + slack);
                     } else {
@@ -724,13 +1056,14 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
     }
 
     // ------------------------------------------------------------------- the draw
-    int cut = ALL;                                 // the last id with l == t that is kept
+    bool written = false;
     if (empty) {
         if (tid == 0 && x.rank == 0 && a.tokens) a.tokens[n] = -1;
         kept = {INFINITY, 0};
-    } else if (a.tokens || check_p || (a.out && kept.q < ALL && kept.q > 0)) {
+    } else if (!settled && (a.tokens || check_p || (a.out && kept.q < ALL && kept.q > 0))) {
         // a check that the fast weights could hardly decide starts with exact ones
-        bool exact = few <= 4096 * (int)C || (check_p && (double)weight_exact(kept.t, x.s, sh.table) < 20.0 * a.slack * (double)z1);
+        bool exact = few <= 4096 * (int)C || !x.s.near ||
+                     (check_p && (float)weight_exact(kept.t, x.s, sh.table) < 4.0f * SLACK * part_of(z1));
         // while t is not sure: what is known of its key, from below and above
         uint32_t known_lo = max(order_of(first.t), LOWEST) >> KS, known_hi = kmax >> KS;
         int moves = 0;
@@ -751,19 +1084,30 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                 x.sums(exact, x.first(), x.count(x.first()), t, sum, ties);
                 x.exchange(warp_sum(sum), warp_sum(ties));
             }
-            // each lane takes two consecutive warps: their ties, then their kept mass
-            const uint32_t wn0 = (uint32_t)x.slot_of(1, 0), wn1 = (uint32_t)x.slot_of(1, 1);
-            const unsigned long long ws0 = x.slot_of(0, 0), ws1 = x.slot_of(0, 1);
-            const uint32_t n_in = warp_scan(wn0 + wn1), n0 = n_in - wn0 - wn1, n1 = n_in - wn1;
+            // each lane takes NS consecutive warps: their ties, then their kept mass
+            uint32_t wn[NS], nb[NS], n_sum = 0;
+            unsigned long long wm[NS];
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                nb[i] = n_sum;                                       // ties before, from the lane's first warp
+                n_sum += wn[i] = (uint32_t)x.slot_of(1, i);
+                wm[i] = x.slot_of(0, i);
+            }
+            const uint32_t n_in = warp_scan(n_sum);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) nb[i] += n_in - n_sum;
             const uint32_t all_ties = __shfl_sync(0xffffffffu, n_in, 31);
             const unsigned long long wt = all_ties ? weight_exact(t, x.s, sh.table) : 0;
             if (check_p) {
                 // is t where the mass before reaches the target?  How many of its ties?
-                const unsigned long long above = warp_sum(ws0 + ws1);
+                const unsigned long long above = x.exchanged_sum(0);
                 const uint32_t may = t == first.t ? min(all_ties, (uint32_t)first.q) : all_ties;
-                const unsigned long long target = (unsigned long long)fmax(ceil((double)top_p * (double)z1), 1.0);
-                const unsigned long long slack = (exact ? 0 : (unsigned long long)((double)above * a.slack) + 64) +
-                                                 (z1_exact ? 0 : (unsigned long long)((double)z1 * a.slack) + 64);
+                const unsigned long long target = goal_of(z1, top_p);
+                // above - top_p z1, with the same weights in both where both are fast
+                const float av = part_of(above), zv = part_of(z1);
+                const unsigned long long slack = exact ? 0
+                    : (unsigned long long)(z1_exact ? SLACK * av
+                                                    : SLACK_W * ((1.0f - top_p) * av + top_p * (zv - av)) + SLACK_SUM * (av + top_p * zv)) + SLACK_UNITS;
                 const bool small = above >= target + slack, large = above + may * wt + slack < target && t > first.t;
                 if ((small || large) && moves < 40) {                 // 33 halve any range of keys to one
                     // the next value first (rounded masses put t off by one), then the middle
@@ -786,17 +1130,29 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                 check_p = false;
             }
             const uint32_t q = (uint32_t)kept.q;
-            const unsigned long long wm0 = ws0 + (min(n0 + wn0, q) - min(n0, q)) * wt, wm1 = ws1 + (min(n1 + wn1, q) - min(n1, q)) * wt;
-            const unsigned long long m_in = warp_scan(wm0 + wm1);
+            unsigned long long m_sum = 0, mb[NS];
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                mb[i] = m_sum;
+                m_sum += wm[i] += (min(nb[i] + wn[i], q) - min(nb[i], q)) * wt;
+            }
+            const unsigned long long m_in = warp_scan(m_sum);
             const unsigned long long z = __shfl_sync(0xffffffffu, m_in, 31);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) mb[i] += m_in - m_sum;
             const bool cuts = a.out && q && q < all_ties;
             const int me = x.rank * SWARPS + warp;
             if (cuts) {
                 // the q-th of the ties
-                const unsigned f0 = __ballot_sync(0xffffffffu, n0 < q && q <= n0 + wn0), f1 = __ballot_sync(0xffffffffu, n1 < q && q <= n1 + wn1);
-                const int who = f0 ? 2 * (__ffs(f0) - 1) : 2 * (__ffs(f1) - 1) + 1;
+                int who = -1;
+                uint32_t there = 0;
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+                    if (nb[i] < q && q <= nb[i] + wn[i]) { who = NS * lane + i; there = nb[i]; }
+                const int src = __ffs(__ballot_sync(0xffffffffu, who >= 0)) - 1;
+                who = __shfl_sync(0xffffffffu, who, src);
+                there = __shfl_sync(0xffffffffu, there, src);
                 if (who == me) {
-                    const uint32_t there = __shfl_sync(0xffffffffu, f0 ? n0 : n1, who / 2);
                     const uint32_t in = warp_scan(ties);
                     uint32_t seen = there + in - ties;
                     if (seen < q && q <= seen + ties) {
@@ -814,18 +1170,23 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                 }
             }
             if (a.tokens) {
-                unsigned long long goal = (unsigned long long)((double)u * (double)z);
-                if (goal >= z) goal = z - 1;
-                const unsigned long long slack = exact ? 0 : (unsigned long long)((double)z * a.slack) + 64;
-                const unsigned long long m0 = m_in - wm0 - wm1, m1 = m_in - wm1;
-                const unsigned f0 = __ballot_sync(0xffffffffu, m0 <= goal && goal < m0 + wm0), f1 = __ballot_sync(0xffffffffu, m1 <= goal && goal < m1 + wm1);
-                const int who = f0 ? 2 * (__ffs(f0) - 1) : 2 * (__ffs(f1) - 1) + 1;
+                bool more;
+                const unsigned long long goal = u < 1.0f ? min(scaled(z, u, more), z - 1) : z - 1;
+                int who = -1;
+                unsigned long long there = 0, mine = sum;
+                uint32_t there_n = 0, my_ties = ties;
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+                    if (mb[i] <= goal && goal < mb[i] + wm[i]) { who = NS * lane + i; there = mb[i]; there_n = nb[i]; }
+                const int src = __ffs(__ballot_sync(0xffffffffu, who >= 0)) - 1;
+                who = __shfl_sync(0xffffffffu, who, src);
                 if (who == me) {
                     // the lane, then the piece, then the element
-                    unsigned long long there = __shfl_sync(0xffffffffu, f0 ? m0 : m1, who / 2), mine = sum;
-                    uint32_t there_n = __shfl_sync(0xffffffffu, f0 ? n0 : n1, who / 2), my_ties = ties;
+                    there = __shfl_sync(0xffffffffu, there, src);
+                    there_n = __shfl_sync(0xffffffffu, there_n, src);
                     int p = 0;
                     bool ok = true;
+                    unsigned long long slack = 0;
                     for (int step = 0; step < 3 && ok; ++step) {
                         for (int p0 = 0;; p0 += 32) {
                             // step 0: the lanes' own ranges; 1: 32 pieces of the range found; 2: the elements of the piece found
@@ -862,6 +1223,11 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                                     }
                                     p = -1;
                                 } else {
+                                    // the sums before the lane less u of all, with the same weights in both; and
+                                    // the lane's own, which are looked at once more
+                                    if (step == 0 && !exact)
+                                        slack = (unsigned long long)(SLACK * (part_of(z) * (2.0f * u * (1.0f - u)) +
+                                                                              part_of(__shfl_sync(0xffffffffu, own, l)))) + SLACK_UNITS;
                                     there = __shfl_sync(0xffffffffu, ex_m, l);
                                     there_n = __shfl_sync(0xffffffffu, ex_n, l);
                                     p = step == 0 ? (warp * 32 + l) * a.per : p + p0 + l;
@@ -877,70 +1243,52 @@ __global__ void __launch_bounds__(ST, 4) k_sample(const __grid_constant__ Sample
                 }
             }
             if (exact && !cuts) break;
-            cluster_sync();
+            cluster_arrive();
+            if (RES && a.out && !cuts) {           // while the draw goes on
+                write_out(cut);
+                written = true;
+            }
+            cluster_wait();
             if (cuts) cut = (int)sh.note[0];
             if (exact || sh.note[1] != 1ull) break;
             exact = true;
         }
     }
+    if (!RES && a.out) cluster_sync();             // nobody reads the row any more: out may be it
 
-    // -------------------------------------------------------------- the truncated row
-    if (a.out) {
-        if (!RES) cluster_sync();                  // nobody reads the row any more: out may be it
-        T *out = static_cast<T *>(a.out) + n * a.ldo;
-        const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
-        const T dropped = P::raw(a.mask_value);
-#pragma unroll 2
-        for (int p = tid; p < a.slice; p += ST) {
-            const int64_t at = x.position(p) - x.shift;
-            if (at >= a.V) break;
-            const uint4 r = x.piece(p);
-            T e[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) e[j] = dropped;
-            if (P::max_of(r) >= kept.t) {
-                float v[E];
-                P::unpack(r, v);
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (v[j] > kept.t || (v[j] == kept.t && kept.q && at + j <= cut)) e[j] = P::raw(v[j]);
-            }
-            if (same && at >= 0 && at + E <= a.V) {
-                *reinterpret_cast<uint4 *>(out + at) = P::pack_raw(e);
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (at + j >= 0 && at + j < a.V) out[at + j] = e[j];
-            }
-        }
-    }
+    if (a.out && !written) write_out(cut);
+    if (x.open) cluster_sync();                    // others may still read the histogram
 }
 
 struct SamplePlan {
-    int C, slice, per;
+    int C, threads, slice, per;
     bool resident;
 };
 
-// CTAs of a row's cluster: the fewest that leave two on an SM, more while SMs would be
-// idle; the pieces of a CTA and of a thread.
+// CTAs of a row's cluster: the fewest that leave two on an SM, more while all rows'
+// CTAs have a place at the same time; the pieces of a CTA and of a thread.
 SamplePlan sample_plan(int64_t n, int V, int E, int sms)
 {
     const int64_t pieces = ((int64_t)V + E - 1 + E - 1) / E;          // wherever the row starts
     auto slice_of = [&](int C) { return (pieces + C - 1) / C; };
+    auto threads_of = [&](int C) { return slice_of(C) > 1024 ? 512 : 256; };
     auto bytes = [&](int C) { return (size_t)slice_of(C) * 16 + HIST_BYTES; };
+    auto fits = [&](int C) { return n * C * threads_of(C) <= (int64_t)sms * 1024; };
     int C = 1;
-    while (C < MAX_CLUSTER && (bytes(C) > SAMPLE_HALF || (n * C < 2 * sms && slice_of(C) > 2 * ST))) C *= 2;
+    while (C < MAX_CLUSTER && (bytes(C) > SAMPLE_HALF || (fits(2 * C) && slice_of(C) > 512))) C *= 2;
     const int slice = (int)slice_of(C);
-    return {C, slice, ((slice + ST - 1) / ST) | 1, bytes(C) <= SAMPLE_SMEM};
+    const bool resident = bytes(C) <= SAMPLE_SMEM;
+    const int threads = resident ? threads_of(C) : 512;
+    return {C, threads, slice, ((slice + threads - 1) / threads) | 1, resident};
 }
 
-template <typename T, bool RES>
+template <typename T, bool RES, int ST>
 int launch_sample(const SampleArgs &a, int64_t n, int C, cudaStream_t st)
 {
     static OncePerDevice once;
-    XH_CUDA(allow_smem(once, k_sample<T, RES>, SAMPLE_SMEM));
+    XH_CUDA(allow_smem(once, k_sample<T, RES, ST>, SAMPLE_SMEM));
     const size_t smem = (RES ? (size_t)a.slice * 16 : 0) + HIST_BYTES;
-    XH_CUDA(launch_head(k_sample<T, RES>, dim3((unsigned)(n * C)), ST, smem, st, (unsigned)C, a));
+    XH_CUDA(launch_head(k_sample<T, RES, ST>, dim3((unsigned)(n * C)), ST, smem, st, (unsigned)C, a));
     return XPRESS_OK;
 }
 
@@ -978,14 +1326,15 @@ extern "C" int xpress_sample(const xpress_sample_args *in, void *stream)
     int log2v = 0;
     while ((1 << log2v) < in->V) ++log2v;
     a.scale = 61 - log2v;
-    // the exponential, three roundings of the exponent (whose mean over the mass is
-    // below log2 V + 5: an element at -x has at most 2^-x of it), the sums
-    a.slack = 1.1f * (1.0f / (1 << 21) + 3.0f * 0.6932f * (log2v + 5) / (1 << 24));
     const SamplePlan p = sample_plan(n, in->V, (int)(16 / es), sms);
     a.slice = p.slice;
     a.per = p.per;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (in->dtype == XPRESS_BF16)
-        return p.resident ? launch_sample<uint16_t, true>(a, n, p.C, st) : launch_sample<uint16_t, false>(a, n, p.C, st);
-    return p.resident ? launch_sample<float, true>(a, n, p.C, st) : launch_sample<float, false>(a, n, p.C, st);
+        return !p.resident ? launch_sample<uint16_t, false, 512>(a, n, p.C, st)
+               : p.threads == 512 ? launch_sample<uint16_t, true, 512>(a, n, p.C, st)
+                                  : launch_sample<uint16_t, true, 256>(a, n, p.C, st);
+    return !p.resident ? launch_sample<float, false, 512>(a, n, p.C, st)
+           : p.threads == 512 ? launch_sample<float, true, 512>(a, n, p.C, st)
+                              : launch_sample<float, true, 256>(a, n, p.C, st);
 }

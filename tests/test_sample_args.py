@@ -82,7 +82,7 @@ def _fake(tmp_path):
 
 def test_variants(tmp_path):
     lib = _fake(tmp_path)
-    for dt, V in itertools.product((X.XPRESS_F32, X.XPRESS_BF16), (1000, 1 << 22)):
+    for dt, V in itertools.product((X.XPRESS_F32, X.XPRESS_BF16), (1000, 151936, 1 << 22)):
         assert lib.xpress_sample(_args(dtype=dt, V=V, ld=V, ldo=V), None) == OK
     _all_launched(lib)
 
