@@ -8,14 +8,18 @@
 // columns let the next tile's products run under the epilogue of the last.
 //
 // Roles (192 threads): warp 0 TMA producer (two K blocks of 128 rows of w and of
-// NT rows of x per copy), warp 1 TMEM allocator and MMA issuer, warps 2-5 epilogue
-// (one TMEM lane quarter each, so that a warp stores 32 consecutive outputs of a
-// row).
+// NT rows of x per copy), warp 1 TMEM allocator and MMA issuer, warps 2-5 epilogue:
+// one TMEM lane quarter each to shared memory, and from there four columns of four
+// rows to a thread, so that a warp stores 128 consecutive outputs of a row.  What it
+// reads of the residual for the first of them is asked for before the sums are waited
+// for.
 //
 // Where tiles are few, the CTAs of a cluster of S split K; each sends every CTA its
 // sums of that CTA's share of the rows (asynchronous stores that the receiver's
 // mbarrier counts), which adds them in rank order: the result does not depend on
 // timing.
+#include <type_traits>
+
 #include "linear.h"
 
 namespace xp {
@@ -35,8 +39,13 @@ struct FewShape {
     static constexpr uint32_t STAGE = LF_SKB * (LF_W + X);       // w's K blocks, then x's
     static constexpr uint32_t TMEM_COLS = 2 * NT < 32 ? 32 : 2 * NT;
     static constexpr uint32_t IDESC = idesc_bf16(LF_BN, NT);
-    static constexpr size_t PART = (size_t)NT * LF_BN * 4;       // sums of a K split
+    // Sums, of a K split those of this CTA's rows from each of the CTAs: by 4 rows of x
+    // (2 where a split leaves no more to a CTA), 4 x 33 places of the weight rows n % 4, n / 4.
+    static constexpr int PLACES = 132;
+    static constexpr size_t PART = (size_t)NT * PLACES * 4;
 };
+
+__device__ __forceinline__ int place_of(int n) { return n % 4 * 33 + n / 4; }
 
 struct FewBars {
     uint64_t full[LF_MAX_STAGES], empty[LF_MAX_STAGES];
@@ -47,9 +56,10 @@ struct FewBars {
     int abort;
 };
 
-// grid: clusters of S CTAs; LF_THREADS threads; stages of STAGE bytes, then the sums
-// of a split [S][groups of vw rows of x][128][vw].
-template <int NT>
+__device__ __forceinline__ void lf_epi_bar() { asm volatile("bar.sync 1, %0;" ::"n"(LF_EPI * 32) : "memory"); }
+
+// grid: clusters of S CTAs; LF_THREADS threads; stages of STAGE bytes, then the sums.
+template <int NT, bool BF16>
 __global__ void __launch_bounds__(LF_THREADS, NT <= 32 ? 2 : 1)
     k_linear_few(const __grid_constant__ LinArgs g, const __grid_constant__ CUtensorMap tmap_w,
                  const __grid_constant__ CUtensorMap tmap_x)
@@ -161,96 +171,106 @@ __global__ void __launch_bounds__(LF_THREADS, NT <= 32 ? 2 : 1)
         __syncwarp();
     } else {
         // ------------------------------------------------------ epilogue
-        const int q = warp & 3;
+        const int q = warp & 3, row = q * 32 + lane, w0 = warp - 2;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        const int share = NT / S, vw = share >= 4 ? 4 : 2;         // rows of x that end here, and travel together
         int buf = 0;
         uint32_t tphase = 0;
         bool ok = true;
         for (int64_t it = first; it < items; it += step) {
-            const int rb = (int)(it / NC), mc = (int)(it % NC), row = q * 32 + lane, n = rb * LF_BN + row;
-            const int rows = min(NT, g.M - mc * NT);
-            const float bias = S == 1 ? lin_bias(g, n) : 0.0f;
-            // the residual of the next 16 rows is asked for before the sums are waited for
-            float next[16];
+            const int rb = (int)(it / NC), mc = (int)(it % NC), n0 = rb * LF_BN + 4 * lane;
+            const int rows = min(NT, g.M - mc * NT);                // of the item
+            const int m0 = mc * NT + rank * share, mine = max(0, min(share, g.M - m0));      // of this CTA
+            Quad<true> bias;
+            lin_bias4(g, n0, bias);
+            Quad<BF16> next[4];
             auto fetch = [&](int j0) {
-                if (S == 1 && g.res && n < g.N)
+                if (g.res && n0 < g.N)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j0 + j < rows) next[j] = lin_res(g, mc * NT + j0 + j, n);
+                    for (int j = 0; j < 4; ++j)
+                        if (j0 + j < mine) lin_res4(g, m0 + j0 + j, n0, next[j]);
             };
-            fetch(0);
+            fetch(4 * w0);
             if (ok) ok = mm_wait(&sh.tfull[buf], tphase, abort, MM_WAIT_CYCLES, S > 1 ? &sh.since : nullptr);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             if (S > 1) { __syncwarp(); cluster_wait(); }            // one item per cluster (the host's grid)
+            const int place = place_of(row);
 #pragma unroll 1
             for (int j0 = 0; j0 < NT && j0 < rows; j0 += 16) {
-                float d[16], r[16];
+                float d[16];
                 if (ok) tmem_ld16(tmem + lane_base + buf * NT + j0, d);
                 else
 #pragma unroll
                     for (int j = 0; j < 16; ++j) d[j] = 0.0f;
                 if (S == 1) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) r[j] = next[j];
-                    fetch(j0 + 16);
-                    if (ok && n < g.N)
+                    for (int j = 0; j < 16; j += 4)
+                        *reinterpret_cast<float4 *>(part + ((j0 + j) * Sh::PLACES + place * 4)) = make_float4(d[j], d[j + 1], d[j + 2], d[j + 3]);
+                } else if (share >= 4) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (j0 + j < rows) {
-                                float v = lin_act(g.act, g.bf16, d[j] + bias);
-                                if (g.res) v += r[j];
-                                lin_store(g, mc * NT + j0 + j, n, v);
-                            }
+                    for (int j = 0; j < 16; j += 4) {
+                        const int jj = j0 + j;
+                        if (jj < rows)
+                            st_async4(cluster_addr(part + ((rank * share + jj % share) * Sh::PLACES + place * 4), jj / share),
+                                      cluster_addr(&sh.joined, jj / share), d + j);
+                    }
                 } else {
-                    // rows of x travel in groups of 4 (2 where a share has no more)
-                    const int share = NT / S;
-                    if (share >= 4) {
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
-                            const int jj = j0 + j;
-                            if (jj < rows)
-                                st_async4(cluster_addr(part + ((rank * share + jj % share) * LF_BN + row * 4), jj / share),
-                                          cluster_addr(&sh.joined, jj / share), d + j);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            const int jj = j0 + j;
-                            if (jj < rows)
-                                st_async2(cluster_addr(part + (rank * share * LF_BN + row * 2), jj / share),
-                                          cluster_addr(&sh.joined, jj / share), d + j);
-                        }
+                    for (int j = 0; j < 16; j += 2) {
+                        const int jj = j0 + j;
+                        if (jj < rows)
+                            st_async2(cluster_addr(part + (rank * share * Sh::PLACES + place * 2), jj / share),
+                                      cluster_addr(&sh.joined, jj / share), d + j);
                     }
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.tempty[buf]);
+            if (S == 1) {
+                lf_epi_bar();
+            } else if (mine > 0) {
+                if (threadIdx.x == 64) mbar_expect_tx(&sh.joined, S * ((mine + vw - 1) / vw * vw) * LF_BN * 4);
+                ok = __all_sync(0xffffffffu, mm_wait_joined(&sh.joined, abort)) && ok;
+            }
+#pragma unroll 1
+            for (int j0 = 4 * w0; j0 < mine; j0 += 4 * LF_EPI) {
+                float v[4][4];                                       // [row][column]
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j][c] = 0.0f;
+                for (int s = 0; s < S; ++s)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int at = c * 33 + lane;
+                        if (vw == 4) {
+                            const float4 p = *reinterpret_cast<const float4 *>(part + ((s * share + j0) * Sh::PLACES + at * 4));
+                            v[0][c] += p.x; v[1][c] += p.y; v[2][c] += p.z; v[3][c] += p.w;
+                        } else {
+                            const float2 p = *reinterpret_cast<const float2 *>(part + (s * share * Sh::PLACES + at * 2));
+                            v[0][c] += p.x; v[1][c] += p.y;
+                        }
+                    }
+                Quad<BF16> r[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = next[j];
+                fetch(j0 + 4 * LF_EPI);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) lin_add4(v[j], bias);
+                lin_act<BF16>(g.act, v);
+                if (ok && n0 < g.N)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j0 + j < mine) lin_store4(g, m0 + j0 + j, n0, v[j], r[j]);
+            }
+            if (S == 1) lf_epi_bar();                               // the sums have been read
             buf ^= 1;
             if (buf == 0) tphase ^= 1;
         }
     }
-    if (S > 1) {
-        __syncwarp();
-        if (warp < 2) cluster_wait();
-        const int rb = (int)(first / NC), mc = (int)(first % NC), share = NT / S, vw = share >= 4 ? 4 : 2;
-        const int m0 = mc * NT + rank * share;                 // this CTA's rows of x: m0 .. m0 + rows - 1
-        const int rows = max(0, min(share, g.M - m0)), sent = (rows + vw - 1) / vw * vw;
-        if (sent > 0) {
-            if (threadIdx.x == 0) mbar_expect_tx(&sh.joined, S * sent * LF_BN * 4);
-            if (mm_wait_joined(&sh.joined, abort))
-                for (int i = threadIdx.x; i < rows * LF_BN; i += LF_THREADS) {
-                    const int j = i / LF_BN, row = i % LF_BN, n = rb * LF_BN + row;
-                    if (n >= g.N) continue;
-                    const float r = g.res ? lin_res(g, m0 + j, n) : 0.0f;
-                    float v = 0.0f;
-                    for (int s = 0; s < S; ++s) v += part[(s * share + j / vw * vw) * LF_BN + row * vw + j % vw];
-                    v = lin_act(g.act, g.bf16, v + lin_bias(g, n));
-                    lin_store(g, m0 + j, n, g.res ? v + r : v);
-                }
-        }
-    }
+    if (S > 1 && warp < 2) { __syncwarp(); cluster_wait(); }
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -284,31 +304,58 @@ int resident(int S)
     cfg.dynamicSmemBytes = MM_SMEM_LIMIT - 1024;
     cfg.attrs = a;
     cfg.numAttrs = 1;
-    if (allow_smem(once, k_linear_few<16>, MM_SMEM_LIMIT - 1024) != cudaSuccess) return 0;
-    if (cudaOccupancyMaxActiveClusters(&n, k_linear_few<16>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    if (allow_smem(once, k_linear_few<16, true>, MM_SMEM_LIMIT - 1024) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveClusters(&n, k_linear_few<16, true>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
     if (dev < MAX_DEVICES) known[dev][i].store(n + 1, std::memory_order_relaxed);
     return n;
 }
 
+// The launch's shape by its estimated time in us, from times measured on GB300 with
+// bias, SiLU and residual, all from HBM:
+//   few rows   a stage (two K blocks) takes a CTA 0.30 us (NT = 16), 0.33 (32) or 0.42
+//              (64) (1 x 4096 x 4096 without a split 14.3, 64 x 4096 x 16384 52), an item
+//              1.5 more, with two CTAs on an SM 1.43 times as long; joining a split 1;
+//              the weights stream at 6.3 TB/s (64 x 16384 x 4096: 28)
+//   many rows  0.59 for a stage of a 256 x 256 tile, 12 to start and for the last tile's
+//              epilogue (500 x 500 x 64: 12.3, 2048 x 4096 x 4096 in two rounds: 53), 7 at
+//              least from tile to tile, the weights' stream at 5 TB/s
+// At 128 x 4096 x 16384 the choice is NT = 64 with S = 2 (33.8; many rows with S = 2:
+// 52.8), at 512 x 4096 x 4096 many rows with S = 2 (24; without a split 32, NT = 64: 36).
 LinPlan plan_linear(int M, int N, int KB, int sms)
 {
-    if (M > 128) {
-        const int64_t tiles = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
-        int S = 1;
-        for (int s = 2; s <= 4; s *= 2)
-            if (tiles <= resident(2 * s) && KB >= 16 * s) S = s;
-        return {0, S};
-    }
-    const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    const int64_t items = (int64_t)((N + LF_BN - 1) / LF_BN) * ((M + NT - 1) / NT);
-    int S = 1;
     const int KP = (KB + LF_SKB - 1) / LF_SKB;
-    for (int s = 2; s <= 8 && items * s <= sms && KP >= 2 * s; s *= 2)
-        if (items <= resident(s)) S = s;
-    return {NT, S};
+    const float bytes = 2.0f * N * KB * LK;
+    LinPlan best{16, 1};
+    float least = INFINITY;
+    const auto offer = [&](int NT, int S, float us) {
+        if (us < least) { least = us; best = {NT, S}; }
+    };
+    const float stage[3] = {0.30f, 0.33f, 0.42f};
+    for (int i = 0, NT = 16; i < 3; ++i, NT *= 2) {
+        const int64_t items = (int64_t)((N + LF_BN - 1) / LF_BN) * ((M + NT - 1) / NT);
+        const int per_sm = NT <= 32 && items >= 2 * sms ? 2 : 1;
+        const float stream = bytes / 6.3e6f, rounds = (float)((items + per_sm * sms - 1) / (per_sm * sms));
+        for (int S = 1; S <= 8 && 2 * S <= KP + 1; S *= 2) {
+            if (S > 1 && items > resident(S)) break;
+            const float work = rounds * ((KP + S - 1) / S * stage[i] + 1.5f) * (per_sm == 2 ? 1.43f : 1.0f);
+            offer(NT, S, 3.5f + 0.02f * NT + (S > 1 ? 1.0f : 0.0f) + (work > stream ? work : stream));
+        }
+        if (M <= NT) break;
+    }
+    if (M > 64) {
+        const int64_t tiles = (int64_t)((M + 255) / 256) * ((N + 255) / 256), pairs = sms / 2;
+        const float stream = bytes / 5e6f;
+        for (int S = 1; S <= 4 && S <= KP; S *= 2) {
+            if (S > 1 && tiles > resident(2 * S)) break;
+            const float tile = 0.59f * ((KP + S - 1) / S), rounds = S > 1 ? 1.0f : (float)((tiles + pairs - 1) / pairs);
+            const float work = tile + (rounds - 1.0f) * (tile > 7.0f ? tile : 7.0f);
+            offer(0, S, 12.0f + (work > stream ? work : stream));
+        }
+    }
+    return best;
 }
 
-template <int NT>
+template <int NT, bool BF16>
 int launch_few(LinArgs g, int S, const void *x, int64_t ldx, const void *w, int64_t ldw, int sms, cudaStream_t st)
 {
     using Sh = FewShape<NT>;
@@ -318,13 +365,13 @@ int launch_few(LinArgs g, int S, const void *x, int64_t ldx, const void *w, int6
     // two CTAs per SM where there are many items, so that one streams while the other
     // starts, drains or stores
     const int per_sm = NT <= 32 && items >= 2 * sms ? 2 : 1;
-    const size_t fixed = 1024 + (S > 1 ? Sh::PART : 0) + 1024;
+    const size_t fixed = 1024 + Sh::PART + 1024;
     g.stages = (int)((MM_SMEM_LIMIT / per_sm - fixed) / Sh::STAGE);
     if (g.stages > LF_MAX_STAGES) g.stages = LF_MAX_STAGES;
     if (S > 1 && g.stages > want) g.stages = want;          // a cluster has one item
     const size_t smem = fixed - 1024 + (size_t)g.stages * Sh::STAGE;
     static OncePerDevice once;
-    XH_CUDA(allow_smem(once, k_linear_few<NT>, MM_SMEM_LIMIT - 1024));
+    XH_CUDA(allow_smem(once, k_linear_few<NT, BF16>, MM_SMEM_LIMIT - 1024));
     // by K blocks only where they are whole: past the last one the rows' padding
     // would be read
     CUtensorMap tw{}, tx{};
@@ -335,7 +382,7 @@ int launch_few(LinArgs g, int S, const void *x, int64_t ldx, const void *w, int6
                               tmap_bytes(&tx, x, (uint64_t)g.K * 2, (uint64_t)g.M, (uint64_t)ldx * 2, 128, NT);
     if (!ok) return XPRESS_ERR_CUDA;
     const int64_t grid = S > 1 ? items * S : items < per_sm * sms ? items : per_sm * sms;
-    XH_CUDA(launch_head(k_linear_few<NT>, dim3((unsigned)grid), LF_THREADS, smem, st, (unsigned)S, g, tw, tx));
+    XH_CUDA(launch_head(k_linear_few<NT, BF16>, dim3((unsigned)grid), LF_THREADS, smem, st, (unsigned)S, g, tw, tx));
     return XPRESS_OK;
 }
 
@@ -369,15 +416,18 @@ extern "C" int xpress_linear(const xpress_linear_args *in, void *ws, size_t ws_b
     g.out = in->out; g.ldo = in->ldo;
     g.act = in->act;
     g.bf16 = bf16;
-    g.vec = aligned(g.out, 16) && g.ldo * es % 16 == 0 && (!g.res || (aligned(g.res, 16) && g.ldr * es % 16 == 0));
-    g.pairs = aligned(g.out, 4 * es) && g.ldo % 4 == 0 && (!g.res || (aligned(g.res, 4 * es) && g.ldr % 4 == 0));
+    g.quads = aligned(g.out, 4 * es) && g.ldo % 4 == 0 && aligned(g.bias, 8) && (!g.res || (aligned(g.res, 4 * es) && g.ldr % 4 == 0));
     g.status = static_cast<int32_t *>(ws);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const LinPlan p = plan_linear(in->M, in->N, (in->K + LK - 1) / LK, sms);
-    if (p.NT == 16) return launch_few<16>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
-    if (p.NT == 32) return launch_few<32>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
-    if (p.NT == 64) return launch_few<64>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
-    if (p.NT == 128) return launch_few<128>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
+    const auto few = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        return bf16 ? launch_few<NT, true>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st)
+                    : launch_few<NT, false>(g, p.S, in->x, in->ldx, in->w, in->ldw, sms, st);
+    };
+    if (p.NT == 16) return few(std::integral_constant<int, 16>());
+    if (p.NT == 32) return few(std::integral_constant<int, 32>());
+    if (p.NT == 64) return few(std::integral_constant<int, 64>());
     g.S = p.S;
     return launch_lin_wide(g, in->x, in->ldx, in->w, in->ldw, sms, st);
 }

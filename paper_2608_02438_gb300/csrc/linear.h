@@ -16,8 +16,7 @@ struct LinArgs {
     int64_t ldo;
     int act;                       // xpress_act
     int bf16;                      // type of out and res
-    int vec;                       // out's and res's rows start on 16 bytes
-    int pairs;                     // ... on 4 elements
+    int quads;                     // bias, and out's and res's rows, start on 4 elements
     int stages;
     int32_t *status;
 };
@@ -64,24 +63,100 @@ __device__ __forceinline__ void tc_mma_bf16_kblock(uint32_t d_tmem, uint32_t a_l
 
 // act(t).  Outputs in bf16 take the fast exponential and division (about 2^-21 off,
 // under a tenth of their rounding); the tail of GELU needs erfc, not 1 + erf.
-__device__ __forceinline__ float lin_act(int act, bool bf16, float t)
+// (One branch for sixteen values: with one for each, and the way through unrolled, the
+// epilogue's code was fetched from L2 in every tile, 10 us of it for 256 x 256.)
+template <bool BF16> __device__ __forceinline__ void lin_act(int act, float (&v)[4][4])
 {
-    if (act == XPRESS_ACT_SILU) return bf16 ? __fdividef(t, 1.0f + __expf(-t)) : t / (1.0f + expf(-t));
-    if (act == XPRESS_ACT_GELU) return 0.5f * t * erfcf(-0.70710678118654752f * t);
-    if (act == XPRESS_ACT_RELU) return t < 0.0f ? 0.0f : t;      // a NaN stays
-    return t;
+    float *t = v[0];
+    // four values at a time: the others keep their registers to themselves
+    const auto hold = [&] {
+        asm volatile("" : "+f"(t[0]), "+f"(t[1]), "+f"(t[2]), "+f"(t[3]), "+f"(t[4]), "+f"(t[5]), "+f"(t[6]), "+f"(t[7]),
+                     "+f"(t[8]), "+f"(t[9]), "+f"(t[10]), "+f"(t[11]), "+f"(t[12]), "+f"(t[13]), "+f"(t[14]), "+f"(t[15]));
+    };
+    if (act == XPRESS_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            t[j] = BF16 ? __fdividef(t[j], 1.0f + __expf(-t[j])) : t[j] / (1.0f + expf(-t[j]));
+            if (!BF16 && j % 4 == 3) hold();
+        }
+    } else if (act == XPRESS_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            t[j] = 0.5f * t[j] * erfcf(-0.70710678118654752f * t[j]);
+            if (j % 2 == 1) hold();
+        }
+    } else if (act == XPRESS_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) t[j] = t[j] < 0.0f ? 0.0f : t[j];       // a NaN stays
+    }
 }
 
-__device__ __forceinline__ float lin_bias(const LinArgs &g, int n) { return g.bias && n < g.N ? bf2f(g.bias[n]) : 0.0f; }
-__device__ __forceinline__ float lin_res(const LinArgs &g, int m, int n)
+// Four consecutive columns n .. of a row: what is read of them ahead of time (out's
+// type: two or four words; bias: two), and the way through the epilogue.
+template <bool BF16> struct Quad {
+    uint32_t w[BF16 ? 2 : 4];
+
+    __device__ __forceinline__ float operator[](int j) const
+    {
+        return BF16 ? __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16) : __uint_as_float(w[BF16 ? 0 : j]);
+    }
+    // From p; `whole`: 16 (8) bytes at once, else the first `n` of the four.
+    __device__ __forceinline__ void load(const void *p, bool whole, int n)
+    {
+        if (whole) {
+            if (BF16) {
+                const uint2 x = *static_cast<const uint2 *>(p);
+                w[0] = x.x;
+                w[1] = x.y;
+            } else {
+                const uint4 x = *static_cast<const uint4 *>(p);
+                w[0] = x.x; w[1] = x.y; w[BF16 ? 0 : 2] = x.z; w[BF16 ? 0 : 3] = x.w;
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (BF16) {
+                const uint32_t v = j < n ? static_cast<const uint16_t *>(p)[j] : 0u;
+                w[j / 2] = j % 2 ? w[j / 2] | v << 16 : v;
+            } else {
+                w[BF16 ? 0 : j] = j < n ? static_cast<const uint32_t *>(p)[j] : 0u;
+            }
+        }
+    }
+};
+template <bool BF16> __device__ __forceinline__ void lin_res4(const LinArgs &g, int m, int n, Quad<BF16> &r)
 {
-    return ld_any(g.res, g.bf16, (size_t)((int64_t)m * g.ldr + n));
+    r.load(static_cast<const uint8_t *>(g.res) + ((int64_t)m * g.ldr + n) * (BF16 ? 2 : 4), g.quads && n + 4 <= g.N, g.N - n);
 }
-__device__ __forceinline__ void lin_store(const LinArgs &g, int m, int n, float v)
+__device__ __forceinline__ void lin_bias4(const LinArgs &g, int n, Quad<true> &b)
 {
+    b.w[0] = b.w[1] = 0;
+    if (g.bias && n < g.N) b.load(g.bias + n, g.quads && n + 4 <= g.N, g.N - n);
+}
+template <bool BF16>
+__device__ __forceinline__ void lin_store4(const LinArgs &g, int m, int n, float (&v)[4], const Quad<BF16> &r)
+{
+    if (g.res)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += r[j];
     const int64_t at = (int64_t)m * g.ldo + n;
-    if (g.bf16) static_cast<uint16_t *>(g.out)[at] = f2bf(v);
-    else static_cast<float *>(g.out)[at] = v;
+    if (g.quads && n + 4 <= g.N) {
+        if (BF16) *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(g.out) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        else *reinterpret_cast<float4 *>(static_cast<float *>(g.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (n + j < g.N) {
+            if (BF16) static_cast<uint16_t *>(g.out)[at + j] = f2bf(v[j]);
+            else static_cast<float *>(g.out)[at + j] = v[j];
+        }
+}
+__device__ __forceinline__ void lin_add4(float (&v)[4], const Quad<true> &b)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += b[j];
 }
 
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z)

@@ -14,10 +14,14 @@
 // memory, which the receiver's mbarrier counts), which adds them in rank order, so
 // that the result does not depend on timing.
 //
-// Roles (384 threads): warp 0 TMA producer (two K blocks of 128 rows per copy; both
+// Roles (640 threads): warp 0 TMA producer (two K blocks of 128 rows per copy; both
 // CTAs load their own halves, the copies complete on the pair leader's barrier),
-// warp 1 TMEM allocator and, in the leader, MMA issuer; warps 4-11 epilogue (lane
-// quarter warp % 4, column half (warp - 4) / 4).
+// warp 1 TMEM allocator and, in the leader, MMA issuer; warps 4-19 epilogue (lane
+// quarter warp % 4, 64 columns (warp - 4) / 4), 16 columns at a time by way of shared
+// memory, so that four lanes store consecutive outputs of a row; the residual is read
+// the same way, 16 columns ahead.
+#include <type_traits>
+
 #include "linear.h"
 
 namespace xp {
@@ -25,7 +29,8 @@ namespace xp {
 namespace {
 
 constexpr int LW_BM = 256, LW_BN = 256;                 // tile of a pair
-constexpr int LW_EPI = 8;
+constexpr int LW_EPI = 16;
+constexpr int LW_COLS = 64;                             // columns of an epilogue warp
 constexpr int LW_THREADS = 32 * (4 + LW_EPI);
 constexpr uint32_t LW_HALF = 128 * 128;                 // 16 KB: a K block of 128 rows of an operand
 constexpr int LW_SKB = 2;                               // K blocks of a stage
@@ -33,7 +38,7 @@ constexpr uint32_t LW_OPND = LW_SKB * LW_HALF;
 constexpr uint32_t LW_STAGE = 2 * LW_OPND;              // x's K blocks, then w's
 constexpr int LW_STAGES = 3;
 constexpr uint32_t LW_IDESC = idesc_bf16(LW_BM, LW_BN);
-constexpr size_t LW_TILE = 32 * 33 * 4;                 // a warp's transpose
+constexpr size_t LW_TILE = 32 * 16 * 4;                 // a warp's transpose
 constexpr size_t LW_SMEM = 1024 + LW_STAGES * LW_STAGE + LW_EPI * LW_TILE;
 constexpr int LW_BAND = 16;                             // row tiles that share the weights while they are in L2
 // Sums of a split tile: 4 columns of the CTA's 128 rows, then the next 4, four banks on.
@@ -113,59 +118,13 @@ __device__ __forceinline__ void tile_at(int64_t t, int MT, int NT, int &row, int
     col = (int)(in / rows) * LW_BN;
 }
 
-// 8 consecutive elements of a row in 16-byte accesses.
-__device__ __forceinline__ void load_res8(const LinArgs &g, int64_t at, float (&v)[8])
-{
-    if (g.bf16) load8(static_cast<const uint16_t *>(g.res) + at, v);
-    else load8(static_cast<const float *>(g.res) + at, v);
-}
-__device__ __forceinline__ void store_out8(const LinArgs &g, int64_t at, const float (&v)[8])
-{
-    if (g.bf16) store8(static_cast<uint16_t *>(g.out) + at, v);
-    else store8(static_cast<float *>(g.out) + at, v);
-}
-
-// The warp's 32 rows by 32 columns of sums, d of row `lane`, through the epilogue to
-// rows m0 .. and columns n0 .. of out.
-__device__ __forceinline__ void emit32(const LinArgs &g, int m0, int n0, const float (&d)[32], float (*tp)[33])
-{
-    const int lane = threadIdx.x % 32, rows = min(32, g.M - m0);
-    if (rows <= 0 || n0 >= g.N) return;
-    if (g.vec && n0 + 32 <= g.N) {
-        if (lane >= rows) return;
-#pragma unroll
-        for (int c = 0; c < 32; c += 8) {
-            float v[8], r[8];
-            if (g.res) load_res8(g, (int64_t)(m0 + lane) * g.ldr + n0 + c, r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = lin_act(g.act, g.bf16, d[c + j] + (g.bias ? bf2f(g.bias[n0 + c + j]) : 0.0f));
-                if (g.res) v[j] += r[j];
-            }
-            store_out8(g, (int64_t)(m0 + lane) * g.ldo + n0 + c, v);
-        }
-        return;
-    }
-    // rows that start anywhere, or a partial tile: transposed, so that a warp stores
-    // consecutive elements
-#pragma unroll
-    for (int j = 0; j < 32; ++j) tp[lane][j] = d[j];
-    __syncwarp();
-    const int n = n0 + lane;
-    if (n < g.N) {
-        const float b = lin_bias(g, n);
-        for (int r = 0; r < rows; ++r) {
-            float v = lin_act(g.act, g.bf16, tp[r][lane] + b);
-            if (g.res) v += lin_res(g, m0 + r, n);
-            lin_store(g, m0 + r, n, v);
-        }
-    }
-    __syncwarp();
-}
+// Where a warp's transpose keeps the four columns 4 c .. of a row: so that eight lanes'
+// accesses by rows as well as by columns hit different banks.
+__device__ __forceinline__ float4 *quad_of(float4 *tp, int row, int c) { return tp + row * 4 + (c ^ (row >> 1 & 3)); }
 
 // grid: pairs of CTAs that take tile after tile (S = 1), or a cluster of S pairs for
 // each tile; LW_THREADS threads, LW_SMEM bytes.
-template <int S>
+template <int S, bool BF16>
 __global__ void __launch_bounds__(LW_THREADS, 1)
     k_linear_wide(const __grid_constant__ LinArgs g, const __grid_constant__ CUtensorMap tmap_x,
                   const __grid_constant__ CUtensorMap tmap_w)
@@ -286,101 +245,148 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
         __syncwarp();
     } else if (warp >= 4) {
         // ------------------------------------------------------ epilogue
-        const int q = warp & 3, half = (warp - 4) / 4;
-        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + half * 128;
+        const int q = warp & 3, part = (warp - 4) / 4, cl = lane % 4, rl = lane / 4;
+        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + part * LW_COLS;
         const uint32_t tempty0 = cluster_addr(&sh.tempty[0], crank & ~1);
-        float (*tp)[33] = reinterpret_cast<float (*)[33]>(base + LW_STAGES * LW_STAGE + (warp - 4) * LW_TILE);
+        float4 *tp = reinterpret_cast<float4 *>(base + LW_STAGES * LW_STAGE + (warp - 4) * LW_TILE);
+        // of a split tile: this thread's quads of the pair's columns, 8 lanes to 32 columns of a row
+        constexpr int share = LW_BN / S, QPT = share / 4 * 128 / (LW_EPI * 32), JOIN = S == 1 ? 1 : QPT;
+        Quad<true> jbias[JOIN];
+        Quad<BF16> jres[JOIN];
+        auto quad_at = [&](int k, int &r, int &c) {
+            const int i = k * LW_EPI * 32 + (int)threadIdx.x - 128;
+            c = i % 8 * 4 + i / (8 * 128) * 32;
+            r = i / 8 % 128;
+        };
+        if (S > 1) {
+            int row, col;
+            tile_at(first, MT, NT, row, col);
+#pragma unroll
+            for (int k = 0; k < JOIN; ++k) {
+                int r, c;
+                quad_at(k, r, c);
+                const int m = row + rank * 128 + r, n = col + split * share + c;
+                lin_bias4(g, n, jbias[k]);
+                if (g.res && m < g.M && n < g.N) lin_res4(g, m, n, jres[k]);
+            }
+        }
+        // The residual of this warp's part of a tile on its way to L2, a tile ahead.
+        auto to_l2 = [&](int row, int col) {
+            const int m = row + rank * 128 + q * 32 + lane;
+            if (!g.res || m >= g.M) return;
+#pragma unroll
+            for (int c = 0; c < LW_COLS; c += BF16 ? 64 : 32) {
+                const int n = min(col + part * LW_COLS + c, g.N - 1);
+                const uint8_t *p = static_cast<const uint8_t *>(g.res) + ((int64_t)m * g.ldr + n) * (BF16 ? 2 : 4);
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+            }
+        };
         int buf = 0;
         uint32_t tphase = 0;
         bool ok = true;
         for (int64_t t = first; t < tiles; t += step) {
             int row, col;
             tile_at(t, MT, NT, row, col);
-            const int m0 = row + rank * 128 + q * 32, n0 = col + half * 128;
+            const int m0 = row + rank * 128 + q * 32, n0 = col + part * LW_COLS;
+            if (S == 1) {
+                if (t == first) to_l2(row, col);
+                if (t + step < tiles) {
+                    tile_at(t + step, MT, NT, row, col);
+                    to_l2(row, col);
+                }
+            }
+            // rows m0 + rl + 8 i, columns c + 4 cl .. of each 16: what the epilogue reads of them
+            // 32 columns ahead
+            Quad<true> bias[2];
+            Quad<BF16> next[2][4];
+            auto fetch = [&](int c, int h) {
+                const int n = n0 + c + 16 * h + 4 * cl;
+                lin_bias4(g, n, bias[h]);
+                if (g.res && n < g.N)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (m0 + rl + 8 * i < g.M) lin_res4(g, m0 + rl + 8 * i, n, next[h][i]);
+            };
+            if (S == 1) {
+                fetch(0, 0);
+                fetch(0, 1);
+            }
             if (ok) ok = wait_cluster(&sh.tfull[buf], tphase, abort);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok && S == 1) break;
             tc_fence_after();
             if (S > 1) { cluster_arrive(); cluster_wait(); }        // no CTA reads its stages any more
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                float d[32];
-                if (ok) tmem_ld32(taddr + buf * LW_BN + c * 32, d);
-                else
+            for (int c = 0; c < LW_COLS; c += 32)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) d[j] = 0.0f;
-                if (c == 3 && S == 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(tempty0 + buf * 8);
-                }
-                if (S == 1) {
-                    emit32(g, m0, n0 + c * 32, d, tp);
-                } else {
-                    constexpr int share = LW_BN / S;                 // columns of a pair
-                    const int cc = half * 128 + c * 32, dst = cc / share * 2 + rank;
-                    const uint32_t there = cluster_addr(base, dst), bar = cluster_addr(&sh.joined, dst);
+                for (int h = 0; h < 2; ++h) {
+                    float d[16];
+                    if (ok) tmem_ld16(taddr + buf * LW_BN + c + 16 * h, d);
+                    else
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4)
-                        st_async4(there + (((split * share + cc % share + j) / 4) * LW_GROUP4 + (q * 32 + lane) * 4) * 4, bar, d + j);
+                        for (int j = 0; j < 16; ++j) d[j] = 0.0f;
+                    if (S == 1) {
+                        if (c + 16 * h + 16 == LW_COLS) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_cluster(tempty0 + buf * 8);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) *quad_of(tp, lane, j) = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
+                        __syncwarp();
+                        float v[4][4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 p = *quad_of(tp, rl + 8 * i, cl);
+                            v[i][0] = p.x; v[i][1] = p.y; v[i][2] = p.z; v[i][3] = p.w;
+                            lin_add4(v[i], bias[h]);
+                        }
+                        lin_act<BF16>(g.act, v);
+                        const int n = n0 + c + 16 * h + 4 * cl;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (m0 + rl + 8 * i < g.M && n < g.N) lin_store4(g, m0 + rl + 8 * i, n, v[i], next[h][i]);
+                        if (c + 32 < LW_COLS) fetch(c + 32, h);
+                        __syncwarp();
+                    } else {
+                        const int cc = part * LW_COLS + c + 16 * h, dst = cc / share * 2 + rank;
+                        const uint32_t there = cluster_addr(base, dst), bar = cluster_addr(&sh.joined, dst);
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4)
+                            st_async4(there + (((split * share + cc % share + j) / 4) * LW_GROUP4 + (q * 32 + lane) * 4) * 4, bar, d + j);
+                    }
                 }
-            }
             buf ^= 1;
             if (buf == 0) tphase ^= 1;
         }
         if (S > 1) {
-            // the pair's columns, added in rank order: 8 lanes to 32 columns of a row
-            constexpr int share = LW_BN / S;
+            // the pair's columns, added in rank order
             int row, col;
             tile_at(first, MT, NT, row, col);
-            row += rank * 128;
-            col += split * share;
             if (threadIdx.x == 128) mbar_expect_tx(&sh.joined, LW_BN * 128 * 4);
             const bool got = __all_sync(0xffffffffu, mm_wait_joined(&sh.joined, abort));
             const float *sums = reinterpret_cast<const float *>(base);
-            const int w8 = warp - 4;
-            for (int c = 0; c < share && got; c += 32) {
-                const int cl = c + lane % 8 * 4, n = col + cl;
-                float b[4];
+            // four at a time
+            float v[4][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) b[j] = lin_bias(g, n + j);
-#pragma unroll 1
-                for (int i = lane / 8; i < 16; i += 4) {
-                    const int r = w8 * 16 + i, m = row + r;
-                    if (m >= g.M || n >= g.N) continue;
-                    const bool quad = g.pairs && n + 4 <= g.N;
-                    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f}, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (g.res) {
-                        const int64_t at = (int64_t)m * g.ldr + n;
-                        if (quad && g.bf16) {
-                            const uint2 p = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(g.res) + at);
-                            x[0] = __uint_as_float(p.x << 16); x[1] = __uint_as_float(p.x & 0xffff0000u);
-                            x[2] = __uint_as_float(p.y << 16); x[3] = __uint_as_float(p.y & 0xffff0000u);
-                        } else if (quad) {
-                            const float4 p = *reinterpret_cast<const float4 *>(static_cast<const float *>(g.res) + at);
-                            x[0] = p.x; x[1] = p.y; x[2] = p.z; x[3] = p.w;
-                        } else {
+            for (int k = 0; k < JOIN; ++k) {
+                int r, c;
+                quad_at(k, r, c);
+                float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (n + j < g.N) x[j] = lin_res(g, m, n + j);
-                        }
-                    }
+                for (int s = 0; s < S; ++s) {
+                    const float4 p = *reinterpret_cast<const float4 *>(sums + ((s * share + c) / 4) * LW_GROUP4 + r * 4);
+                    a.x += p.x; a.y += p.y; a.z += p.z; a.w += p.w;
+                }
+                v[k % 4][0] = a.x; v[k % 4][1] = a.y; v[k % 4][2] = a.z; v[k % 4][3] = a.w;
+                lin_add4(v[k % 4], jbias[k]);
+                if (k % 4 != 3) continue;
+                lin_act<BF16>(g.act, v);
 #pragma unroll
-                    for (int k = 0; k < S; ++k) {
-                        const float4 p = *reinterpret_cast<const float4 *>(sums + ((k * share + cl) / 4) * LW_GROUP4 + r * 4);
-                        v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = lin_act(g.act, g.bf16, v[j] + b[j]) + x[j];
-                    const int64_t at = (int64_t)m * g.ldo + n;
-                    if (quad && g.bf16)
-                        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(g.out) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-                    else if (quad)
-                        *reinterpret_cast<float4 *>(static_cast<float *>(g.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
-                    else
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (n + j < g.N) lin_store(g, m, n + j, v[j]);
+                for (int i = k - 3; i <= k; ++i) {
+                    quad_at(i, r, c);
+                    const int m = row + rank * 128 + r, n = col + split * share + c;
+                    if (got && m < g.M && n < g.N) lin_store4(g, m, n, v[i % 4], jres[i]);
                 }
             }
         }
@@ -397,12 +403,12 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
     if (threadIdx.x == 0 && sh.abort) set_status(g.status, ST_TIMEOUT);
 }
 
-template <int S>
+template <int S, bool BF16>
 int launch(const LinArgs &g, const CUtensorMap &tx, const CUtensorMap &tw, int64_t pairs, cudaStream_t st)
 {
     static OncePerDevice once;
-    XH_CUDA(allow_smem(once, k_linear_wide<S>, LW_SMEM));
-    XH_CUDA(launch_head(k_linear_wide<S>, dim3((unsigned)(2 * pairs)), LW_THREADS, LW_SMEM, st, 2u * S, g, tx, tw));
+    XH_CUDA(allow_smem(once, k_linear_wide<S, BF16>, LW_SMEM));
+    XH_CUDA(launch_head(k_linear_wide<S, BF16>, dim3((unsigned)(2 * pairs)), LW_THREADS, LW_SMEM, st, 2u * S, g, tx, tw));
     return XPRESS_OK;
 }
 
@@ -418,9 +424,13 @@ int launch_lin_wide(const LinArgs &g, const void *x, int64_t ldx, const void *w,
                                         tmap_bytes(&tw, w, (uint64_t)g.K * 2, (uint64_t)g.N, (uint64_t)ldw * 2, 128, 128);
     if (!ok) return XPRESS_ERR_CUDA;
     const int64_t tiles = (int64_t)((g.M + LW_BM - 1) / LW_BM) * ((g.N + LW_BN - 1) / LW_BN);
-    return g.S == 4   ? launch<4>(g, tx, tw, tiles * 4, st)
-           : g.S == 2 ? launch<2>(g, tx, tw, tiles * 2, st)
-                      : launch<1>(g, tx, tw, tiles < sms / 2 ? tiles : sms / 2, st);
+    const auto go = [&](auto bf16) {
+        constexpr bool BF16 = decltype(bf16)::value;
+        return g.S == 4   ? launch<4, BF16>(g, tx, tw, tiles * 4, st)
+               : g.S == 2 ? launch<2, BF16>(g, tx, tw, tiles * 2, st)
+                          : launch<1, BF16>(g, tx, tw, tiles < sms / 2 ? tiles : sms / 2, st);
+    };
+    return g.bf16 ? go(std::true_type()) : go(std::false_type());
 }
 
 }  // namespace xp

@@ -78,7 +78,8 @@ def test_binding_refuses(lib, call):
 def test_variants(tmp_path):
     lib = _library(tmp_path, "linear", "linear_wide")
     lib.xpress_linear.argtypes = [C.POINTER(X.XpressLinearArgs), C.c_void_p, C.c_size_t, C.c_void_p]
-    for M, (N, K) in itertools.product((1, 16, 24, 50, 100, 200, 300, 2000), ((4096, 4096), (500, 16384), (38912, 520))):
-        g = _args(M=M, N=N, K=K, ldx=K, ldw=K, ldo=N, ldr=N)
+    for dt, M, (N, K) in itertools.product((X.XPRESS_F32, X.XPRESS_BF16), (1, 16, 24, 50, 100, 200, 300, 2000),
+                                           ((4096, 4096), (500, 16384), (38912, 520))):
+        g = _args(out_dtype=dt, M=M, N=N, K=K, ldx=K, ldw=K, ldo=N, ldr=N)
         assert lib.xpress_linear(g, 4096, 256, None) == X.XPRESS_OK
     _all_launched(lib)
