@@ -553,7 +553,7 @@ int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_
  *   out     [n_seq * rows, V], pitch ldo, or NULL: the kept logits, mask_value in all
  *           other places; may be logits (same pitch).  For rows that go on to
  *           xpress_accept see mask_value of xpress_process_logits.
- * Masses are compared to about 2^-31 of the row's, in sums that do not depend on
+ * Masses are compared to about 2^-30 of the row's, in sums that do not depend on
  * any order: calls repeat bit for bit.  No workspace; one kernel launch.
  * Errors: INVALID_ARG (NULL logits / temperature, neither tokens nor out, tokens
  * without u, a pitch below V, misaligned pointers), UNSUPPORTED (dtype, V above

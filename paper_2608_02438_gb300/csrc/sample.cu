@@ -22,7 +22,7 @@
 //              contains u Z looks for the element
 //
 // Every decision compares masses.  They are 64-bit fixed-point sums, so that no
-// order of additions matters, of weights to 2^-31 (weight_exact).  Those take about
+// order of additions matters, of weights to 2^-30 (weight_exact2).  Those take about
 // 40 instructions, so passes over a whole row first use the hardware's exponential;
 // where a decision falls within what that may be off, it is taken again with the
 // exact weights.
@@ -32,9 +32,9 @@ namespace xp {
 
 namespace {
 
-// 2^(j / 64) as 33-bit integers, from the exponential's series.
+// 2^(j / 64) 2^30, from the exponential's series.
 struct ExpTable {
-    uint64_t v[64];
+    uint32_t v[64];
 };
 constexpr ExpTable make_exp_table()
 {
@@ -43,7 +43,7 @@ constexpr ExpTable make_exp_table()
         const double x = j * 0.693147180559945309417232 / 64;
         double term = 1.0, sum = 1.0;
         for (int i = 1; i < 24; ++i) { term *= x / i; sum += term; }
-        t.v[j] = (uint64_t)(sum * 4294967296.0 + 0.5);
+        t.v[j] = (uint32_t)(sum * 1073741824.0 + 0.5);
     }
     return t;
 }
@@ -170,37 +170,97 @@ __device__ __forceinline__ Scale make_scale(float m, float T, int bits)
                  fabsf(ph) < 5e5f && reach < 1e30f};
 }
 
-// w = 2^(K (l - m)) as a 64-bit fixed-point number, to 2^-31 of its value (and half a
+// Two values at a time.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pack2(float a, float b)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
+__device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { return fma2(b, both(-1.0f), a); }
+
+// w = 2^(K (l - m)) as a 64-bit fixed-point number, to 2^-30 of its value (and half a
 // unit).  The difference and its product with K are kept in two parts; of the
 // exponent, the steps of 1/64 come from a table, the rest g (|g| <= 1/128) from the
 // series of 2^g - 1, whose fifth term is below 2^-42.
-__device__ __forceinline__ unsigned long long weight_exact(float l, const Scale &s, const unsigned long long *table)
+__device__ __forceinline__ void weight_exact2(float l0, float l1, const Scale &s, const uint32_t *table, unsigned long long (&w)[2])
 {
-    const float dh = __fsub_rn(l, s.m), bb = __fsub_rn(dh, l);
-    const float dl = __fadd_rn(__fsub_rn(l, __fsub_rn(dh, bb)), __fsub_rn(-s.m, bb));
-    const float ph = fmaxf(__fmul_rn(dh, s.kh), -70.0f);            // 2^-70 is below half a unit
-    const float pl = fmaf(dh, s.kh, -ph) + fmaf(dh, s.kl, dl * s.kh);
-    const float steps = rintf(ph * 64.0f);
-    const float g = fmaf(steps, -0.015625f, ph) + pl;
-    const float e = g * fmaf(g, fmaf(g, fmaf(g, 9.61812910e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f);
-    const int i = (int)steps;
-    const unsigned long long t = table[i & 63];
-    const unsigned long long w = t + (unsigned long long)(((long long)t * __float2int_rn(e * 4294967296.0f)) >> 32);
-    // w has 32 bits behind the point, and 2^(i >> 6) to come
-    const int up = s.bits - 32 + (i >> 6), down = min(max(-up, 1), 63);
-    const unsigned long long r = up >= 0 ? w << max(up, 0) : (w + (1ull << (down - 1))) >> down;
-    return l == s.m ? 1ull << s.bits : r;                            // (both may be infinite)
+    const f32x2 l = pack2(l0, l1), nm = both(-s.m), kh = both(s.kh);
+    const f32x2 dh = add2(l, nm), bb = sub2(dh, l), dl = add2(sub2(l, sub2(dh, bb)), sub2(nm, bb));
+    float p[2], steps[2], e[2];
+    unpack2(mul2(dh, kh), p[0], p[1]);
+    p[0] = fmaxf(p[0], -70.0f);                                      // 2^-70 is below half a unit
+    p[1] = fmaxf(p[1], -70.0f);
+    const f32x2 ph = pack2(p[0], p[1]);
+    const f32x2 pl = add2(fma2(dh, kh, mul2(ph, both(-1.0f))), fma2(dh, both(s.kl), mul2(dl, kh)));
+    const f32x2 t = fma2(ph, both(64.0f), both(MAGIC));              // its low bits: 64 ph as an integer
+    const f32x2 g = add2(fma2(add2(t, both(-MAGIC)), both(-0.015625f), ph), pl);
+    unpack2(t, steps[0], steps[1]);
+    f32x2 q = fma2(g, both(9.61812910e-3f), both(5.55041087e-2f));
+    q = fma2(g, q, both(2.40226507e-1f));
+    q = fma2(g, q, both(6.93147181e-1f));
+    unpack2(mul2(mul2(g, q), both(274877906944.0f)), e[0], e[1]);    // (2^g - 1) 2^38
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = (int)(__float_as_uint(steps[k]) - __float_as_uint(MAGIC));
+        const int tj = (int)table[i & 63];                           // 2^(j / 64) 2^30
+        const unsigned long long x = (unsigned long long)((long long)tj * 64 + __mulhi(tj, __float2int_rn(e[k])));
+        // x has 36 bits behind the point, and 2^(i >> 6) to come
+        const int up = s.bits - 36 + (i >> 6), down = min(max(-up, 1), 63);
+        w[k] = up >= 0 ? x << max(up, 0) : (x + (1ull << (down - 1))) >> down;
+    }
+    // (both may be infinite)
+    if (l0 == s.m) w[0] = 1ull << s.bits;
+    if (l1 == s.m) w[1] = 1ull << s.bits;
+}
+__device__ __forceinline__ unsigned long long weight_exact(float l, const Scale &s, const uint32_t *table)
+{
+    unsigned long long w[2];
+    weight_exact2(l, l, s, table, w);
+    return w[0];
 }
 // The same with the hardware's exponential of the exponent's fraction: 2^-22 off, and
 // 2^-24 from the fraction's roundings (K l is split into an integer, its fraction and
 // the product's remainder).
+__device__ __forceinline__ f32x2 weight_fast2(float l0, float l1, const Scale &s)
+{
+    if (!s.near)                                   // (a guess: such rows are summed exactly)
+        return pack2(ex2_approx(fminf(l0 - s.m, 0.0f) * s.kh), ex2_approx(fminf(l1 - s.m, 0.0f) * s.kh));
+    const f32x2 l = pack2(fmaxf(l0, s.floor), fmaxf(l1, s.floor)), kh = both(s.kh);
+    const f32x2 ph = mul2(l, kh), i = add2(ph, both(MAGIC)), n = add2(i, both(-MAGIC));
+    const f32x2 f = add2(sub2(ph, n), add2(fma2(l, kh, mul2(ph, both(-1.0f))), fma2(l, both(s.kl), both(-s.rest))));
+    float f0, f1, i0, i1;
+    unpack2(f, f0, f1);
+    unpack2(i, i0, i1);
+    return pack2(__uint_as_float(__float_as_uint(ex2_approx(f0)) + (__float_as_uint(i0) << 23) + s.back),
+                 __uint_as_float(__float_as_uint(ex2_approx(f1)) + (__float_as_uint(i1) << 23) + s.back));
+}
 __device__ __forceinline__ float weight_fast(float l, const Scale &s)
 {
-    if (!s.near) return ex2_approx(fminf(l - s.m, 0.0f) * s.kh);     // (a guess: such rows are summed exactly)
-    l = fmaxf(l, s.floor);
-    const float ph = __fmul_rn(l, s.kh), i = __fadd_rn(ph, MAGIC);
-    const float f = __fsub_rn(ph, __fsub_rn(i, MAGIC)) + (fmaf(l, s.kh, -ph) + fmaf(l, s.kl, -s.rest));
-    return __uint_as_float(__float_as_uint(ex2_approx(f)) + (__float_as_uint(i) << 23) + s.back);
+    float a, b;
+    unpack2(weight_fast2(l, l, s), a, b);
+    return a;
 }
 // What fast weights may be off, and a sum of them by its own roundings (three levels
 // of 2^-24 each), in 2^-26 of their size, a tenth added; and by fixed-point roundings.
@@ -247,7 +307,7 @@ __device__ __forceinline__ uint32_t ld_cluster1(uint32_t addr)
 __device__ __forceinline__ void cluster_sync() { cluster_arrive(); cluster_wait(); }
 
 template <int SWARPS> struct SampleShared {
-    unsigned long long table[64];                                    // 2^(j / 64)
+    uint32_t table[64];                                              // 2^(j / 64) 2^30
     unsigned long long slot[2][3][MAX_CLUSTER * SWARPS];             // what the cluster's warps exchange: [turn][value][warp]
     unsigned long long scan[2][SWARPS];
     unsigned long long note[4];                                      // written by one thread of the cluster: the id cut, a draw to repeat
@@ -545,28 +605,37 @@ struct Sampler {
             P::unpack(r, v);
             if (EXACT) {
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const unsigned long long w = weight_exact(v[j], s, sh.table);
-                    fixed += v[j] > t ? w : 0ull;
-                    ties += v[j] == t;
+                for (int j = 0; j < E; j += 2) {
+                    unsigned long long w[2];
+                    weight_exact2(v[j], v[j + 1], s, sh.table, w);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        fixed += v[j + k] > t ? w[k] : 0ull;
+                        ties += v[j + k] == t;
+                    }
                 }
             } else {
-                float w[E];
+                f32x2 w[E / 2];
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    w[j] = weight_fast(v[j], s);
+                for (int j = 0; j < E; j += 2) {
+                    w[j / 2] = weight_fast2(v[j], v[j + 1], s);
                     if (!ROW) {
-                        if (!(v[j] > t)) w[j] = 0.0f;
-                        ties += v[j] == t;
+                        float a, b;
+                        unpack2(w[j / 2], a, b);
+                        w[j / 2] = pack2(v[j] > t ? a : 0.0f, v[j + 1] > t ? b : 0.0f);
+                        ties += (v[j] == t) + (v[j + 1] == t);
                     }
                 }
 #pragma unroll
-                for (int o = E / 2; o > 0; o >>= 1)
+                for (int o = E / 4; o > 0; o >>= 1)
 #pragma unroll
-                    for (int j = 0; j < o; ++j) w[j] += w[j + o];
+                    for (int j = 0; j < o; ++j) w[j] = add2(w[j], w[j + o]);
+                float a, c;
+                unpack2(w[0], a, c);
+                a += c;
                 // hi + lo keeps what the addition rounds away
-                const float x = __fadd_rn(hi, w[0]), b = __fsub_rn(x, hi);
-                lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(x, b)), __fsub_rn(w[0], b));
+                const float x = __fadd_rn(hi, a), b = __fsub_rn(x, hi);
+                lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(x, b)), __fsub_rn(a, b));
                 hi = x;
             }
         }
@@ -591,12 +660,16 @@ struct Sampler {
             float v[E];
             P::unpack(r, v);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const unsigned long long w = weight_exact(v[j], s, sh.table);
-                sum += v[j] > t ? w : 0ull;
-                sum0 += v[j] > t0 ? w : 0ull;
-                ties += v[j] == t;
-                ties0 += v[j] == t0;
+            for (int j = 0; j < E; j += 2) {
+                unsigned long long w[2];
+                weight_exact2(v[j], v[j + 1], s, sh.table, w);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    sum += v[j + k] > t ? w[k] : 0ull;
+                    sum0 += v[j + k] > t0 ? w[k] : 0ull;
+                    ties += v[j + k] == t;
+                    ties0 += v[j + k] == t0;
+                }
             }
         }
     }

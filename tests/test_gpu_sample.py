@@ -1,7 +1,7 @@
 """xpress_sample on the GPU against its definition in 64 bits.
 
 Kept places and tokens are whole numbers: they have to be equal, unless the definition's
-own decision is closer to its border than the masses are compared (2^-31 of the row's, by
+own decision is closer to its border than the masses are compared (2^-30 of the row's, by
 the entry point's documentation; taken as 2^-28 here).  Such a row may give either side."""
 import math
 
