@@ -9,23 +9,35 @@
 // T <= 0 keeps the first maximum alone.  All filters keep a prefix of the order, so
 // what is kept is a threshold t, with q of the elements equal to t (the first ones).
 //
-// A cluster of C CTAs takes a row.  The row is read once, into the CTAs' shared
-// memory; every further pass over it stays there.  A thread owns consecutive
-// 16-byte pieces, an odd number of them: the lanes' accesses then hit different
-// banks, and sums per thread, warp and CTA are in the order of the ids.
-//   maximum    with the load; with it the smallest of the maxima of as many groups
-//              of lanes as k needs, a bound below the k-th largest
-//   thresholds by histograms of the order-preserving bits between a lower bound and
-//              the maximum, 2048 bins: one level where these are bf16 values of two
-//              or three octaves, up to three levels for fp32
+// A cluster of C CTAs takes a row.  The row is read once, by asynchronous copies into
+// the CTAs' shared memory; every further pass over it stays there.  A thread owns
+// consecutive 16-byte pieces, an odd number of them: the lanes' accesses then hit
+// different banks, and sums per thread, warp and CTA are in the order of the ids.
+//   maximum    with it the smallest of the maxima of as many groups of lanes as k
+//              needs: a bound below the k-th largest element
+//   the few    where at most 1024 elements can be kept (a small k, greedy rows), they
+//              are gathered in every CTA, which finds the thresholds and draws alone
+//   thresholds else by histograms between a lower bound and the maximum: 1024 bins of
+//              single bf16 values, or of equal width first and of keys after that,
+//              until a bin's largest and smallest elements decide.  By numbers for
+//              top-k; by rounded masses for top-p, which the draw's sums confirm or
+//              move on from
 //   draw       sums per warp, exchanged through the cluster; the warp whose range
 //              contains u Z looks for the element
 //
-// Every decision compares masses.  They are 64-bit fixed-point sums, so that no
-// order of additions matters, of weights to 2^-30 (weight_exact2).  Those take about
-// 40 instructions, so passes over a whole row first use the hardware's exponential;
-// where a decision falls within what that may be off, it is taken again with the
-// exact weights.
+// Every decision compares masses: 64-bit fixed-point sums, in which no order of
+// additions matters, of weights to 2^-30 (weight_exact2, about 28 instructions).
+// Passes over a whole row first use the hardware's exponential (weight_fast2, about
+// 10); where a decision falls within what that may be off, 2^-21 of the mass, it is
+// taken again with exact weights: one row in 200 of a softmax over 15000 likely tokens.
+//
+// Bound by latency: a row is a chain of some ten passes, barriers and scans.  One row
+// of 151936 bf16, top-k 50 and top-p 0.9: 13.6 us (load 1.3, maximum 1.8, the few 3.8,
+// thresholds 3.6, draw 1.4).  32 x 17 truncated rows of it: 192 us, 1.7 TB/s; shared
+// memory holds 76 rows at a time, for 20 us (median) each.  64 rows without filters:
+// 26 us; 5 of a row's 15 are the weights, at the issue limit.  What it took before:
+// one row 19 and 544 rows 443 us with CTAs of two passes per level, 64-bit atomics on
+// masses and 64-bit floating point at two lanes a cycle.
 #include "matmul_fp8.h"
 
 namespace xp {
@@ -1338,17 +1350,20 @@ struct SamplePlan {
     bool resident;
 };
 
-// CTAs of a row's cluster: the fewest that leave two on an SM, more while all rows'
-// CTAs have a place at the same time; the pieces of a CTA and of a thread.
+// CTAs of a row's cluster: the fewest that leave two on an SM; more while they have
+// more than 2048 pieces and all rows' CTAs have a place at the same time (64 rows of
+// 151936 bf16: 4 CTAs, 28 us, 32 with 2; 68 rows of 32000: 2 CTAs, 15 us, 17 with 1, 16
+// with 4).  8 for a few rows only (one row 15 us, 16 with 4; 17 rows 19 with 4, 24 with
+// 8).  The pieces of a CTA and of a thread.
 SamplePlan sample_plan(int64_t n, int V, int E, int sms)
 {
     const int64_t pieces = ((int64_t)V + E - 1 + E - 1) / E;          // wherever the row starts
     auto slice_of = [&](int C) { return (pieces + C - 1) / C; };
     auto threads_of = [&](int C) { return slice_of(C) > 1024 ? 512 : 256; };
     auto bytes = [&](int C) { return (size_t)slice_of(C) * 16 + HIST_BYTES; };
-    auto fits = [&](int C) { return n * C * threads_of(C) <= (int64_t)sms * 1024; };
+    auto fits = [&](int C) { return n * C * threads_of(C) <= (int64_t)sms * 1024 && (C < 8 || n * C <= sms / 2); };
     int C = 1;
-    while (C < MAX_CLUSTER && (bytes(C) > SAMPLE_HALF || (fits(2 * C) && slice_of(C) > 512))) C *= 2;
+    while (C < MAX_CLUSTER && (bytes(C) > SAMPLE_HALF || (fits(2 * C) && slice_of(C) > 2048))) C *= 2;
     const int slice = (int)slice_of(C);
     const bool resident = bytes(C) <= SAMPLE_SMEM;
     const int threads = resident ? threads_of(C) : 512;

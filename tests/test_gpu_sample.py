@@ -352,3 +352,58 @@ def test_rules_then_draw():
     ruled = torch.empty_like(logits)
     X.process_logits(logits, ruled, repetition=torch.full((n,), 1.3, device="cuda"), history=hist, history_offsets=off)
     run(ruled, 0.8, u=torch.rand(n, device="cuda", generator=g), k=50, p=0.9, mask=-8192.0)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("f", [dict(), dict(p=0.9), dict(k=9000, p=0.7), dict(k=100), dict(min_p=0.98), dict(k=1025), dict(k=1024, p=0.5)])
+@pytest.mark.parametrize("V", [20000, 151936])
+def test_flat_rows(dt, f, V):
+    """Logits next to one another: thousands are kept, in bf16 most of them equal."""
+    g = _gen(17)
+    logits = rows_of(3, V, dt, g, 0.02)
+    run(logits, 1.1, u=torch.rand(3, device="cuda", generator=g), **f)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("p", [1e-30, 1e-7, 0.5, 0.9999, 1.0 - 2.0 ** -24])
+@pytest.mark.parametrize("k", [None, 300, 2500])
+def test_extreme_top_p(dt, p, k):
+    g = _gen(18)
+    logits = rows_of(4, 5000, dt, g)
+    # at the last p the tail's masses are below what is told apart: such rows are near
+    run(logits, 1.0, u=torch.rand(4, device="cuda", generator=g), p=p, k=k, most_near=1.0 if p > 0.99 else 0.02)
+
+
+@pytest.mark.parametrize("sizes", [(1, 1), (1024, 1024), (1025, 700), (3000, 1), (3000, 2999)])
+def test_ties_at_the_limit_of_the_few(sizes):
+    """As many equal maxima as are settled at once, one more, and many; k of them are kept."""
+    ties, k = sizes
+    for dt in (BF16, F32):
+        logits = torch.full((2, 20000), -2.0, dtype=dt, device="cuda")
+        logits[:, 3:3 + 5 * ties:5] = 4.0
+        tokens, out = torch.empty(2, dtype=torch.int32, device="cuda"), torch.empty_like(logits)
+        one = lambda v, t: torch.full((2,), v, dtype=t, device="cuda")  # noqa: E731
+        X.sample(logits, one(0.01, F32), u=torch.tensor([0.0, 0.999], device="cuda"), tokens_out=tokens, out=out, top_k=one(k, torch.int32))
+        kept = list(range(3, 3 + 5 * k, 5))
+        assert all((out[i] > -INF).nonzero()[:, 0].tolist() == kept for i in range(2))
+        assert tokens.tolist() == [kept[0], kept[int(0.999 * k)]]
+        X.sample(logits, one(0.0, F32), u=one(0.7, F32), tokens_out=tokens, out=out)          # greedy: the first of them
+        assert tokens.tolist() == [3, 3] and all((out[i] > -INF).nonzero()[:, 0].tolist() == [3] for i in range(2))
+
+
+def test_two_calls_at_once():
+    g = _gen(19)
+    a, b = rows_of(300, 20011, BF16, g), rows_of(200, 9001, F32, g)
+    ua, ub = torch.rand(300, device="cuda", generator=g), torch.rand(200, device="cuda", generator=g)
+    Ta, Tb = torch.full((300,), 0.9, device="cuda"), torch.full((200,), 1.2, device="cuda")
+    pa, kb = torch.full((300,), 0.9, device="cuda"), torch.full((200,), 30, dtype=torch.int32, device="cuda")
+    ta, tb = (torch.empty(n, dtype=torch.int32, device="cuda") for n in (300, 200))
+    oa, ob = torch.empty_like(a), torch.empty_like(b)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        X.sample(a, Ta, u=ua, tokens_out=ta, out=oa, top_p=pa, stream=s1)
+        X.sample(b, Tb, u=ub, tokens_out=tb, out=ob, top_k=kb, stream=s2)
+    torch.cuda.synchronize()
+    check(a, Ta, ua, ta, oa, p=pa)
+    check(b, Tb, ub, tb, ob, k=kb)
