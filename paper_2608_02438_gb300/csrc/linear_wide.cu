@@ -29,8 +29,8 @@ namespace xp {
 namespace {
 
 constexpr int LW_BM = 256, LW_BN = 256;                 // tile of a pair
-constexpr int LW_EPI = 16;
-constexpr int LW_COLS = 64;                             // columns of an epilogue warp
+constexpr int LW_EPI = 8;
+constexpr int LW_COLS = 128;                            // columns of an epilogue warp
 constexpr int LW_THREADS = 32 * (4 + LW_EPI);
 constexpr uint32_t LW_HALF = 128 * 128;                 // 16 KB: a K block of 128 rows of an operand
 constexpr int LW_SKB = 2;                               // K blocks of a stage
@@ -38,7 +38,7 @@ constexpr uint32_t LW_OPND = LW_SKB * LW_HALF;
 constexpr uint32_t LW_STAGE = 2 * LW_OPND;              // x's K blocks, then w's
 constexpr int LW_STAGES = 3;
 constexpr uint32_t LW_IDESC = idesc_bf16(LW_BM, LW_BN);
-constexpr size_t LW_TILE = 32 * 16 * 4;                 // a warp's transpose
+constexpr size_t LW_TILE = 2 * 32 * 16 * 4;             // a warp's transposes
 constexpr size_t LW_SMEM = 1024 + LW_STAGES * LW_STAGE + LW_EPI * LW_TILE;
 constexpr int LW_BAND = 16;                             // row tiles that share the weights while they are in L2
 // Sums of a split tile: 4 columns of the CTA's 128 rows, then the next 4, four banks on.
@@ -47,7 +47,7 @@ static_assert(64 * LW_GROUP4 * 4 <= LW_STAGES * LW_STAGE, "the sums of a split f
 
 struct LinBars {
     uint64_t full[LW_STAGES], empty[LW_STAGES];
-    uint64_t tfull[2], tempty[2];
+    uint64_t tfull[2], tread[2], tempty[2];    // tread: by this CTA's epilogue; tempty (leader): by both CTAs'
     uint64_t drain, joined;
     long long since;
     uint32_t tmem_base;
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < LW_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 2 * LW_EPI); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tread[i], LW_EPI); mbar_init(&sh.tempty[i], 2); }
         mbar_init(&sh.drain, 1);
         mbar_init(&sh.joined, 1);
         sh.abort = 0;
@@ -243,11 +243,27 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
         int dummy = 0;
         mm_wait(&sh.drain, 0, &dummy, MM_WAIT_CYCLES / 20);
         __syncwarp();
+    } else if (warp == 2 && S == 1) {
+        // ------------------------------------ accumulators read, to the leader
+        // (an arrival on another CTA's barrier waits for the thread's stores: the
+        // epilogue's warps would stand still for theirs)
+        if (lane == 0) {
+            int buf = 0;
+            uint32_t tphase = 0;
+            for (int64_t t = first; t < tiles; t += step) {
+                if (!mm_wait(&sh.tread[buf], tphase, abort)) break;
+                tc_fence_after();
+                tc_fence_before();
+                mbar_arrive_cluster(cluster_addr(&sh.tempty[buf], crank & ~1));
+                buf ^= 1;
+                if (buf == 0) tphase ^= 1;
+            }
+        }
+        __syncwarp();
     } else if (warp >= 4) {
         // ------------------------------------------------------ epilogue
         const int q = warp & 3, part = (warp - 4) / 4, cl = lane % 4, rl = lane / 4;
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + part * LW_COLS;
-        const uint32_t tempty0 = cluster_addr(&sh.tempty[0], crank & ~1);
         float4 *tp = reinterpret_cast<float4 *>(base + LW_STAGES * LW_STAGE + (warp - 4) * LW_TILE);
         // of a split tile: this thread's quads of the pair's columns, 8 lanes to 32 columns of a row
         constexpr int share = LW_BN / S, QPT = share / 4 * 128 / (LW_EPI * 32), JOIN = S == 1 ? 1 : QPT;
@@ -295,67 +311,104 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
                     to_l2(row, col);
                 }
             }
-            // rows m0 + rl + 8 i, columns c + 4 cl .. of each 16: what the epilogue reads of them
-            // 32 columns ahead
-            Quad<true> bias[2];
-            Quad<BF16> next[2][4];
-            auto fetch = [&](int c, int h) {
-                const int n = n0 + c + 16 * h + 4 * cl;
-                lin_bias4(g, n, bias[h]);
-                if (g.res && n < g.N)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (m0 + rl + 8 * i < g.M) lin_res4(g, m0 + rl + 8 * i, n, next[h][i]);
+            const auto wait = [&] {
+                if (ok) ok = wait_cluster(&sh.tfull[buf], tphase, abort);
+                ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
             };
             if (S == 1) {
-                fetch(0, 0);
-                fetch(0, 1);
-            }
-            if (ok) ok = wait_cluster(&sh.tfull[buf], tphase, abort);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok && S == 1) break;
-            tc_fence_after();
-            if (S > 1) { cluster_arrive(); cluster_wait(); }        // no CTA reads its stages any more
-#pragma unroll 1
-            for (int c = 0; c < LW_COLS; c += 32)
+                // A tile's part, 16 columns at a time by way of shared memory, what is read for
+                // them 32 columns ahead: rows m0 + rl + 8 i, columns 4 cl .. of each 16.  `whole`:
+                // all of it is inside out, by quads, so that nothing needs a check.
+                const auto part_of_tile = [&](auto whole) {
+                    constexpr bool WHOLE = decltype(whole)::value;
+                    constexpr int ES = BF16 ? 2 : 4;
+                    const int64_t at = (int64_t)(m0 + rl) * g.ldo + n0 + 4 * cl, rat = (int64_t)(m0 + rl) * g.ldr + n0 + 4 * cl;
+                    uint8_t *out = static_cast<uint8_t *>(g.out) + at * ES;
+                    const uint8_t *res = static_cast<const uint8_t *>(g.res) + rat * ES;
+                    const int64_t ostep = 8 * g.ldo * ES, rstep = 8 * g.ldr * ES;
+                    Quad<true> bias[2];
+                    Quad<BF16> next[2][4];
+                    bias[0].w[0] = bias[0].w[1] = bias[1].w[0] = bias[1].w[1] = 0;
+                    const auto fetch = [&](int c, int h) {
+                        const int n = n0 + c + 16 * h + 4 * cl;
+                        if (WHOLE) {
+                            if (g.bias) bias[h].load(g.bias + n, true, 4);
+                        } else {
+                            lin_bias4(g, n, bias[h]);
+                        }
+                        if (g.res)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                            for (int i = 0; i < 4; ++i) {
+                                if (WHOLE) next[h][i].load(res + i * rstep + (c + 16 * h) * ES, true, 4);
+                                else if (n < g.N && m0 + rl + 8 * i < g.M) lin_res4(g, m0 + rl + 8 * i, n, next[h][i]);
+                            }
+                    };
+                    fetch(0, 0);
+                    fetch(0, 1);
+                    wait();
+                    if (!ok) return;
+#pragma unroll 1
+                    for (int c = 0; c < LW_COLS; c += 32)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float d[16];
+                            tmem_ld16(taddr + buf * LW_BN + c + 16 * h, d);
+                            if (h == 1 && c + 32 == LW_COLS) {
+                                tc_fence_before();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&sh.tread[buf]);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) *quad_of(tp + h * 128, lane, j) = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
+                            __syncwarp();
+                            float v[4][4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float4 p = *quad_of(tp + h * 128, rl + 8 * i, cl);
+                                v[i][0] = p.x; v[i][1] = p.y; v[i][2] = p.z; v[i][3] = p.w;
+                                lin_add4(v[i], bias[h]);
+                            }
+                            __syncwarp();
+                            lin_act<BF16>(g.act, v);
+                            const int n = n0 + c + 16 * h + 4 * cl;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if (!WHOLE) {
+                                    if (m0 + rl + 8 * i < g.M && n < g.N) lin_store4(g, m0 + rl + 8 * i, n, v[i], next[h][i]);
+                                    continue;
+                                }
+                                if (g.res)
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) v[i][j] += next[h][i][j];
+                                uint8_t *p = out + i * ostep + (c + 16 * h) * ES;
+                                if (BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[i][0], v[i][1]), pack_bf16(v[i][2], v[i][3]));
+                                else *reinterpret_cast<float4 *>(p) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+                            }
+                            if (c + 32 < LW_COLS) fetch(c + 32, h);
+                        }
+                };
+                if (g.quads && m0 + 32 <= g.M && n0 + LW_COLS <= g.N) part_of_tile(std::true_type());
+                else part_of_tile(std::false_type());
+                if (!ok) break;
+            } else {
+                wait();
+                cluster_arrive();                                    // no CTA reads its stages any more
+                cluster_wait();
+#pragma unroll 1
+                for (int c = 0; c < LW_COLS; c += 16) {
                     float d[16];
-                    if (ok) tmem_ld16(taddr + buf * LW_BN + c + 16 * h, d);
+                    if (ok) tmem_ld16(taddr + buf * LW_BN + c, d);
                     else
 #pragma unroll
                         for (int j = 0; j < 16; ++j) d[j] = 0.0f;
-                    if (S == 1) {
-                        if (c + 16 * h + 16 == LW_COLS) {
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive_cluster(tempty0 + buf * 8);
-                        }
+                    const int cc = part * LW_COLS + c, dst = cc / share * 2 + rank;
+                    const uint32_t there = cluster_addr(base, dst), bar = cluster_addr(&sh.joined, dst);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) *quad_of(tp, lane, j) = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
-                        __syncwarp();
-                        float v[4][4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float4 p = *quad_of(tp, rl + 8 * i, cl);
-                            v[i][0] = p.x; v[i][1] = p.y; v[i][2] = p.z; v[i][3] = p.w;
-                            lin_add4(v[i], bias[h]);
-                        }
-                        lin_act<BF16>(g.act, v);
-                        const int n = n0 + c + 16 * h + 4 * cl;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (m0 + rl + 8 * i < g.M && n < g.N) lin_store4(g, m0 + rl + 8 * i, n, v[i], next[h][i]);
-                        if (c + 32 < LW_COLS) fetch(c + 32, h);
-                        __syncwarp();
-                    } else {
-                        const int cc = part * LW_COLS + c + 16 * h, dst = cc / share * 2 + rank;
-                        const uint32_t there = cluster_addr(base, dst), bar = cluster_addr(&sh.joined, dst);
-#pragma unroll
-                        for (int j = 0; j < 16; j += 4)
-                            st_async4(there + (((split * share + cc % share + j) / 4) * LW_GROUP4 + (q * 32 + lane) * 4) * 4, bar, d + j);
-                    }
+                    for (int j = 0; j < 16; j += 4)
+                        st_async4(there + (((split * share + cc % share + j) / 4) * LW_GROUP4 + (q * 32 + lane) * 4) * 4, bar, d + j);
                 }
+            }
             buf ^= 1;
             if (buf == 0) tphase ^= 1;
         }
