@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(LF_THREADS, NT <= 32 ? 2 : 1)
                 fetch(j0 + 4 * LF_EPI);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) lin_add4(v[j], bias);
-                lin_act<BF16>(g.act, v);
+                lin_act<BF16, 16>(g.act, v[0]);
                 if (ok && n0 < g.N)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)

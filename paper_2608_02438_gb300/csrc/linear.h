@@ -63,31 +63,31 @@ __device__ __forceinline__ void tc_mma_bf16_kblock(uint32_t d_tmem, uint32_t a_l
 
 // act(t).  Outputs in bf16 take the fast exponential and division (about 2^-21 off,
 // under a tenth of their rounding); the tail of GELU needs erfc, not 1 + erf.
-// (One branch for sixteen values: with one for each, and the way through unrolled, the
-// epilogue's code was fetched from L2 in every tile, 10 us of it for 256 x 256.)
-template <bool BF16> __device__ __forceinline__ void lin_act(int act, float (&v)[4][4])
+// (One branch for all N values, 16 or 32: with one for each, and the way through
+// unrolled, the epilogue's code was fetched from L2 in every tile, 10 us of it for
+// 256 x 256.)
+template <bool BF16, int N> __device__ __forceinline__ void lin_act(int act, float *t)
 {
-    float *t = v[0];
-    // four values at a time: the others keep their registers to themselves
-    const auto hold = [&] {
-        asm volatile("" : "+f"(t[0]), "+f"(t[1]), "+f"(t[2]), "+f"(t[3]), "+f"(t[4]), "+f"(t[5]), "+f"(t[6]), "+f"(t[7]),
-                     "+f"(t[8]), "+f"(t[9]), "+f"(t[10]), "+f"(t[11]), "+f"(t[12]), "+f"(t[13]), "+f"(t[14]), "+f"(t[15]));
+    // a few values at a time: the others keep their registers to themselves
+    const auto hold = [&](float *h) {
+        asm volatile("" : "+f"(h[0]), "+f"(h[1]), "+f"(h[2]), "+f"(h[3]), "+f"(h[4]), "+f"(h[5]), "+f"(h[6]), "+f"(h[7]),
+                     "+f"(h[8]), "+f"(h[9]), "+f"(h[10]), "+f"(h[11]), "+f"(h[12]), "+f"(h[13]), "+f"(h[14]), "+f"(h[15]));
     };
     if (act == XPRESS_ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < N; ++j) {
             t[j] = BF16 ? __fdividef(t[j], 1.0f + __expf(-t[j])) : t[j] / (1.0f + expf(-t[j]));
-            if (!BF16 && j % 4 == 3) hold();
+            if (!BF16 && j % 4 == 3) hold(t + j / 16 * 16);
         }
     } else if (act == XPRESS_ACT_GELU) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < N; ++j) {
             t[j] = 0.5f * t[j] * erfcf(-0.70710678118654752f * t[j]);
-            if (j % 2 == 1) hold();
+            if (j % 2 == 1) hold(t + j / 16 * 16);
         }
     } else if (act == XPRESS_ACT_RELU) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) t[j] = t[j] < 0.0f ? 0.0f : t[j];       // a NaN stays
+        for (int j = 0; j < N; ++j) t[j] = t[j] < 0.0f ? 0.0f : t[j];        // a NaN stays
     }
 }
 

@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
                 tc_fence_after();
             };
             if (S == 1) {
-                // A tile's part, 16 columns at a time by way of shared memory, what is read for
-                // them 32 columns ahead: rows m0 + rl + 8 i, columns 4 cl .. of each 16.  `whole`:
+                // A tile's part, 32 columns at a time by way of shared memory, what is read for
+                // the next ones ahead: rows m0 + rl + 8 i, columns 4 cl .. of each 16.  `whole`:
                 // all of it is inside out, by quads, so that nothing needs a check.
                 const auto part_of_tile = [&](auto whole) {
                     constexpr bool WHOLE = decltype(whole)::value;
@@ -348,44 +348,49 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
                     fetch(0, 1);
                     wait();
                     if (!ok) return;
+                    constexpr int H = BF16 ? 2 : 1;          // 16 columns each, as many as registers allow
 #pragma unroll 1
                     for (int c = 0; c < LW_COLS; c += 32)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float d[16];
-                            tmem_ld16(taddr + buf * LW_BN + c + 16 * h, d);
-                            if (h == 1 && c + 32 == LW_COLS) {
+                        for (int h0 = 0; h0 < 2; h0 += H) {
+                            float d[16 * H];
+                            if constexpr (H == 2) tmem_ld32(taddr + buf * LW_BN + c, d);
+                            else tmem_ld16(taddr + buf * LW_BN + c + 16 * h0, d);
+                            if (h0 + H == 2 && c + 32 == LW_COLS) {
                                 tc_fence_before();
                                 __syncwarp();
                                 if (lane == 0) mbar_arrive(&sh.tread[buf]);
                             }
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) *quad_of(tp + h * 128, lane, j) = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
+                            for (int j = 0; j < 4 * H; ++j)
+                                *quad_of(tp + (h0 + j / 4) * 128, lane, j % 4) = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
                             __syncwarp();
-                            float v[4][4];
+                            float v[4 * H][4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float4 p = *quad_of(tp + h * 128, rl + 8 * i, cl);
-                                v[i][0] = p.x; v[i][1] = p.y; v[i][2] = p.z; v[i][3] = p.w;
-                                lin_add4(v[i], bias[h]);
+                            for (int k = 0; k < 4 * H; ++k) {
+                                const float4 p = *quad_of(tp + (h0 + k / 4) * 128, rl + 8 * (k % 4), cl);
+                                v[k][0] = p.x; v[k][1] = p.y; v[k][2] = p.z; v[k][3] = p.w;
+                                lin_add4(v[k], bias[h0 + k / 4]);
                             }
                             __syncwarp();
-                            lin_act<BF16>(g.act, v);
-                            const int n = n0 + c + 16 * h + 4 * cl;
+                            lin_act<BF16, 16 * H>(g.act, v[0]);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
+                            for (int k = 0; k < 4 * H; ++k) {
+                                const int h = h0 + k / 4, i = k % 4, n = n0 + c + 16 * h + 4 * cl;
                                 if (!WHOLE) {
-                                    if (m0 + rl + 8 * i < g.M && n < g.N) lin_store4(g, m0 + rl + 8 * i, n, v[i], next[h][i]);
+                                    if (m0 + rl + 8 * i < g.M && n < g.N) lin_store4(g, m0 + rl + 8 * i, n, v[k], next[h][i]);
                                     continue;
                                 }
                                 if (g.res)
 #pragma unroll
-                                    for (int j = 0; j < 4; ++j) v[i][j] += next[h][i][j];
+                                    for (int j = 0; j < 4; ++j) v[k][j] += next[h][i][j];
                                 uint8_t *p = out + i * ostep + (c + 16 * h) * ES;
-                                if (BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[i][0], v[i][1]), pack_bf16(v[i][2], v[i][3]));
-                                else *reinterpret_cast<float4 *>(p) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+                                if (BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[k][0], v[k][1]), pack_bf16(v[k][2], v[k][3]));
+                                else *reinterpret_cast<float4 *>(p) = make_float4(v[k][0], v[k][1], v[k][2], v[k][3]);
                             }
-                            if (c + 32 < LW_COLS) fetch(c + 32, h);
+                            if (c + 32 < LW_COLS)
+#pragma unroll
+                                for (int h = h0; h < h0 + H; ++h) fetch(c + 32, h);
                         }
                 };
                 if (g.quads && m0 + 32 <= g.M && n0 + LW_COLS <= g.N) part_of_tile(std::true_type());
@@ -434,7 +439,7 @@ __global__ void __launch_bounds__(LW_THREADS, 1)
                 v[k % 4][0] = a.x; v[k % 4][1] = a.y; v[k % 4][2] = a.z; v[k % 4][3] = a.w;
                 lin_add4(v[k % 4], jbias[k]);
                 if (k % 4 != 3) continue;
-                lin_act<BF16>(g.act, v);
+                lin_act<BF16, 16>(g.act, v[0]);
 #pragma unroll
                 for (int i = k - 3; i <= k; ++i) {
                     quad_at(i, r, c);
