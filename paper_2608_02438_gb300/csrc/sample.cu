@@ -76,6 +76,7 @@ struct SampleArgs {
 
 constexpr int BINS = 1024;                       // of a histogram
 constexpr int FEW = BINS;                        // elements that are sorted: as many to a thread as bins
+constexpr int PAIRS = 128;                       // ... by comparing each with all
 constexpr int MAX_CLUSTER = 8;
 constexpr int ALL = 0x7fffffff;
 constexpr size_t HIST_BYTES = BINS * 16 + FEW * 8;        // counts, masses, largest and smallest key; a CTA's part of the few
@@ -461,8 +462,8 @@ struct Sampler {
         return warp_sum(threadIdx.x % 32 < SWARPS ? sh.scan[which][threadIdx.x % 32] : 0ull);
     }
 
-    // The elements from t up, of the whole row and in the order of the ids, NB to each
-    // thread of every CTA: their order's word above the id, 0 past the last one.  Their
+    // The elements from t up, of the whole row and in the order of the ids, up to NB to
+    // each thread of every CTA: their order's word above the id, 0 past the last one.  Their
     // number; above FEW nothing is done.
     __device__ int gather(float t, unsigned long long (&e)[NB])
     {
@@ -480,7 +481,7 @@ struct Sampler {
             for (int j = 0; j < E; ++j) c += v[j] >= t;
         }
         uint32_t at = (uint32_t)block_scan(c, 0);
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; c && at < FEW && i < n; ++i) {
             if (!(some >> (i & 31) & 1u)) continue;
             float v[E];
             P::unpack(piece(first() + i), v);
@@ -871,33 +872,18 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
 #pragma unroll 4
         for (int p = tid; p < a.slice; p += ST) mx = fmaxf(mx, P::max_of(x.fetch(p)));
     }
-    // the maxima of groups of 2^g lanes, at least top_k of them: the smallest bounds
-    // the top_k-th largest element from below
-    uint32_t key = order_of(mx), group = ~0u, groups = 0;
-    {
-        int g = -1;
-        if (top_k > 0) {
-            const int64_t pieces = ((int64_t)a.V + x.shift + E - 1) / E, full = pieces / a.slice;
-            const int64_t threads = full * min(ST, a.slice) + min((int64_t)ST, pieces - full * a.slice);    // that have elements
-            if (threads >= top_k) g = min(5, 31 - __clz((int)threads / top_k));
-        }
-#pragma unroll
-        for (int i = 0; i <= 5; ++i) {
-            if (i == g) {
-                groups = __popc(__ballot_sync(0xffffffffu, key >= LOWEST)) >> g;
-                group = __reduce_min_sync(0xffffffffu, key >= LOWEST ? key : ~0u);
-            }
-            if (i < 5) key = max(key, __shfl_xor_sync(0xffffffffu, key, 1 << i));
-        }
-    }
+    // The r-th largest of the threads' maxima, r of C for top_k: the smallest of the CTAs'
+    // bounds the top_k-th largest element from below, with about a third more above it.
+    // (To 16 bits.)
+    const uint32_t key = order_of(mx);
+    const int r_k = (top_k + (int)C - 1) / (int)C, of = min(ST, a.slice);
+    uint32_t bound = 0;
+    if (top_k > 1 && r_k <= of)
+        for (int bit = 31; bit >= 16; --bit)
+            if (__syncthreads_count(key >= (bound | 1u << bit)) >= r_k) bound |= 1u << bit;
     cluster_wait();
-    x.exchange(key, (unsigned long long)groups << 32 | (uint32_t)~group);
-    const uint32_t kmax = x.exchanged_max(0);
-    uint32_t kgroup = ~x.exchanged_max(1), n_groups = 0;
-#pragma unroll
-    for (int i = 0; i < NS; ++i) n_groups += (uint32_t)(x.slot_of(1, i) >> 32);
-    n_groups = __reduce_add_sync(0xffffffffu, n_groups);
-    if ((int)n_groups < top_k) kgroup = 0;
+    x.exchange(__reduce_max_sync(0xffffffffu, key), (uint32_t)~bound);
+    const uint32_t kmax = x.exchanged_max(0), kbound = ~x.exchanged_max(1);
 
     Kept kept{-INFINITY, 0};
     // The truncated row; cut: the last id with l == t that is kept.  (Pieces below the
@@ -965,6 +951,41 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             unsigned long long e[NB];
             const int total = x.gather(t, e);
             if (total > FEW) return false;
+            if (total <= PAIRS) {
+                // every one against every other: how many stand before it, and their mass
+                settled = true;
+                if (!a.out && x.rank > 0) return true;
+                ulonglong2 *all = reinterpret_cast<ulonglong2 *>(x.hist);
+                const unsigned long long mine = e[0] ^ 0xffffffffull, w = tid < total ? weight_exact(S::value_of(e[0]), x.s, sh.table) : 0;
+                if (tid < total) all[tid] = make_ulonglong2(mine, w);
+                __syncthreads();
+                int place = 0;
+                unsigned long long before = 0;
+                if (tid < total) {
+#pragma unroll 4
+                    for (int i = 0; i < total; ++i) {
+                        const ulonglong2 o = all[i];
+                        place += o.x > mine;
+                        before += o.x > mine ? o.y : 0ull;
+                    }
+                }
+                const int of_k = min(total, k) - 1;
+                if (tid < total && place == of_k) sh.mass = before + w;
+                __syncthreads();
+                const unsigned long long goal = p_on ? goal_of(sh.mass, top_p) : ~0ull;
+                const bool keep = tid < total && place <= of_k && before < goal;
+                if (keep && (place == of_k || before + w >= goal)) sh.note[2] = e[0];     // the last one
+                const unsigned long long at = x.block_scan(keep ? w : 0ull, 0);
+                kept = {S::value_of(sh.note[2]), 1};
+                cut = (int)(uint32_t)sh.note[2];
+                if (a.tokens && x.rank == 0) {
+                    const unsigned long long z = warp_sum(tid % 32 < S::SWARPS ? sh.scan[0][tid % 32] : 0ull);
+                    bool more;
+                    const unsigned long long draw = u < 1.0f ? min(scaled(z, u, more), z - 1) : z - 1;
+                    if (keep && at <= draw && draw < at + w) a.tokens[n] = (int)(uint32_t)e[0];
+                }
+                return true;
+            }
             uint32_t last = max(order_of(low), order_of(t)), q = ALL;  // kept: words above last, and the first q of those equal to it
             if (total > k) {
 #pragma unroll
@@ -1031,12 +1052,15 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             }
             return true;
         };
-        if (few == 1) settle(m, 1);
+        const float lo_k = kbound >= LOWEST ? fmaxf(low, F::value(kbound)) : low;
+        if (few == 1) {
+            settle(m, 1);
+        } else if (m < INFINITY && (min_p > 0.0f || (k_on && kbound >= LOWEST && top_k <= FEW / 2 && 2 * r_k <= of))) {
+            if (settle(k_on ? lo_k : low, k_on ? top_k : ALL)) k_on = p_on = false;
+        }
         // ------------------------------------------------------------ top-k
         if (k_on) {
-            float lo = kgroup >= LOWEST ? fmaxf(low, F::value(kgroup)) : low;
-            // above the smallest of g maxima there are about g ln g elements
-            if (kgroup >= LOWEST && n_groups <= 128 && settle(lo, top_k)) k_on = p_on = false;
+            float lo = lo_k;
             uint32_t klo = order_of(lo) >> KS, khi = top, left = top_k;
             for (int level = 0; k_on; ++level) {
                 const int bits = S::level_bits(klo, khi);
