@@ -13,10 +13,12 @@
 // the CTAs' shared memory; every further pass over it stays there.  A thread owns
 // consecutive 16-byte pieces, an odd number of them: the lanes' accesses then hit
 // different banks, and sums per thread, warp and CTA are in the order of the ids.
-//   maximum    with it the smallest of the maxima of as many groups of lanes as k
-//              needs: a bound below the k-th largest element
-//   the few    where at most 1024 elements can be kept (a small k, greedy rows), they
-//              are gathered in every CTA, which finds the thresholds and draws alone
+//   maximum    with it, by bisection, the k/C-th largest of the threads' maxima of
+//              each CTA: the smallest is a bound below the k-th largest element
+//   the few    where at most 1024 elements are above it, or above min-p's limit, they
+//              are gathered in every CTA, which finds the thresholds and draws alone:
+//              128 or fewer by comparing each with all (three barriers), more by
+//              histograms of them
 //   thresholds else by histograms between a lower bound and the maximum: 1024 bins of
 //              single bf16 values, or of equal width first and of keys after that,
 //              until a bin's largest and smallest elements decide.  By numbers for
@@ -32,12 +34,16 @@
 // taken again with exact weights: one row in 200 of a softmax over 15000 likely tokens.
 //
 // Bound by latency: a row is a chain of some ten passes, barriers and scans.  One row
-// of 151936 bf16, top-k 50 and top-p 0.9: 13.6 us (load 1.3, maximum 1.8, the few 3.8,
-// thresholds 3.6, draw 1.4).  32 x 17 truncated rows of it: 192 us, 1.7 TB/s; shared
-// memory holds 76 rows at a time, for 20 us (median) each.  64 rows without filters:
-// 26 us; 5 of a row's 15 are the weights, at the issue limit.  What it took before:
-// one row 19 and 544 rows 443 us with CTAs of two passes per level, 64-bit atomics on
-// masses and 64-bit floating point at two lanes a cycle.
+// of 151936 bf16, top-k 50 and top-p 0.9: 11.3 us (load 1.3, bound 1.0, exchange 1.3,
+// the few 5.6, the rest 2.1).  32 x 17 truncated rows of it under mixed filters: 165 us,
+// 2.0 TB/s; shared memory holds 76 rows at a time, for 16 us (median) each: with top-k 20
+// 136 us for all, 300 187, top-p alone 343.  64 rows without filters: 26 us; 5 of a
+// row's 15 are the weights, at the issue limit.  What it took before: one row 19 and 544
+// rows 443 us with CTAs of two passes per level, 64-bit atomics on masses and 64-bit
+// floating point at two lanes a cycle; 15 and 201 with histograms for all of the few
+// and a bound from the maxima of groups of lanes (266 elements above it, not 68).
+// (Of top-p alone the likely few gathered first, as for a top-k of 512: 340 us for 343
+// where they are enough, 41 for 34 where not: left out.)
 #include "matmul_fp8.h"
 
 namespace xp {
@@ -1376,8 +1382,8 @@ struct SamplePlan {
 
 // CTAs of a row's cluster: the fewest that leave two on an SM; more while they have
 // more than 2048 pieces and all rows' CTAs have a place at the same time (64 rows of
-// 151936 bf16: 4 CTAs, 28 us, 32 with 2; 68 rows of 32000: 2 CTAs, 15 us, 17 with 1, 16
-// with 4).  8 for a few rows only (one row 15 us, 16 with 4; 17 rows 19 with 4, 24 with
+// 151936 bf16: 4 CTAs, 28 us, 32 with 2; 68 rows of 32000: 2 CTAs, 11.5 us, 13.5 with
+// 4).  8 for a few rows only (one row 11.3 us, 12.2 with 4; 17 rows 14 with 4, 16 with
 // 8).  The pieces of a CTA and of a thread.
 SamplePlan sample_plan(int64_t n, int V, int E, int sms)
 {

@@ -407,3 +407,39 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     check(a, Ta, ua, ta, oa, p=pa)
     check(b, Tb, ub, tb, ob, k=kb)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("order", ["mixed", "falling", "rising", "one of 64"])
+@pytest.mark.parametrize("k", [2, 16, 127, 128, 129, 400, 511, 513])
+def test_few_elements_wherever_they_are(dt, order, k):
+    """The largest spread over the row, all in its first or last part, or a few to each part."""
+    g = _gen(20)
+    V = 40003
+    logits = rows_of(4, V, torch.float32, g)
+    if order != "mixed":
+        logits = torch.sort(logits, dim=1, descending=order != "rising").values
+    if order == "one of 64":
+        V = 40000
+        logits = logits[:, :V].reshape(4, V // 64, 64).transpose(1, 2).reshape(4, V)
+    logits = logits.to(dt).contiguous()
+    u = torch.rand(4, device="cuda", generator=g)
+    run(logits, 0.9, u=u, k=k)
+    run(logits, 0.9, u=u, k=k, p=0.8)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("f", [dict(), dict(p=0.9), dict(k=300), dict(k=3000, p=0.99)])
+@pytest.mark.parametrize("kept", [1, 2, 127, 128, 129, 1023, 1024, 1025, 9000])
+def test_min_p_keeps_so_many(dt, f, kept):
+    """min-p alone, or before the other filters, leaves a given number."""
+    g = _gen(21)
+    V, n = 30011, 4
+    logits = torch.full((n, V), -20.0, device="cuda")
+    for i in range(n):
+        at = torch.randperm(V, device="cuda", generator=g)[:kept]
+        logits[i, at] = torch.rand(kept, device="cuda", generator=g) * 2.0
+    logits = logits.to(dt)
+    u = torch.rand(n, device="cuda", generator=g)
+    run(logits, 1.0, u=u, min_p=0.1, **f)
+    run(logits, 1.0, u=u, min_p=0.1, want_out=False, **f)
