@@ -317,10 +317,11 @@ int resident(int S)
 //              1.5 more, with two CTAs on an SM 1.43 times as long; joining a split 1;
 //              the weights stream at 6.3 TB/s (64 x 16384 x 4096: 28)
 //   many rows  0.59 for a stage of a 256 x 256 tile, 12 to start and for the last tile's
-//              epilogue (500 x 500 x 64: 12.3, 2048 x 4096 x 4096 in two rounds: 53), 7 at
+//              epilogue (500 x 500 x 64: 11.9, 2048 x 4096 x 4096 in two rounds: 51), 7 at
 //              least from tile to tile, the weights' stream at 5 TB/s
-// At 128 x 4096 x 16384 the choice is NT = 64 with S = 2 (33.8; many rows with S = 2:
-// 52.8), at 512 x 4096 x 4096 many rows with S = 2 (24; without a split 32, NT = 64: 36).
+// At 128 x 4096 x 16384 the choice is NT = 64 with S = 2 (34; many rows with S = 2:
+// 52), at 512 x 4096 x 4096 many rows with S = 2 (24; without a split 30, NT = 64: 31).
+// Of 28 shapes timed with every plan, 25 get their fastest to 5 %, the worst 1.12 of it.
 LinPlan plan_linear(int M, int N, int KB, int sms)
 {
     const int KP = (KB + LF_SKB - 1) / LF_SKB;
