@@ -29,16 +29,17 @@
 //
 // Every decision compares masses: 64-bit fixed-point sums, in which no order of
 // additions matters, of weights to 2^-30 (weight_exact2, about 28 instructions).
-// Passes over a whole row first use the hardware's exponential (weight_fast2, about
-// 10); where a decision falls within what that may be off, 2^-21 of the mass, it is
+// Sums of a whole row first use the hardware's exponential (weight_fast2, about 10);
+// where a decision falls within what that may be off, 2^-21 of the mass, it is
 // taken again with exact weights: one row in 200 of a softmax over 15000 likely tokens.
 //
 // Bound by latency: a row is a chain of some ten passes, barriers and scans.  One row
-// of 151936 bf16, top-k 50 and top-p 0.9: 11.3 us (load 1.3, bound 1.0, exchange 1.3,
-// the few 5.6, the rest 2.1).  32 x 17 truncated rows of it under mixed filters: 165 us,
-// 2.0 TB/s; shared memory holds 76 rows at a time, for 16 us (median) each: with top-k 20
-// 136 us for all, 300 187, top-p alone 343.  64 rows without filters: 26 us; 5 of a
-// row's 15 are the weights, at the issue limit.  What it took before: one row 19 and 544
+// of 151936 bf16, top-k 50 and top-p 0.9: 11.2 us (load 1.3, bound 1.0, exchange 1.3,
+// the few 5.6, the rest 2.0).  32 x 17 truncated rows of it under mixed filters: 157 us,
+// 2.1 TB/s; shared memory holds 76 rows at a time, for 16 us (median) each: with top-k 20
+// 127 us for all, 300 179, top-p alone 333.  64 rows without filters: 26.5 us; 5 of a
+// row's 15 are the weights, at the issue limit, and a row that has to be taken again
+// needs 15 more.  What it took before: one row 19 and 544
 // rows 443 us with CTAs of two passes per level, 64-bit atomics on masses and 64-bit
 // floating point at two lanes a cycle; 15 and 201 with histograms for all of the few
 // and a bound from the maxima of groups of lanes (266 elements above it, not 68).
@@ -122,6 +123,11 @@ template <> struct Piece<uint16_t> {
         return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16,
                           e[6] | (uint32_t)e[7] << 16);
     }
+    static __device__ __forceinline__ float pick(const uint4 &r, int j)
+    {
+        const uint32_t w = j & 4 ? (j & 2 ? r.w : r.z) : (j & 2 ? r.y : r.x);
+        return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+    }
     static constexpr uint16_t NEG_INF = 0xff80;
     static __device__ __forceinline__ uint16_t raw(float v) { return f2bf(v); }
     static __device__ __forceinline__ float value(uint32_t key)      // of a key
@@ -150,6 +156,10 @@ template <> struct Piece<float> {
     static __device__ __forceinline__ uint4 pack_raw(const float (&e)[4])
     {
         return make_uint4(__float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3]));
+    }
+    static __device__ __forceinline__ float pick(const uint4 &r, int j)
+    {
+        return __uint_as_float(j & 2 ? (j & 1 ? r.w : r.z) : (j & 1 ? r.y : r.x));
     }
     static constexpr float NEG_INF = -INFINITY;
     static __device__ __forceinline__ float raw(float v) { return v; }
@@ -246,8 +256,8 @@ __device__ __forceinline__ void weight_exact2(float l0, float l1, const Scale &s
         const int tj = (int)table[i & 63];                           // 2^(j / 64) 2^30
         const unsigned long long x = (unsigned long long)((long long)tj * 64 + __mulhi(tj, __float2int_rn(e[k])));
         // x has 36 bits behind the point, and 2^(i >> 6) to come
-        const int up = s.bits - 36 + (i >> 6), down = min(max(-up, 1), 63);
-        w[k] = up >= 0 ? x << max(up, 0) : (x + (1ull << (down - 1))) >> down;
+        const int down = 62 - s.bits - (i >> 6);                     // 1 at least: bits is below 62
+        w[k] = down > 63 ? 0ull : ((x << 26) + (1ull << (down - 1))) >> down;
     }
     // (both may be infinite)
     if (l0 == s.m) w[0] = 1ull << s.bits;
@@ -608,64 +618,83 @@ struct Sampler {
         }
     }
 
-    // Sum of the weights of l > t and number of l == t in n pieces from p of this CTA
-    // (ROW: of every element, none of which is limited by t).
-    template <bool EXACT, bool ROW>
-    __device__ void sums(int p, int n, float t, unsigned long long &sum, uint32_t &ties) const
+    // Exact weights of a piece's elements above t0, two at a time (a warp goes on until
+    // its fullest piece is done): what exceeds t to `sum`, all of it to `sum0` (BOTH).
+    template <bool BOTH>
+    __device__ __forceinline__ void add_exact(const uint4 &r, float t, float t0, unsigned long long &sum, uint32_t &ties,
+                                              unsigned long long &sum0, uint32_t &ties0) const
     {
-        unsigned long long fixed = 0;
-        float hi = 0.0f, lo = 0.0f;
-        ties = 0;
-#pragma unroll 2
-        for (int i = 0; i < n; ++i) {
-            const uint4 r = piece(p + i);
-            if (!ROW && P::max_of(r) < t) continue;
-            float v[E];
-            P::unpack(r, v);
-            if (EXACT) {
+        float v[E];
+        P::unpack(r, v);
+        uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < E; j += 2) {
-                    unsigned long long w[2];
-                    weight_exact2(v[j], v[j + 1], s, sh.table, w);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        fixed += v[j + k] > t ? w[k] : 0ull;
-                        ties += v[j + k] == t;
-                    }
-                }
-            } else {
-                f32x2 w[E / 2];
-#pragma unroll
-                for (int j = 0; j < E; j += 2) {
-                    w[j / 2] = weight_fast2(v[j], v[j + 1], s);
-                    if (!ROW) {
-                        float a, b;
-                        unpack2(w[j / 2], a, b);
-                        w[j / 2] = pack2(v[j] > t ? a : 0.0f, v[j + 1] > t ? b : 0.0f);
-                        ties += (v[j] == t) + (v[j + 1] == t);
-                    }
-                }
-#pragma unroll
-                for (int o = E / 4; o > 0; o >>= 1)
-#pragma unroll
-                    for (int j = 0; j < o; ++j) w[j] = add2(w[j], w[j + o]);
-                float a, c;
-                unpack2(w[0], a, c);
-                a += c;
-                // hi + lo keeps what the addition rounds away
-                const float x = __fadd_rn(hi, a), b = __fsub_rn(x, hi);
-                lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(x, b)), __fsub_rn(a, b));
-                hi = x;
-            }
+        for (int j = 0; j < E; ++j) {
+            m |= v[j] > (BOTH ? t0 : t) ? 1u << j : 0u;
+            ties += v[j] == t;
+            if (BOTH) ties0 += v[j] == t0;
         }
-        const float one = __uint_as_float((uint32_t)(127 + s.bits) << 23);
-        sum = EXACT ? fixed : __float2ull_rn(hi * one) + (unsigned long long)__float2ll_rn(lo * one);
+        while (m) {
+            const int j0 = __ffs(m) - 1;
+            m &= m - 1;
+            const int j1 = m ? __ffs(m) - 1 : -1;
+            m &= m - 1;
+            const float a = P::pick(r, j0), b = P::pick(r, j1);
+            unsigned long long w[2];
+            weight_exact2(a, b, s, sh.table, w);
+            if (j1 < 0) w[1] = 0;
+            sum += (!BOTH || a > t ? w[0] : 0ull) + (!BOTH || b > t ? w[1] : 0ull);
+            if (BOTH) sum0 += w[0] + w[1];
+        }
     }
+    // Sum of the weights of l > t and number of l == t in n pieces from p of this CTA
+    // (fast weights: of every element; t is -inf).
     __device__ void sums(bool exact, int p, int n, float t, unsigned long long &sum, uint32_t &ties) const
     {
-        if (exact) sums<true, false>(p, n, t, sum, ties);
-        else if (t == -INFINITY) sums<false, true>(p, n, t, sum, ties);
-        else sums<false, false>(p, n, t, sum, ties);
+        sum = 0;
+        ties = 0;
+        if (exact) {
+            unsigned long long none = 0;
+            uint32_t none0 = 0;
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                const uint4 r = piece(p + i);
+                if (t == -INFINITY) {                                // (by pieces' places: 29.4 us for 26.5)
+                    float v[E];
+                    P::unpack(r, v);
+#pragma unroll
+                    for (int j = 0; j < E; j += 2) {
+                        unsigned long long w[2];
+                        weight_exact2(v[j], v[j + 1], s, sh.table, w);
+                        sum += w[0] + w[1];
+                    }
+                } else if (P::max_of(r) >= t) {
+                    add_exact<false>(r, t, t, sum, ties, none, none0);
+                }
+            }
+            return;
+        }
+        float hi = 0.0f, lo = 0.0f;
+#pragma unroll 2
+        for (int i = 0; i < n; ++i) {
+            float v[E];
+            P::unpack(piece(p + i), v);
+            f32x2 w[E / 2];
+#pragma unroll
+            for (int j = 0; j < E; j += 2) w[j / 2] = weight_fast2(v[j], v[j + 1], s);
+#pragma unroll
+            for (int o = E / 4; o > 0; o >>= 1)
+#pragma unroll
+                for (int j = 0; j < o; ++j) w[j] = add2(w[j], w[j + o]);
+            float a, c;
+            unpack2(w[0], a, c);
+            a += c;
+            // hi + lo keeps what the addition rounds away
+            const float x = __fadd_rn(hi, a), b = __fsub_rn(x, hi);
+            lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(x, b)), __fsub_rn(a, b));
+            hi = x;
+        }
+        const float one = __uint_as_float((uint32_t)(127 + s.bits) << 23);
+        sum = __float2ull_rn(hi * one) + (unsigned long long)__float2ll_rn(lo * one);
     }
     // sums() of this thread's pieces with exact weights for t, and for a lower t0 beside it.
     __device__ void sums_two(float t, float t0, unsigned long long &sum, uint32_t &ties, unsigned long long &sum0, uint32_t &ties0) const
@@ -673,23 +702,10 @@ struct Sampler {
         sum = sum0 = 0;
         ties = ties0 = 0;
         const int n = count(first());
+#pragma unroll 1
         for (int i = 0; i < n; ++i) {
             const uint4 r = piece(first() + i);
-            if (P::max_of(r) < t0) continue;
-            float v[E];
-            P::unpack(r, v);
-#pragma unroll
-            for (int j = 0; j < E; j += 2) {
-                unsigned long long w[2];
-                weight_exact2(v[j], v[j + 1], s, sh.table, w);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    sum += v[j + k] > t ? w[k] : 0ull;
-                    sum0 += v[j + k] > t0 ? w[k] : 0ull;
-                    ties += v[j + k] == t;
-                    ties0 += v[j + k] == t0;
-                }
-            }
+            if (P::max_of(r) >= t0) add_exact<true>(r, t, t0, sum, ties, sum0, ties0);
         }
     }
 
@@ -925,7 +941,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
     const bool empty = kmax < LOWEST;
     bool k_on = false, p_on = false, check_p = false, settled = false;
     int cut = ALL;
-    int few = ALL;                                 // at most so many are kept
+    bool one = false;                              // the first maximum alone is kept
     unsigned long long z1 = 0;                     // mass of what min-p and top-k keep
     bool z1_exact = false;
     Kept first{-INFINITY, 0};                      // ... as a threshold
@@ -944,7 +960,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
         if (low > -3.402823466e38f) kept = {low, ALL};
         if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {
             kept = {m, 1};
-            few = 1;
+            one = true;
         } else {
             k_on = top_k > 0 && top_k < a.V && m < INFINITY;
             p_on = top_p < 1.0f && m < INFINITY;
@@ -1059,7 +1075,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             return true;
         };
         const float lo_k = kbound >= LOWEST ? fmaxf(low, F::value(kbound)) : low;
-        if (few == 1) {
+        if (one) {
             settle(m, 1);
         } else if (m < INFINITY && (min_p > 0.0f || (k_on && kbound >= LOWEST && top_k <= FEW / 2 && 2 * r_k <= of))) {
             if (settle(k_on ? lo_k : low, k_on ? top_k : ALL)) k_on = p_on = false;
@@ -1075,7 +1091,6 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
                 for (int i = 0; i < NB; ++i) wide[i] = b[i];
                 const bool found = x.find_bin(wide, left, level & 1, bits > 0);
                 if (!found) break;                                    // fewer than k
-                few = top_k;
                 if (level == 0 && (bits ? sh.count : sh.mass) + sh.before <= FEW) {
                     const float t = bits ? P::value(sh.smallest) : P::value(khi - sh.bin);
                     __syncthreads();
@@ -1101,7 +1116,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
         if (p_on) {
             unsigned long long sum;
             uint32_t ties;
-            z1_exact = few <= 4096 * (int)C || !x.s.near;
+            z1_exact = kept.t > -INFINITY || !x.s.near;
             x.sums(z1_exact, x.first(), x.count(x.first()), kept.t, sum, ties);
             x.exchange(warp_sum(sum), warp_sum(ties));
             z1 = x.exchanged_sum(0);
@@ -1176,9 +1191,9 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
         if (tid == 0 && x.rank == 0 && a.tokens) a.tokens[n] = -1;
         kept = {INFINITY, 0};
     } else if (!settled && (a.tokens || check_p || (a.out && kept.q < ALL && kept.q > 0))) {
-        // a check that the fast weights could hardly decide starts with exact ones
-        bool exact = few <= 4096 * (int)C || !x.s.near ||
-                     (check_p && (float)weight_exact(kept.t, x.s, sh.table) < 4.0f * SLACK * part_of(z1));
+        // (fast weights for whole rows only: with the checks by exact ones at once, a third
+        // form of the sums and its slack are gone from the code; 5 to 8 % everywhere)
+        bool exact = kept.t > -INFINITY || !x.s.near;
         // while t is not sure: what is known of its key, from below and above
         uint32_t known_lo = max(order_of(first.t), LOWEST) >> KS, known_hi = kmax >> KS;
         int moves = 0;
@@ -1186,7 +1201,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             const float t = kept.t;
             unsigned long long sum;
             uint32_t ties;
-            if (check_p && exact && !z1_exact) {
+            if (check_p && !z1_exact) {
                 unsigned long long sum0;
                 uint32_t ties0;
                 x.sums_two(t, first.t, sum, ties, sum0, ties0);
@@ -1219,11 +1234,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
                 const uint32_t may = t == first.t ? min(all_ties, (uint32_t)first.q) : all_ties;
                 const unsigned long long target = goal_of(z1, top_p);
                 // above - top_p z1, with the same weights in both where both are fast
-                const float av = part_of(above), zv = part_of(z1);
-                const unsigned long long slack = exact ? 0
-                    : (unsigned long long)(z1_exact ? SLACK * av
-                                                    : SLACK_W * ((1.0f - top_p) * av + top_p * (zv - av)) + SLACK_SUM * (av + top_p * zv)) + SLACK_UNITS;
-                const bool small = above >= target + slack, large = above + may * wt + slack < target && t > first.t;
+                const bool small = above >= target, large = above + may * wt < target && t > first.t;
                 if ((small || large) && moves < 40) {                 // 33 halve any range of keys to one
                     // the next value first (rounded masses put t off by one), then the middle
                     const uint32_t at = order_of(t) >> KS;
@@ -1236,11 +1247,6 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
                 }
                 const unsigned long long over = target > above ? target - above : 1;
                 const unsigned long long need = wt ? min((over + wt - 1) / wt, (unsigned long long)max(may, 1u)) : 1;
-                const bool sure = target > above + (need - 1) * wt + slack && (above + need * wt >= target + slack);
-                if (!sure && !(exact && z1_exact)) {
-                    exact = true;                                     // once more, with exact masses
-                    continue;
-                }
                 kept.q = (int)need;
                 check_p = false;
             }
