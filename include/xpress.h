@@ -454,8 +454,8 @@ int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws
  * 256-byte aligned, zeroed once by the caller; it only holds the status word
  * (xpress_get_device_status reads and clears it) and may be shared by calls, with
  * xpress_matmul_fp8 too.  Reproducible: the order of every sum is fixed.
- * Errors: INVALID_ARG, UNSUPPORTED (out_dtype, act, K above 2^24, M or N above
- * 2^30), WORKSPACE, CUDA. */
+ * Errors: INVALID_ARG (out = residual with another pitch too), UNSUPPORTED
+ * (out_dtype, act, K above 2^24, M or N above 2^30), WORKSPACE, CUDA. */
 typedef struct {
     int M, N, K;
     int out_dtype;          /* xpress_dtype of out and residual */
@@ -556,8 +556,8 @@ int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_
  * Masses are compared to about 2^-30 of the row's, in sums that do not depend on
  * any order: calls repeat bit for bit.  No workspace; one kernel launch.
  * Errors: INVALID_ARG (NULL logits / temperature, neither tokens nor out, tokens
- * without u, a pitch below V, misaligned pointers), UNSUPPORTED (dtype, V above
- * 2^24, 2^28 rows or more), CUDA. */
+ * without u, a pitch below V, out = logits with another pitch, misaligned
+ * pointers), UNSUPPORTED (dtype, V above 2^24, 2^28 rows or more), CUDA. */
 typedef struct {
     int n_seq, rows, V;
     int dtype;                       /* xpress_dtype of logits and out */

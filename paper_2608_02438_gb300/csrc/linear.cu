@@ -403,7 +403,8 @@ extern "C" int xpress_linear(const xpress_linear_args *in, void *ws, size_t ws_b
     const uintptr_t es = bf16 ? 2 : 4;
     if (in->ldx < in->K || in->ldw < in->K || in->ldx % 8 || in->ldw % 8 || !aligned(in->x, 16) || !aligned(in->w, 16) ||
         in->ldo < in->N || !aligned(in->out, es) || !aligned(in->bias, 2) ||
-        (in->residual && (in->ldr < in->N || !aligned(in->residual, es))))
+        (in->residual && (in->ldr < in->N || !aligned(in->residual, es) ||
+                          (in->residual == in->out && in->ldr != in->ldo && in->M > 1))))
         return XPRESS_ERR_INVALID_ARG;
     if (in->K > MAX_DIM / 64 || in->M > MAX_DIM || in->N > MAX_DIM) return XPRESS_ERR_UNSUPPORTED;
     if (!ws || !aligned(ws, 256) || ws_bytes < xpress_linear_workspace_size()) return XPRESS_ERR_WORKSPACE;

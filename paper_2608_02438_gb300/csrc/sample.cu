@@ -1436,6 +1436,7 @@ extern "C" int xpress_sample(const xpress_sample_args *in, void *stream)
         !aligned(in->temperature, 4) || !aligned(in->top_k, 4) || !aligned(in->top_p, 4) || !aligned(in->min_p, 4))
         return XPRESS_ERR_INVALID_ARG;
     const int64_t n = (int64_t)in->n_seq * in->rows;
+    if (in->out == in->logits && in->ldo != in->ld && n > 1) return XPRESS_ERR_INVALID_ARG;
     if (n == 0) return XPRESS_OK;
     const int sms = current_sms();
     if (sms < 1) return XPRESS_ERR_CUDA;

@@ -83,3 +83,9 @@ def test_variants(tmp_path):
         g = _args(out_dtype=dt, M=M, N=N, K=K, ldx=K, ldw=K, ldo=N, ldr=N)
         assert lib.xpress_linear(g, 4096, 256, None) == X.XPRESS_OK
     _all_launched(lib)
+
+
+def test_in_place_needs_the_same_pitch(lib):
+    """out over residual in rows of another pitch: an output would replace another row's residual."""
+    assert lib.xpress_linear(_args(ldr=104), 4096, 256, None) == BAD
+    assert lib.xpress_linear(_args(ldo=104), 4096, 256, None) == BAD

@@ -95,3 +95,9 @@ def test_cluster_sizes(tmp_path, n, V, most):
         before = lib.fake_launches()
         assert lib.xpress_sample(_args(n_seq=n, rows=1, V=V, ld=V, ldo=V), None) == OK
         assert lib.fake_launches() == before + 1 and lib.fake_last_cluster() <= most
+
+
+def test_in_place_needs_the_same_pitch(lib):
+    """out over logits in rows of another pitch: a written row would replace another one's logits."""
+    assert lib.xpress_sample(_args(out=4096, ldo=1008), None) == BAD
+    assert lib.xpress_sample(_args(out=4096, ld=1001), None) == BAD
