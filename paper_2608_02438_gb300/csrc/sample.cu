@@ -28,29 +28,31 @@
 //              contains u Z looks for the element
 //
 // Every decision compares masses: 64-bit fixed-point sums, in which no order of
-// additions matters, of weights to 2^-30 (weight_exact2, about 28 instructions).
-// Sums of a whole row first use the hardware's exponential (weight_fast2, about 10);
-// where a decision falls within what that may be off, 2^-21 of the mass, it is
-// taken again with exact weights: one row in 200 of a softmax over 15000 likely tokens.
+// additions matters, of weights to 2^-29.8 (weight_exact2).  Sums of a whole row first
+// use the hardware's exponential (weight_fast2, a third of the instructions); where a
+// decision falls within what that may be off, 2^-21 of the mass, it is taken again with
+// exact weights: one row in 200 of a softmax over 15000 likely tokens.
 //
 // Bound by latency: a row is a chain of some ten passes, barriers and scans.  One row
 // of 151936 bf16, top-k 50 and top-p 0.9: 11.2 us (load 1.3, bound 1.0, exchange 1.3,
-// the few 5.6, the rest 2.0).  32 x 17 truncated rows of it under mixed filters: 157 us,
+// the few 5.6, the rest 2.0).  32 x 17 truncated rows of it under mixed filters: 155 us,
 // 2.1 TB/s; shared memory holds 76 rows at a time, for 16 us (median) each: with top-k 20
-// 127 us for all, 300 179, top-p alone 333.  64 rows without filters: 26.5 us; 5 of a
-// row's 15 are the weights, at the issue limit, and a row that has to be taken again
-// needs 15 more.  What it took before: one row 19 and 544 rows 443 us with CTAs of two
-// passes per level, 64-bit atomics on masses and 64-bit floating point at two lanes a cycle; 15 and 201 with histograms for all of the few
-// and a bound from the maxima of groups of lanes (266 elements above it, not 68).
-// (Of top-p alone the likely few gathered first, as for a top-k of 512: 340 us for 343
-// where they are enough, 41 for 34 where not: left out.)
+// 128 us for all, 300 179, top-p alone 326.  64 rows without filters: 25 us; 5 of a row's
+// 15 are the weights, at the issue limit, and a row that has to be taken again needs 13
+// more.  What it took before: one row 19 and 544 rows 443 us with CTAs of two passes per
+// level, 64-bit atomics on masses and 64-bit floating point at two lanes a cycle; 15 and
+// 201 with histograms for all of the few and a bound from the maxima of groups of lanes
+// (266 elements above it, not 68); 64 rows 26.6 with weights of 36 bits behind the point
+// before their shift, which 64-bit shifts made.  (Of top-p alone the likely few gathered
+// first, as for a top-k of 512: 340 us for 343 where they are enough, 41 for 34 where
+// not: left out.)
 #include "matmul_fp8.h"
 
 namespace xp {
 
 namespace {
 
-// 2^(j / 64) 2^30, from the exponential's series.
+// 2^(j / 64) 2^31, from the exponential's series.
 struct ExpTable {
     uint32_t v[64];
 };
@@ -61,7 +63,7 @@ constexpr ExpTable make_exp_table()
         const double x = j * 0.693147180559945309417232 / 64;
         double term = 1.0, sum = 1.0;
         for (int i = 1; i < 24; ++i) { term *= x / i; sum += term; }
-        t.v[j] = (uint32_t)(sum * 1073741824.0 + 0.5);
+        t.v[j] = (uint32_t)(sum * 2147483648.0 + 0.5);
     }
     return t;
 }
@@ -228,7 +230,7 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
 __device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
 __device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { return fma2(b, both(-1.0f), a); }
 
-// w = 2^(K (l - m)) as a 64-bit fixed-point number, to 2^-30 of its value (and half a
+// w = 2^(K (l - m)) as a 64-bit fixed-point number, to 2^-29.8 of its value (and half a
 // unit).  The difference and its product with K are kept in two parts; of the
 // exponent, the steps of 1/64 come from a table, the rest g (|g| <= 1/128) from the
 // series of 2^g - 1, whose fifth term is below 2^-42.
@@ -248,15 +250,15 @@ __device__ __forceinline__ void weight_exact2(float l0, float l1, const Scale &s
     f32x2 q = fma2(g, both(9.61812910e-3f), both(5.55041087e-2f));
     q = fma2(g, q, both(2.40226507e-1f));
     q = fma2(g, q, both(6.93147181e-1f));
-    unpack2(mul2(mul2(g, q), both(274877906944.0f)), e[0], e[1]);    // (2^g - 1) 2^38
+    unpack2(mul2(mul2(g, q), both(8589934592.0f)), e[0], e[1]);      // (2^g - 1) 2^33
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int i = (int)(__float_as_uint(steps[k]) - __float_as_uint(MAGIC));
-        const int tj = (int)table[i & 63];                           // 2^(j / 64) 2^30
-        const unsigned long long x = (unsigned long long)((long long)tj * 64 + __mulhi(tj, __float2int_rn(e[k])));
-        // x has 36 bits behind the point, and 2^(i >> 6) to come
-        const int down = 62 - s.bits - (i >> 6);                     // 1 at least: bits is below 62
-        w[k] = down > 63 ? 0ull : ((x << 26) + (1ull << (down - 1))) >> down;
+        const uint32_t tj = table[i & 63];                           // 2^(j / 64) 2^31
+        const uint32_t y = tj + (uint32_t)__mulhi((int)(tj >> 1), __float2int_rn(e[k]));         // 31 bits behind the point
+        const int up = s.bits - 31 + (i >> 6);                       // 30 at most
+        w[k] = up >= 0 ? (unsigned long long)y * (1u << max(up, 0))
+                       : (unsigned long long)((__funnelshift_rc(y, 0u, (uint32_t)(-up - 1)) + 1u) >> 1);
     }
     // (both may be infinite)
     if (l0 == s.m) w[0] = 1ull << s.bits;
@@ -335,7 +337,7 @@ __device__ __forceinline__ uint32_t ld_cluster1(uint32_t addr)
 __device__ __forceinline__ void cluster_sync() { cluster_arrive(); cluster_wait(); }
 
 template <int SWARPS> struct SampleShared {
-    uint32_t table[64];                                              // 2^(j / 64) 2^30
+    uint32_t table[64];                                              // 2^(j / 64) 2^31
     unsigned long long slot[2][3][MAX_CLUSTER * SWARPS];             // what the cluster's warps exchange: [turn][value][warp]
     unsigned long long scan[2][SWARPS];
     unsigned long long note[4];                                      // written by one thread of the cluster: the id cut, a draw to repeat
