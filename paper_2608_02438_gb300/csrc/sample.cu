@@ -962,9 +962,13 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
         if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {
             kept = {m, 1};
             one = true;
+        } else if (m == INFINITY) {
+            // equal weights: the first top_k, and top-p's share of their number
+            if (top_k > 0) kept.q = top_k;
+            check_p = top_p < 1.0f;
         } else {
-            k_on = top_k > 0 && top_k < a.V && m < INFINITY;
-            p_on = top_p < 1.0f && m < INFINITY;
+            k_on = top_k > 0 && top_k < a.V;
+            p_on = top_p < 1.0f;
         }
         uint32_t b[NB];
         unsigned long long wide[NB];
