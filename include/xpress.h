@@ -544,11 +544,11 @@ int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_
  *   kept by top_p: what stands before v in the order has less mass than top_p
  *           times the mass of what min_p and top_k keep
  *   token = the first id v at which the kept w_0 + .. + w_v exceeds u times their sum
- * The first of the order is always kept.  A filter is off where its array is NULL
- * or its value is top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN.  T <= 0 (or NaN)
- * keeps the first of the order alone.  NaN and -inf logits are never kept; of a row
- * that has +inf only these can be, at equal weights.  A row without anything to keep
- * gives token -1.
+ * The first of the order is always kept (alone at min_p > 1).  A filter is off where
+ * its array is NULL or its value is top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN.
+ * T <= 0 (or NaN) keeps the first of the order alone.  NaN and -inf logits are never
+ * kept; of a row that has +inf only these can be, at equal weights.  A row without
+ * anything to keep gives token -1.
  *   u       [n_seq * rows] in [0, 1) (cut to it; NaN: 0), with tokens
  *   tokens  [n_seq * rows] int32 or NULL
  *   out     [n_seq * rows, V], pitch ldo, or NULL: the kept logits, mask_value in all

@@ -959,7 +959,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             low = fmaxf(rest > 0.0f ? nextafterf(sum, INFINITY) : sum, low);
         }
         if (low > -3.402823466e38f) kept = {low, ALL};
-        if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {
+        if (!(temp > 0.0f) || top_k == 1 || top_p <= 0.0f || min_p > 1.0f) {          // (no weight is above 1)
             kept = {m, 1};
             one = true;
         } else if (m == INFINITY) {

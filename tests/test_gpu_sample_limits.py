@@ -1,4 +1,5 @@
-"""xpress_sample where its definition is at a limit: rows with infinities under every filter.
+"""xpress_sample where its definition is at a limit: rows with infinities under every filter,
+and min_p above 1.
 
 The definition is followed as the entry point states it, in 64 bits.  Masses: by its
 documentation they are compared to about 2^-30 of the row's, taken as 2^-28 here; a kept
@@ -92,7 +93,7 @@ def verify_all(logits, T, us, k=None, p=None, min_p=None):
 @pytest.mark.parametrize("dt", [BF16, F32])
 @pytest.mark.parametrize("infs", [1, 2, 5, 128, 1024, 1500])
 @pytest.mark.parametrize("f", [dict(), dict(k=1), dict(k=2), dict(k=1100), dict(p=0.5), dict(p=0.3), dict(p=1e-9), dict(p=0.999),
-                               dict(k=4, p=0.7), dict(k=2000, p=0.4, min_p=0.5), dict(min_p=0.9)])
+                               dict(k=4, p=0.7), dict(k=2000, p=0.4, min_p=0.5), dict(min_p=0.9), dict(k=3, min_p=2.0)])
 def test_infinities_share_under_the_filters(dt, infs, f):
     """+inf logits have equal masses, all of it: the first top_k of them, and of these what top-p keeps."""
     g = _gen(31)
@@ -106,6 +107,8 @@ def test_infinities_share_under_the_filters(dt, infs, f):
     for i in range(n):                                            # whole numbers: no mass is next to a border
         m = int((logits[i] == INF).sum())
         m = min(m, f.get("k", m))
+        if f.get("min_p", 0.0) > 1.0:
+            m = 1
         if "p" in f:
             m = max(1, math.ceil(float(torch.tensor(f["p"], dtype=F32)) * m))
         assert int((rows[i] > -INF).sum()) == m
@@ -117,3 +120,23 @@ def test_infinities_in_rows_past_shared_memory(dt, V):
     logits[:, 7::1000] = INF
     for f in (dict(k=3), dict(p=0.5), dict(k=300, p=0.25)):
         verify_all(logits, 1.0, [0.1, 0.9], **f)
+
+
+# ------------------------------------------------------------- min_p above 1
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("ties", [1, 2, 300, 3000])
+@pytest.mark.parametrize("min_p", [1.0, 1.0000001, 3.0, INF])
+def test_min_p_above_one_keeps_the_first(dt, ties, min_p):
+    """No weight reaches it; the first of the order is always kept.  At 1 all maxima are."""
+    logits = torch.full((2, 20000), -1.0, dtype=dt, device="cuda")
+    logits[:, 4:4 + 3 * ties:3] = 2.5
+    for f in (dict(), dict(k=2), dict(p=0.9)):
+        tokens, rows = draw(logits, 0.7, torch.tensor([0.0, 0.99], device="cuda"), min_p=min_p, **f)
+        m = ties if min_p == 1.0 else 1
+        m = min(m, f.get("k", m))
+        if "p" in f:
+            m = math.ceil(float(torch.tensor(f["p"], dtype=F32)) * m)
+        for i, u in enumerate((0.0, 0.99)):
+            assert torch.nonzero(rows[i] > -INF)[:, 0].tolist() == list(range(4, 4 + 3 * m, 3))
+            assert int(tokens[i]) == 4 + 3 * math.floor(float(torch.tensor(u, dtype=F32)) * m)
