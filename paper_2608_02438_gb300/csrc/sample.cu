@@ -28,7 +28,9 @@
 //              contains u Z looks for the element
 //
 // Every decision compares masses: 64-bit fixed-point sums, in which no order of
-// additions matters, of weights to 2^-29.8 (weight_exact2).  Sums of a whole row first
+// additions matters, of weights to 2^-29.8 (weight_exact2).  Their scale first leaves
+// room for V weights of 1, and is refined to what the row's mass leaves: a flat tail of
+// V weights that each fall below a unit may hold 2^-14 of it.  Sums of a whole row first
 // use the hardware's exponential (weight_fast2, a third of the instructions); where a
 // decision falls within what that may be off, 2^-21 of the mass, it is taken again with
 // exact weights: one row in 200 of a softmax over 15000 likely tokens.
@@ -78,12 +80,14 @@ struct SampleArgs {
     float mask_value;
     int slice;                     // 16-byte pieces of a CTA
     int per;                       // ... of a thread (odd)
-    int scale;                     // a weight of 1 is 2^scale
+    int scale;                     // a weight of 1 is 2^scale until a row's mass is known
     ExpTable table;
 };
 
 constexpr int BINS = 1024;                       // of a histogram
 constexpr int FEW = BINS;                        // elements that are sorted: as many to a thread as bins
+constexpr int ROOM = 61;                         // masses stay below 2^ROOM or little above
+constexpr int FEW_SCALE = ROOM - 10;             // a weight of 1 in sums of FEW
 constexpr int PAIRS = 128;                       // ... by comparing each with all
 constexpr int MAX_CLUSTER = 8;
 constexpr int ALL = 0x7fffffff;
@@ -440,6 +444,29 @@ struct Sampler {
 #pragma unroll
         for (int i = 0; i < NS; ++i) v = max(v, (uint32_t)slot_of(which, i));
         return __reduce_max_sync(0xffffffffu, v);
+    }
+    // A finer scale for sums that are no more than z, where z leaves room: by how many bits.
+    __device__ __forceinline__ int refine(unsigned long long z)
+    {
+        const int up = max(0, __clzll(z) - (64 - ROOM));
+        s.bits += up;
+        return up;
+    }
+    // ... for sums of elements from t up, from an estimate (2^-12 off).
+    __device__ void refine_from(float t)
+    {
+        float z = 0.0f;
+        for (int i = 0; i < count(first()); ++i) {
+            const uint4 r = piece(first() + i);
+            if (P::max_of(r) < t) continue;
+            float v[E];
+            P::unpack(r, v);
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (v[j] >= t) z += weight_fast(v[j], s);
+        }
+        exchange(warp_sum(__float2ull_rn(z * __uint_as_float((uint32_t)(127 + s.bits) << 23))), 0);
+        refine(exchanged_sum(0));
     }
     // The smallest key above `key` (or the largest below it) of any element; ~0 (0) if there is none.
     __device__ uint32_t next_key(uint32_t key, bool above)
@@ -946,6 +973,12 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
     unsigned long long z1 = 0;                     // mass of what min-p and top-k keep
     bool z1_exact = false;
     Kept first{-INFINITY, 0};                      // ... as a threshold
+    // Sums are off by half a unit for each of their elements.  Whether the first scale
+    // keeps that below 2^-31 of the mass (which is 1 at least, and min_p for each of them);
+    // else a pass over them comes first (64 rows of 151936, top-k 20000: 109 us, 96 without).
+    const uint32_t many = 1u << (a.scale - 30);
+    const bool coarse = kmax == order_of(INFINITY) || (uint32_t)a.V <= many || (top_k > 0 && (uint32_t)top_k <= many) ||
+                        min_p * (float)many >= 1.0f;
     if (!empty) {
         const float m = F::value(kmax);
         x.s = make_scale(m, temp, a.scale);
@@ -978,6 +1011,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             unsigned long long e[NB];
             const int total = x.gather(t, e);
             if (total > FEW) return false;
+            x.s.bits = FEW_SCALE;
             if (total <= PAIRS) {
                 // every one against every other: how many stand before it, and their mass
                 settled = true;
@@ -1122,20 +1156,27 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             unsigned long long sum;
             uint32_t ties;
             z1_exact = kept.t > -INFINITY || !x.s.near;
+            if (z1_exact && !coarse) x.refine_from(kept.t);
             x.sums(z1_exact, x.first(), x.count(x.first()), kept.t, sum, ties);
             x.exchange(warp_sum(sum), warp_sum(ties));
             z1 = x.exchanged_sum(0);
             const unsigned long long nt = min(x.exchanged_sum(1), (unsigned long long)kept.q);
             if (nt) z1 += nt * weight_exact(kept.t, x.s, sh.table);
+            unsigned long long units = SLACK_UNITS;
+            if (!z1_exact) {
+                const int up = x.refine(z1);
+                z1 <<= up;
+                units <<= up;
+            }
             const unsigned long long target = goal_of(z1, top_p);
             // only the target is off: its masses are exact
-            const unsigned long long slack = z1_exact ? 0 : (unsigned long long)(part_of(z1) * (SLACK * top_p)) + SLACK_UNITS;
+            const unsigned long long slack = z1_exact ? 0 : (unsigned long long)(part_of(z1) * (SLACK * top_p)) + units;
             const int down = max(0, 33 - __clzll(z1));                // z1 >> down has 31 bits
-            const float unit = __uint_as_float((uint32_t)(127 + a.scale - down) << 23);
+            const float unit = __uint_as_float((uint32_t)(127 + x.s.bits - down) << 23);
             // what may be left out has at most 1 - top_p of the mass
             float lo = fmaxf(low, kept.t);
             {
-                const float share = (1.0f - top_p) * ((float)z1 * __uint_as_float((uint32_t)(127 - a.scale) << 23)) / (float)a.V;
+                const float share = (1.0f - top_p) * ((float)z1 * __uint_as_float((uint32_t)(127 - x.s.bits) << 23)) / (float)a.V;
                 const float d = (logf(share) - 0.01f) * temp;
                 lo = fminf(fmaxf(lo, m + d * (d < 0.0f ? 1.001f : 0.999f) - 1e-5f * fabsf(m)), m);
             }
@@ -1199,6 +1240,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
         // (fast weights for whole rows only: with the checks by exact ones at once, a third
         // form of the sums and its slack are gone from the code; 5 to 8 % everywhere)
         bool exact = kept.t > -INFINITY || !x.s.near;
+        if (exact && !coarse && !one && !p_on) x.refine_from(kept.t);
         // while t is not sure: what is known of its key, from below and above
         uint32_t known_lo = max(order_of(first.t), LOWEST) >> KS, known_hi = kmax >> KS;
         int moves = 0;
@@ -1378,6 +1420,7 @@ __global__ void __launch_bounds__(ST, 1024 / ST) k_sample(const __grid_constant_
             if (cuts) cut = (int)sh.note[0];
             if (exact || sh.note[1] != 1ull) break;
             exact = true;
+            x.refine(z);
         }
     }
     if (!RES && a.out) cluster_sync();             // nobody reads the row any more: out may be it

@@ -1,5 +1,5 @@
 """xpress_sample where its definition is at a limit: rows with infinities under every filter,
-and min_p above 1.
+min_p above 1, and rows of which a large flat tail holds little of the mass.
 
 The definition is followed as the entry point states it, in 64 bits.  Masses: by its
 documentation they are compared to about 2^-30 of the row's, taken as 2^-28 here; a kept
@@ -140,3 +140,66 @@ def test_min_p_above_one_keeps_the_first(dt, ties, min_p):
         for i, u in enumerate((0.0, 0.99)):
             assert torch.nonzero(rows[i] > -INF)[:, 0].tolist() == list(range(4, 4 + 3 * m, 3))
             assert int(tokens[i]) == 4 + 3 * math.floor(float(torch.tensor(u, dtype=F32)) * m)
+
+
+# ------------------------------------------------------------- flat tails
+
+def tail(V, dt, value, at, spread=0.0, top=0.0, n=4, seed=32):
+    """Rows of one likely token and a tail around `value` below it."""
+    logits = torch.full((n, V), top + value, device="cuda")
+    if spread:
+        logits += spread * torch.randn((n, V), device="cuda", generator=_gen(seed))
+    logits[:, at] = top
+    return logits.to(dt)
+
+
+# weights below and around half of 2^-(61 - ceil(log2 V)), which all V may sum to
+TAILS = [(1 << 24, BF16, -27.0), (1 << 24, BF16, -25.0), (1 << 23, F32, -27.3), (1000003, BF16, -29.25), (700001, BF16, -28.5), (300007, F32, -29.0)]
+
+
+@pytest.mark.parametrize("V, dt, value", TAILS)
+@pytest.mark.parametrize("spread", [0.0, 0.5])
+def test_tokens_of_a_flat_tail(V, dt, value, spread):
+    """The likely token last: small numbers draw from the tail, at its masses."""
+    logits = tail(V, dt, value, V - 1, spread)
+    share = float(torch.exp(logits[0, :-1].double()).sum())
+    verify_all(logits, 1.0, [share * 0.1, share * 0.5, share * 0.9, 0.5])
+
+
+@pytest.mark.parametrize("V, dt, value", TAILS[:4])
+@pytest.mark.parametrize("spread", [0.0, 0.5])
+def test_top_p_inside_a_flat_tail(V, dt, value, spread):
+    logits = tail(V, dt, value, 11, spread)
+    share = float(torch.exp(logits[0].double()).sum()) - 1.0
+    p = 1.0 - share * 0.4                                         # in steps of 2^-24
+    verify_all(logits, 1.0, [0.0, 0.5, 0.9999, 1.0 - 2.0 ** -24], p=p)
+
+
+@pytest.mark.parametrize("f", [dict(min_p=1e-13), dict(k=1 << 23), dict(k=1 << 23, p=0.99999), dict(min_p=1e-13, p=0.99999)])
+@pytest.mark.parametrize("spread", [0.0, 0.25])
+def test_filters_that_leave_a_flat_tail(f, spread):
+    V = 1 << 24
+    logits = tail(V, BF16, -27.0, V - 1, spread)
+    share = float(torch.exp(logits[0, :-1].double()).sum())
+    verify_all(logits, 1.0, [share * 0.01, share * 0.1, share * 0.3, 0.5], **f)
+
+
+@pytest.mark.parametrize("top, T, value", [(1e6, 1.0, -27.0), (0.0, 1e29, -27e29), (-1e6, 0.5, -13.5)])
+@pytest.mark.parametrize("f", [dict(), dict(p=0.99999), dict(k=5_000_000)])
+def test_flat_tails_of_large_and_far_logits(top, T, value, f):
+    """Logits far from 0, where the exponent's parts take more than a float's bits, and a huge temperature."""
+    V = 1 << 23
+    logits = tail(V, F32, value, V - 1, 0.0, top)
+    share = (V - 1) * math.exp(-27.0)
+    verify_all(logits, T, [share * 0.1, share * 0.5, 0.5, 0.99], **f)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("many", [2, 1000, 70000])
+def test_several_likely_tokens_and_a_tail(dt, many):
+    V = 1 << 22
+    logits = tail(V, dt, -26.0, V - 1, 0.3)
+    logits[:, V - many:] = 0.0
+    share = float(torch.exp(logits[0, :V - many].double()).sum()) / many
+    for f in (dict(), dict(p=0.9), dict(p=1.0 - 2.0 ** -20), dict(k=V // 2)):
+        verify_all(logits, 1.0, [share * 0.2, share * 0.8, 0.3, 0.95], **f)
