@@ -45,7 +45,7 @@ class Rules:
     -1 for a row that is not masked.  A mask needs the table of the rows that it is
     to be used on (ValueError without: nothing else tells a row's state).
 
-    What is emitted is allowed by its target row's state, unless that state allows
+    What a round emits is allowed by its target row's state, unless that state allows
     nothing: such a row is MASKED throughout and some forbidden token comes out of it
     (id 0 at temperature 0).  End the request instead of asking for that row."""
     repetition: torch.Tensor | None = None
@@ -180,13 +180,13 @@ class DraftHead:
         """The next token of each of b requests from the target's logits [b, V] (the
         prompt's last position, say) under the rules and filters, drawn with the
         numbers u [b] in [0, 1): int32 [b].  A grammar (rules.mask) needs the rows'
-        states mask_row [b]."""
+        states mask_row [b]; a state that allows nothing gives -1."""
         rules = rules or Rules()
         if (rules.mask is None) != (mask_row is None):
             raise ValueError("Rules.mask and mask_row go together (-1 in mask_row leaves a row unmasked)")
         out = torch.empty_like(logits)
         tokens = torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)
-        X.process_logits(logits, out, mask_row=mask_row, mask_value=MASKED, **rules.common())
+        X.process_logits(logits, out, mask_row=mask_row, **rules.common())            # -inf: never drawn, at any temperature
         X.sample(out, temperature, u=u, tokens_out=tokens, **vars(filters or Filters()))
         return tokens
 
