@@ -87,10 +87,27 @@ class Filters:
         return any(v is not None for v in vars(self).values())
 
 
+def _padded(rows: int, cols: int, device) -> torch.Tensor:
+    """An uninitialised bf16 [rows, cols] whose rows start on 16 bytes."""
+    return torch.empty((rows, (cols + 7) // 8 * 8), dtype=torch.bfloat16, device=device)[:, :cols]
+
+
+def _rows_on_16_bytes(w: torch.Tensor) -> torch.Tensor:
+    """w, or where a row of it starts elsewhere, a copy with padded rows."""
+    if w.dtype != torch.bfloat16 or w.dim() != 2:
+        return w
+    rows, cols = w.shape
+    if w.data_ptr() % 16 == 0 and w.stride(0) % 8 == 0 and w.stride(0) >= cols and w.stride(1) == 1:
+        return w
+    return _padded(rows, cols, w.device).copy_(w.detach())
+
+
 @dataclass
 class FeedForward:
     """A block in front of the head, x + W2 act(W1 norm(x) + b1) + b2: norm_weight [H],
-    W1 [I, H], W2 [H, I], b1 [I] and b2 [H] (None: no bias), bf16; act an XPRESS_ACT_*."""
+    W1 [I, H], W2 [H, I], b1 [I] and b2 [H] (None: no bias), bf16; act an XPRESS_ACT_*.
+    Any I: weights whose rows do not all start on 16 bytes, as binding.linear wants
+    them, are copied once, here, on torch's current stream."""
     norm_weight: torch.Tensor
     W1: torch.Tensor
     W2: torch.Tensor
@@ -98,12 +115,15 @@ class FeedForward:
     b2: torch.Tensor | None = None
     act: int = X.XPRESS_ACT_SILU
 
+    def __post_init__(self):
+        self.W1, self.W2 = _rows_on_16_bytes(self.W1), _rows_on_16_bytes(self.W2)
+
     def __call__(self, x, residual, eps: float):
         """x, residual [n, H] (residual may be None) -> the block's output [n, H]."""
         n, dev = x.shape[0], x.device
         total = torch.empty_like(x, memory_format=torch.contiguous_format) if residual is not None else x
         normed = torch.empty((n, x.shape[1]), dtype=torch.bfloat16, device=dev)
-        inner = torch.empty((n, (self.W1.shape[0] + 7) // 8 * 8), dtype=torch.bfloat16, device=dev)[:, :self.W1.shape[0]]
+        inner = _padded(n, self.W1.shape[0], dev)
         out = torch.empty_like(normed)
         X.rmsnorm(x, self.norm_weight, eps, residual=residual, sum_out=total if residual is not None else None, y_out=normed)
         X.linear(normed, self.W1, inner, bias=self.b1, act=self.act)
@@ -131,6 +151,9 @@ class DraftHead:
         refiner.stream.wait_stream(here)
         self.w, self.w_scale = X.quantize_weight(W_lm, stream=refiner.stream)
         here.wait_stream(refiner.stream)
+        if block is not None:
+            for t in (block.W1, block.W2):               # (copies may be this stream's memory)
+                t.record_stream(refiner.stream)
 
     def base_logits(self, x, residual=None, rules: Rules | None = None) -> dict:
         """x [b, B, H] (the drafter's last layer, before its final norm) -> h
