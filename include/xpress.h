@@ -450,7 +450,8 @@ int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws
  * (XPRESS_ACT_NONE: the identity; GELU is t Phi(t)).  bias and residual are
  * optional (NULL).  Any M >= 0, N, K >= 1; x and w 16-byte aligned with pitches
  * that are multiples of 8 (the padding is never used).  out may be residual's
- * memory (same pitch).  workspace: xpress_linear_workspace_size() bytes,
+ * memory (same pitch); otherwise its rows share no byte with what is read (the
+ * caller's to see to; the torch binding refuses it).  workspace: xpress_linear_workspace_size() bytes,
  * 256-byte aligned, zeroed once by the caller; it only holds the status word
  * (xpress_get_device_status reads and clears it) and may be shared by calls, with
  * xpress_matmul_fp8 too.  Reproducible: the order of every sum is fixed.
@@ -554,6 +555,9 @@ int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_
  *   out     [n_seq * rows, V], pitch ldo, or NULL: the kept logits, mask_value in all
  *           other places; may be logits (same pitch).  For rows that go on to
  *           xpress_accept see mask_value of xpress_process_logits.
+ * out and tokens share no byte with what is read (the caller's to see to; the torch
+ * binding refuses it), but for out = logits, and tokens = u or, with rows = 1, tokens =
+ * a sequence's parameters.
  * Masses are compared to about 2^-30 of the row's, in sums that do not depend on
  * any order: calls repeat bit for bit.  No workspace; one kernel launch.
  * Errors: INVALID_ARG (NULL logits / temperature, neither tokens nor out, tokens

@@ -411,10 +411,10 @@ def matmul_fp8_status(stream=None) -> int:
 def linear(x, w, out, bias=None, act: int = XPRESS_ACT_NONE, residual=None, stream=None) -> int:
     """out [M, N] (bf16 or fp32) = residual + act(x w^T + bias) for bf16 x [M, K],
     w [N, K], bias [N] and residual [M, N] of out's type, which may be out (see
-    xpress_linear).  x's and w's rows start on 16 bytes.  Asynchronous; returns
-    XPRESS_OK; matmul_fp8_status() reads the device status of the calls so far.
-    The first call on a device makes the status word: not inside a graph
-    capture."""
+    xpress_linear; an out that overlaps what is read in any other way is refused).
+    x's and w's rows start on 16 bytes.  Asynchronous; returns XPRESS_OK;
+    matmul_fp8_status() reads the device status of the calls so far.  The first
+    call on a device makes the status word: not inside a graph capture."""
     call, args = (_ext or _load_ext()).linear, (x, w, out, bias, act, residual)
     code = call(*args) if stream is None else _on_stream(stream, call, args)
     if code:
@@ -448,8 +448,8 @@ def sample(logits, temperature, u=None, tokens_out=None, out=None, rows: int = 1
     int32 [n_seq * rows] with the random numbers u fp32 [n_seq * rows] in [0, 1),
     and / or the truncated rows into out (the same type; may be logits), under
     each sequence's temperature fp32, top_k int32, top_p fp32 and min_p fp32
-    [n_seq] (see xpress_sample for the filters).  Asynchronous; returns
-    XPRESS_OK."""
+    [n_seq] (see xpress_sample for the filters; outputs that overlap what is read
+    in another way than it allows are refused).  Asynchronous; returns XPRESS_OK."""
     call = (_ext or _load_ext()).sample
     args = (logits, temperature, u, tokens_out, out, rows, top_k, top_p, min_p, mask_value)
     code = call(*args) if stream is None else _on_stream(stream, call, args)

@@ -22,6 +22,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <map>
 #include <string>
@@ -91,6 +92,45 @@ int narrow(const char *name, int64_t n)
 {
     if (n > INT32_MAX) bad_value(name, ": ", n, " is above the supported size");
     return (int)n;
+}
+
+// Memory that a call reads or writes: n rows of `bytes`, `pitch` bytes apart.
+struct Place {
+    const char *name;
+    uintptr_t at;
+    int64_t n, pitch, bytes;
+
+    Place(const char *name, const void *p, int64_t n, int64_t pitch, int64_t cols, int64_t es)
+        : name(name), at(reinterpret_cast<uintptr_t>(p)), n(cols > 0 && p ? n : 0), pitch(pitch * es), bytes(cols * es) {}
+    Place(const char *name, const void *p, int64_t n) : Place(name, p, 1, n, n, 4) {}      // a vector of 4-byte elements
+    int64_t end() const { return (n - 1) * pitch + bytes; }
+};
+
+// Whether two places share a byte.  (Rows longer than their pitch are the entry points' to refuse.)
+bool share(const Place &a, const Place &b)
+{
+    if (!a.n || !b.n || (a.n > 1 && a.pitch < a.bytes) || (b.n > 1 && b.pitch < b.bytes)) return false;
+    const int64_t d = (int64_t)(b.at - a.at);                        // where b begins, from a
+    if (d >= a.end() || -d >= b.end()) return false;
+    if (a.n > 1 && b.n > 1 && a.pitch == b.pitch) {
+        // rows that keep between one another
+        const int64_t r = (d % a.pitch + a.pitch) % a.pitch;
+        if (r >= a.bytes && r + b.bytes <= a.pitch) return false;
+    }
+    const Place &few = a.n < b.n ? a : b, &other = a.n < b.n ? b : a;
+    const int64_t off = a.n < b.n ? -d : d;                          // where `few` begins, from the other
+    for (int64_t i = 0; i < few.n; ++i) {
+        // the last of the other's rows that begins before this one ends
+        const int64_t from = off + i * few.pitch, last = from + few.bytes - 1;
+        if (last < 0) continue;
+        const int64_t row = other.n == 1 ? 0 : std::min(last / other.pitch, other.n - 1);
+        if (row * other.pitch + other.bytes > from) return true;
+    }
+    return false;
+}
+void apart(const Place &out, const Place &in)
+{
+    if (share(out, in)) bad_value(out.name, " overlaps ", in.name);
 }
 
 // Torch's current stream on the tensors' device, which has to be the current one.
@@ -219,6 +259,12 @@ PyObject *linear(PyObject *, PyObject *const *v, Py_ssize_t n)
     g.out = matrix("out", v[2], M, N, out.scalar_type(), dev, g.ldo);
     if (given(v[3])) g.bias = vector("bias", v[3], N, BF16, dev);
     if (given(v[5])) g.residual = matrix("residual", v[5], M, N, out.scalar_type(), dev, g.ldr);
+    const int64_t es = out.element_size();
+    const Place to("out", g.out, M, g.ldo, N, es);
+    apart(to, {"x", g.x, M, g.ldx, K, 2});
+    apart(to, {"w", g.w, N, g.ldw, K, 2});
+    apart(to, {"bias", g.bias, 1, N, N, 2});
+    if (g.residual != g.out) apart(to, {"residual", g.residual, M, g.ldr, N, es});      // (one place: the entry point sees to the pitch)
     void *st = current_stream(dev);
     if (M == 0) return PyLong_FromLong(XPRESS_OK);                    // empty tensors have no address
     return PyLong_FromLong(xpress_linear(&g, matmul_workspace(dev), xpress_linear_workspace_size(), st));
@@ -353,6 +399,19 @@ PyObject *sample(PyObject *, PyObject *const *v, Py_ssize_t n)
     if (given(v[8])) g.min_p = static_cast<float *>(vector("min_p", v[8], n_seq, F32, dev));
     g.mask_value = (float)PyFloat_AsDouble(v[9]);
     if (PyErr_Occurred()) return nullptr;
+    const int64_t es = x.element_size();
+    const Place in("logits", g.logits, total, g.ld, V, es), to("out", g.out, total, g.ldo, V, es), tok("tokens_out", g.tokens, total);
+    if (g.out != g.logits) apart(to, in);                            // (one place: the entry point sees to the pitch)
+    apart(tok, in);
+    apart(tok, to);
+    for (const Place &p : {Place("temperature", g.temperature, n_seq), Place("top_k", g.top_k, n_seq), Place("top_p", g.top_p, n_seq),
+                           Place("min_p", g.min_p, n_seq)}) {
+        apart(to, p);
+        if (rows > 1 || p.at != tok.at) apart(tok, p);               // (a row's own are read before its token is written)
+    }
+    const Place u("u", g.u, total);
+    apart(to, u);
+    if (u.at != tok.at) apart(tok, u);
     void *st = current_stream(dev);
     return PyLong_FromLong(total == 0 ? XPRESS_OK : xpress_sample(&g, st));   // empty tensors have no address
     END_HANDLE_TH_ERRORS
