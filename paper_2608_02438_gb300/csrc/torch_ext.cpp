@@ -90,7 +90,7 @@ const at::Tensor &rank2(const char *name, PyObject *o)
 
 int narrow(const char *name, int64_t n)
 {
-    if (n > INT32_MAX) bad_value(name, ": ", n, " is above the supported size");
+    if (n > INT32_MAX || n < INT32_MIN) bad_value(name, ": ", n, " is outside the supported range");
     return (int)n;
 }
 
