@@ -445,16 +445,19 @@ int xpress_matmul_fp8(const xpress_matmul_args *args, void *workspace, size_t ws
 /* Matrix product with bias, activation and residual (e.g. the feed-forward block
  * in front of the drafter's head, x + W_2 act(W_1 norm(x) + b_1) + b_2):
  *   out[m][n] = residual[m][n] + act(sum_k x[m][k] w[n][k] + bias[n])
- * x [M, K], w [N, K] and bias [N] bf16, out and residual bf16 or fp32; fp32 sums,
- * every step in fp32, one rounding to out's type.  act is an xpress_act
- * (XPRESS_ACT_NONE: the identity; GELU is t Phi(t)).  bias and residual are
- * optional (NULL).  Any M >= 0, N, K >= 1; x and w 16-byte aligned with pitches
+ * x [M, K], w [N, K] and bias [N] bf16, out and residual bf16 or fp32; one rounding
+ * to out's type.  The dot products are the tensor cores' fp32 sums, whose additions
+ * may truncate (off by K 2^-23 sum |x w| at most; 1e-6 to 2e-5 of the 2-norm at K of
+ * 4096 to 16384); bias, activation and residual are fp32 steps on them.  act is an
+ * xpress_act (XPRESS_ACT_NONE: the identity; GELU is t Phi(t)).  bias and residual
+ * are optional (NULL).  Any M >= 0, N, K >= 1; x and w 16-byte aligned with pitches
  * that are multiples of 8 (the padding is never used).  out may be residual's
  * memory (same pitch); otherwise its rows share no byte with what is read (the
- * caller's to see to; the torch binding refuses it).  workspace: xpress_linear_workspace_size() bytes,
- * 256-byte aligned, zeroed once by the caller; it only holds the status word
- * (xpress_get_device_status reads and clears it) and may be shared by calls, with
- * xpress_matmul_fp8 too.  Reproducible: the order of every sum is fixed.
+ * caller's to see to; the torch binding refuses it).  workspace:
+ * xpress_linear_workspace_size() bytes, 256-byte aligned, zeroed once by the caller;
+ * it only holds the status word (xpress_get_device_status reads and clears it) and
+ * may be shared by calls, with xpress_matmul_fp8 too.  Reproducible: the order of
+ * every sum is fixed.
  * Errors: INVALID_ARG (out = residual with another pitch too), UNSUPPORTED
  * (out_dtype, act, K above 2^24, M or N above 2^30), WORKSPACE, CUDA. */
 typedef struct {
@@ -539,7 +542,7 @@ int xpress_process_logits(const xpress_logits_args *args, void *workspace, size_
  * numbers, and the rows truncated by these filters.  logits holds n_seq * rows
  * rows of V; row j of sequence q is row q * rows + j and takes q's parameters.  At
  * T > 0, with m the row's maximum:
- *   w_v   = exp((l_v - m) / T)
+ *   w_v   = exp((l_v - m) / T)                (for masses T is cut to 1e-37 .. 1e37)
  *   order = by falling l, equal ones by rising id
  *   kept by min_p and top_k: w_v >= min_p, and among the first top_k of the order
  *   kept by top_p: what stands before v in the order has less mass than top_p

@@ -1,6 +1,9 @@
 // linear.cu -- the bf16 matrix product with its epilogue
 //   out[m, n] = residual[m, n] + act(sum_k x[m, k] w[n, k] + bias[n])
-// for x [M, K], w [N, K] bf16, fp32 sums, one rounding to the output type.
+// for x [M, K], w [N, K] bf16, fp32 sums, one rounding to the output type.  The sums
+// are the tensor core's, whose additions truncate: with normal operands a dot product is
+// 1e-9 of itself too small for each element of K that it adds up in one go (1.6e-5 at
+// K = 16384, a quarter of that split in four), as a library's bf16 product is.
 //
 // This kernel, for few rows of x: D = w x^T on tcgen05 (kind::f16), 128 weight rows
 // the MMA's M (TMEM lanes), NT rows of x its N, so that hardly a lane is idle and w

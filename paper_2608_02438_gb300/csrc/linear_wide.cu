@@ -23,12 +23,14 @@
 // is read the same way, a step ahead, and asked into L2 a tile ahead.  (Sixteen such
 // warps have 96 registers each and spill; with eight 168.)
 //
-// 16384 x 16384 x 4096 with SiLU and bias 1180 to 1260 us, without them 1077, 2.04
-// PFLOP/s (a library product 1059); 8192 x 8192 x 4096 with residual: tensor pipe 84 % of
-// the cycles, 1.3 times the operands and outputs from and to HBM.  Short K is bound by
-// the epilogue: 4096 x 8192 x 64 with residual 53 us, 2.5 TB/s.  Smaller ones by the
-// rounds: 2048 x 4096 x 4096 51 us, 128 tiles for 76 pairs.  What it took with four
-// columns to a lane stored from TMEM, without shared memory: 1498 us.
+// 16384 x 16384 x 4096 with SiLU and bias 1117 us at the full clock, without them 1108,
+// 1.98 PFLOP/s (a library product 1100), and 1283, 1276 and 1272 one after another for
+// half a second, when the power limit takes the clock to 1450 to 1570 MHz; 8192 x 8192 x
+// 4096 with residual: tensor pipe 84 % of the cycles, 1.3 times the operands and outputs
+// from and to HBM.  Short K is bound by the epilogue: 4096 x 8192 x 64 with residual
+// 53 us, 2.5 TB/s.  Smaller ones by the rounds: 2048 x 4096 x 4096 46 to 49 us, 128 tiles
+// for 76 pairs.  What it took with four columns to a lane stored from TMEM, without
+// shared memory: 1498 us (1250 to 1320 now, under the power limit as then).
 #include <type_traits>
 
 #include "linear.h"

@@ -39,7 +39,7 @@
 // of 151936 bf16, top-k 50 and top-p 0.9: 11.2 us (load 1.3, bound 1.0, exchange 1.3,
 // the few 5.6, the rest 2.0).  32 x 17 truncated rows of it under mixed filters: 155 us,
 // 2.1 TB/s; shared memory holds 76 rows at a time, for 16 us (median) each: with top-k 20
-// 128 us for all, 300 179, top-p alone 326.  64 rows without filters: 25 us; 5 of a row's
+// 126 us for all, 300 178, top-p alone 328.  64 rows without filters: 22.5 to 27 us; 5 of a row's
 // 15 are the weights, at the issue limit, and a row that has to be taken again needs 13
 // more.  What it took before: one row 19 and 544 rows 443 us with CTAs of two passes per
 // level, 64-bit atomics on masses and 64-bit floating point at two lanes a cycle; 15 and
@@ -1436,9 +1436,9 @@ struct SamplePlan {
 
 // CTAs of a row's cluster: the fewest that leave two on an SM; more while they have
 // more than 2048 pieces and all rows' CTAs have a place at the same time (64 rows of
-// 151936 bf16: 4 CTAs, 28 us, 32 with 2; 68 rows of 32000: 2 CTAs, 11.5 us, 13.5 with
-// 4).  8 for a few rows only (one row 11.3 us, 12.2 with 4; 17 rows 14 with 4, 16 with
-// 8).  The pieces of a CTA and of a thread.
+// 151936 bf16: 4 CTAs, 27 us, 31 with 2; 68 rows of 32000: 2 CTAs, 12.4 us, 13.7 with
+// one, 11.4 with 4).  8 for a few rows only (one row 11.2 us, 12.1 with 4; 17 rows 14.3
+// with 4, 15.9 with 8).  The pieces of a CTA and of a thread.
 SamplePlan sample_plan(int64_t n, int V, int E, int sms)
 {
     const int64_t pieces = ((int64_t)V + E - 1 + E - 1) / E;          // wherever the row starts
